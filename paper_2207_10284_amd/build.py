@@ -1,5 +1,5 @@
-"""Build libmra.so (the HIP kernels and the C ABI, gfx950) and _binding.so (the
-torch binding of ops.py's calls, host code) in-tree.
+"""Build libmra.so and libmra_exact.so (the HIP kernels and their C ABIs, gfx950)
+and _binding.so (the torch binding of ops.py's calls, host code) in-tree.
 
     python -m paper_2207_10284_amd.build
 
@@ -21,9 +21,11 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libmra.so")
+LIB_EXACT = os.path.join(PKG, "libmra_exact.so")
 BINDING = os.path.join(PKG, "_binding.so")
 SOURCES = ["api.cpp", "pool.hip", "coarse.hip", "select.hip", "select_global.hip", "tile.hip",
            "bwd.hip", "multilevel.hip", "noalloc.hip"]
+EXACT_SOURCES = ["exact_api.cpp", "exact_fwd.hip", "exact_bwd.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
@@ -66,20 +68,27 @@ def _build_binding() -> str:
     return BINDING
 
 
-def build(verbose: bool = False) -> str:
-    os.makedirs(BUILD, exist_ok=True)
-    with cf.ThreadPoolExecutor(max_workers=8) as ex:
-        binding = ex.submit(_build_binding)
-        objs = list(ex.map(_compile, SOURCES))
-        binding.result()
-    tmp = LIB + ".tmp"
+def _link(objs, lib: str) -> None:
+    tmp = lib + ".tmp"
     cmd = [HIPCC, "-shared", "-fPIC", f"--offload-arch={ARCH}", *objs, "-o", tmp]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"link failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
-    os.replace(tmp, LIB)
+    os.replace(tmp, lib)
+
+
+def build(verbose: bool = False) -> str:
+    os.makedirs(BUILD, exist_ok=True)
+    with cf.ThreadPoolExecutor(max_workers=8) as ex:
+        binding = ex.submit(_build_binding)
+        exact = [ex.submit(_compile, s) for s in EXACT_SOURCES]
+        objs = list(ex.map(_compile, SOURCES))
+        exact = [f.result() for f in exact]
+        binding.result()
+    _link(objs, LIB)
+    _link(exact, LIB_EXACT)
     if verbose:
-        print(f"built {LIB} and {BINDING}")
+        print(f"built {LIB}, {LIB_EXACT} and {BINDING}")
     return LIB
 
 

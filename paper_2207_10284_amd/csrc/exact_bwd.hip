@@ -1,0 +1,406 @@
+// Gradients of exact softmax attention (mra_exact.h). The probabilities are formed
+// again from the forward's log normalisers, P_ij = exp(S_ij - L_i), in two passes that
+// each own what they sum, so no sum depends on the order of workgroups:
+//
+// exact_dq_kernel: a wave owns 32 queries of one head and walks the keys:
+//   delta_i = G_i . Z_i (also written for the second pass), D_ij = P_ij (G_i . v_j - delta_i),
+//   dQ_i = scale sum_j D_ij k_j; with a position bias the sums of D over the diagonals.
+//   S^T = K Q^T and V G^T leave a lane 16 keys of one query, the B operand of
+//   dQ^T += K^T D^T.
+// exact_dkv_kernel: a wave owns 32 keys of one key head and walks the queries of its
+//   heads: S = Q K^T and G V^T leave a lane 16 queries of one key, the B operands of
+//   dV^T += G^T P and dK^T += Q^T D.
+// S and dP are formed in both: seven products instead of five, but no atomic sums
+// and no partial dQ of n_k / 32 times the size.
+//
+// exact_bias_kernel: the diagonal sums of a head's blocks, added and then collected
+// by bucket, in a fixed order.
+#include "exact_tile.h"
+
+namespace mra {
+
+constexpr int kDqRows = kExactWaves * 32;
+
+int exact_dq_blocks(int nq) { return (nq + kDqRows - 1) / kDqRows; }
+// the window's entries, then the sums of the tiles below and above it
+int exact_window(int far) { return window_entries(far) + 2; }
+
+template <int NP, int D, bool BIAS>
+__global__ __launch_bounds__(kExactThreads) void exact_dq_kernel(ExactArgs a, ExactGrads g, int qblocks) {
+  constexpr int KT = kStageRows<NP, D>, TILES = KT / 32, KC = D / 16, NT = D / 32;
+  using St = Stage<NP, D, KT, kExactThreads>;
+  constexpr int STEP = TILES * kTileBytes<D>;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  float* win = reinterpret_cast<float*>(smem + 4 * St::kBytes);
+  const int entries = BIAS ? window_entries(a.far) : 0;
+  // a window of diagonal sums per wave and half wave (the halves' keys are four apart)
+  float* acc = win + entries;
+  const int tid = threadIdx.x, lane = lane_id(), w = wave_uniform(tid / kWave), hf = lane >> 5;
+  const int gi = xcd_remap(blockIdx.x, gridDim.x);
+  const int bh = gi / qblocks, qb = qblocks - 1 - (gi - bh * qblocks);   // causal: the longest first
+  const int b = bh / a.H, h = bh - b * a.H, hk = h / a.group;
+  const int row0 = qb * kDqRows + w * 32, i = row0 + (lane & 31), ic = min(i, a.nq - 1);
+  const int limit = key_limit(a, b), start = first_position(a, b);
+  const int kend = a.causal ? min(limit, start + min((qb + 1) * kDqRows, a.nq)) : limit;
+  const int stages = kend > 0 ? (kend + KT - 1) / KT : 0;
+  const char* kp = a.k.p + b * a.k.sb + hk * a.k.sh;
+  const char* vp = a.v.p + b * a.v.sb + hk * a.v.sh;
+  const int pos0 = start + row0;
+
+  TileAddr<D> at;
+  at.init();
+  u32x4 qf[NP][KC], gf[NP][KC];
+  f32x16 dq[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) dq[t] = splat16(0.0f);
+  load_operand<NP, D>(a.q.p + b * a.q.sb + h * a.q.sh + ic * a.q.sn, i < a.nq, qf);
+  float delta = 0.0f;
+  {
+    constexpr int LB = NP == 1 ? KC : 2 * KC;
+    const int half = hf * (D / 2) * (NP == 1 ? 2 : 4);
+    const u32x4* gr = reinterpret_cast<const u32x4*>(g.dout.p + b * g.dout.sb + h * g.dout.sh + ic * g.dout.sn + half);
+    const u32x4* zr = reinterpret_cast<const u32x4*>(a.out.p + b * a.out.sb + h * a.out.sh + ic * a.out.sn + half);
+#pragma unroll
+    for (int c = 0; c < LB; ++c) {
+      const u32x4 x = gr[c], y = zr[c];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if constexpr (NP == 1) {
+          delta = fmaf(bf16_to_f32(x[e] & 0xFFFFu), bf16_to_f32(y[e] & 0xFFFFu), delta);
+          delta = fmaf(bf16_to_f32(x[e] >> 16), bf16_to_f32(y[e] >> 16), delta);
+        } else {
+          delta = fmaf(__uint_as_float(x[e]), __uint_as_float(y[e]), delta);
+        }
+      }
+    }
+    delta = halves_sum(delta);
+  }
+  load_operand<NP, D>(g.dout.p + b * g.dout.sb + h * g.dout.sh + ic * g.dout.sn, i < a.nq, gf);
+  const long long at_row = (long long)bh * a.nq + ic;
+  const float L = g.lse[at_row];
+  if (lane < 32 && i < a.nq) g.delta[at_row] = delta;
+  // no key counts: no weight; the same for rows past the last
+  const bool none = i >= a.nq || L == -INFINITY;
+  const float nl = none ? -INFINITY : -L * kLog2e;
+  if (none) delta = 0.0f;
+  float lo = 0.0f, hi = 0.0f, sum_lo = 0.0f, sum_hi = 0.0f;
+  float* mine = acc + (w * 2 + hf) * entries;
+  if constexpr (BIAS) {
+    fill_window(a, h, win, tid, kExactThreads);
+    for (int x = tid; x < 2 * kExactWaves * entries; x += kExactThreads) acc[x] = 0.0f;
+    lo = bias_value(a, h, 0) * kLog2e;
+    hi = bias_value(a, h, 2 * a.far) * kLog2e;
+  }
+
+  St ks, vs;
+  uint64_t ok = 0;
+  if (stages > 0) {
+    ks.load(kp, a.k.sn, 0, limit, tid);
+    vs.load(vp, a.v.sn, 0, limit, tid);
+    ok = key_bits<KT>(mask_byte(a, b, 0), 0, limit);
+    ks.store(smem, ok, tid);
+    vs.store(smem + St::kBytes, ok, tid);
+  }
+  __syncthreads();
+  for (int st = 0; st < stages; ++st) {
+    char* cur = smem + (st & 1) * 2 * St::kBytes;
+    const bool more = st + 1 < stages;
+    uint32_t byte = 0;
+    if (more) {
+      ks.load(kp, a.k.sn, (st + 1) * KT, limit, tid);
+      vs.load(vp, a.v.sn, (st + 1) * KT, limit, tid);
+      byte = mask_byte(a, b, (st + 1) * KT);
+    }
+#pragma unroll
+    for (int x = 0; x < TILES; ++x) {
+      const uint32_t kb = (uint32_t)(ok >> (32 * x));
+      const int k0 = st * KT + 32 * x;
+      const uint32_t bits = a.causal ? kb & low_bits(pos0 + (lane & 31) - k0 + 1) : kb;
+      if (__ballot(bits != 0) == 0) continue;
+      char* ktile = cur + x * kTileBytes<D>;
+      f32x16 s = product<NP, D>(at, ktile, STEP, qf, splat16(0.0f));
+      f32x16 dp = product<NP, D>(at, cur + St::kBytes + x * kTileBytes<D>, STEP, gf, splat16(-delta));
+      float mul = a.scale_log2, add = nl;
+      const int d0 = k0 - pos0;
+      BiasKind kind = kBiasNear;
+      const int at_win = d0 + a.far + kWinPad - (lane & 31) + 4 * hf;
+      if constexpr (BIAS) {
+        kind = bias_kind(d0, a.far);
+        if (kind == kBiasNear) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.scale_log2, win[at_win + reg_row(r)]);
+          mul = 1.0f;
+        } else {
+          add = nl + (kind == kBiasLow ? lo : hi);
+        }
+      }
+      if (__ballot(bits != ~0u) != 0) select_rows(s, bits, -INFINITY);
+      float ds[16];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) ds[r] = __builtin_amdgcn_exp2f(fmaf(s[r], mul, add)) * dp[r];
+      if constexpr (BIAS) {
+        if (kind == kBiasNear) {
+          // each lane of a half its own diagonal, so no two lanes of an addition meet; the
+          // additions of one wave are made in their order
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            __hip_atomic_fetch_add(&mine[at_win + reg_row(r)], ds[r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+        } else {
+          float t = 0.0f;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) t += ds[r];
+          if (kind == kBiasLow) sum_lo += t;
+          else sum_hi += t;
+        }
+      }
+      accumulate_t<NP, D>(at, ktile, STEP, pack_weights<NP>(ds), dq);
+    }
+    if (more) {
+      char* nxt = smem + ((st + 1) & 1) * 2 * St::kBytes;
+      ok = key_bits<KT>(byte, (st + 1) * KT, limit);
+      ks.store(nxt, ok, tid);
+      vs.store(nxt + St::kBytes, ok, tid);
+    }
+    __syncthreads();
+  }
+  store_rows<NP, D>(dq, a.scale, g.dq.p + b * g.dq.sb + h * g.dq.sh + ic * g.dq.sn, i < a.nq);
+  if constexpr (BIAS) {
+    if (g.diag == nullptr) return;
+    sum_lo = wave_sum(sum_lo);
+    sum_hi = wave_sum(sum_hi);
+    if (lane == 0) {
+      win[2 * w] = sum_lo;                         // the bias window is idle
+      win[2 * w + 1] = sum_hi;
+    }
+    __syncthreads();
+    const int parts = a.B * qblocks;
+    float* out = g.diag + ((long long)h * parts + (long long)b * qblocks + qb) * (entries + 2);
+    for (int x = tid; x < entries; x += kExactThreads) {
+      float t = 0.0f;
+#pragma unroll
+      for (int p = 0; p < 2 * kExactWaves; ++p) t += acc[p * entries + x];
+      out[x] = t;
+    }
+    if (tid < 2) out[entries + tid] = win[tid] + win[2 + tid] + win[4 + tid] + win[6 + tid];
+  }
+}
+
+template <int NP, int D, bool BIAS>
+__global__ __launch_bounds__(kExactThreads) void exact_dkv_kernel(ExactArgs a, ExactGrads g, int kblocks) {
+  constexpr int QT = kStageRows<NP, D>, TILES = QT / 32, KC = D / 16, NT = D / 32;
+  using St = Stage<NP, D, QT, kExactThreads>;
+  constexpr int STEP = TILES * kTileBytes<D>;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  float* rows = reinterpret_cast<float*>(smem + 4 * St::kBytes);   // [2][2][QT]: -L (log2 units), -delta
+  float* win = rows + 4 * QT;
+  const int tid = threadIdx.x, lane = lane_id(), w = wave_uniform(tid / kWave), hf = lane >> 5;
+  const int gi = xcd_remap(blockIdx.x, gridDim.x);
+  const int bk = gi / kblocks, kblk = gi - bk * kblocks;
+  const int b = bk / a.Hkv, hk = bk - b * a.Hkv;
+  const int block0 = kblk * kExactWaves * 32, k0 = block0 + w * 32, j = k0 + (lane & 31), jc = min(j, a.nk - 1);
+  const int limit = key_limit(a, b), start = first_position(a, b);
+  const bool counts = j < limit && (a.key_mask == nullptr || a.key_mask[(long long)b * a.mask_stride + jc] != 0);
+  const bool any = __ballot(counts) != 0;          // of the wave's keys
+
+  TileAddr<D> at;
+  at.init();
+  u32x4 kf[NP][KC], vf[NP][KC];
+  load_operand<NP, D>(a.k.p + b * a.k.sb + hk * a.k.sh + jc * a.k.sn, counts, kf);
+  load_operand<NP, D>(a.v.p + b * a.v.sb + hk * a.v.sh + jc * a.v.sn, counts, vf);
+  f32x16 dk[NT], dv[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) dk[t] = dv[t] = splat16(0.0f);
+
+  // causal: the first query whose position reaches the block's first key
+  const int first = a.causal ? min(max(block0 - start, 0), a.nq) / QT * QT : 0;
+  const int stages = block0 < limit ? (a.nq - first + QT - 1) / QT : 0;   // per head
+  for (int hg = 0; hg < a.group && stages > 0; ++hg) {
+    const int h = hk * a.group + hg;
+    const char* qp = a.q.p + b * a.q.sb + h * a.q.sh;
+    const char* gp = g.dout.p + b * g.dout.sb + h * g.dout.sh;
+    const long long lrow = ((long long)b * a.H + h) * a.nq;
+    float lo = 0.0f, hi = 0.0f;
+    if constexpr (BIAS) {
+      fill_window(a, h, win, tid, kExactThreads);
+      lo = bias_value(a, h, 0) * kLog2e;
+      hi = bias_value(a, h, 2 * a.far) * kLog2e;
+    }
+    St qs, gs;
+    float nl = 0.0f, nd = 0.0f;                    // of query tid of the stage
+    auto load = [&](int q0) {
+      qs.load(qp, a.q.sn, q0, a.nq, tid);
+      gs.load(gp, g.dout.sn, q0, a.nq, tid);
+      if (tid < QT) {
+        const int q = min(q0 + tid, a.nq - 1);
+        const float L = g.lse[lrow + q];
+        const bool none = q0 + tid >= a.nq || L == -INFINITY;
+        nl = none ? -INFINITY : -L * kLog2e;
+        nd = none ? 0.0f : -g.delta[lrow + q];
+      }
+    };
+    auto store = [&](int buf, int q0) {
+      const uint64_t ok = key_bits<QT>(1, q0, a.nq);
+      qs.store(smem + buf * 2 * St::kBytes, ok, tid);
+      gs.store(smem + buf * 2 * St::kBytes + St::kBytes, ok, tid);
+      if (tid < QT) {
+        rows[buf * 2 * QT + tid] = nl;
+        rows[buf * 2 * QT + QT + tid] = nd;
+      }
+    };
+    load(first);
+    store(0, first);
+    __syncthreads();
+    for (int st = 0; st < stages; ++st) {
+      const int buf = st & 1, q0 = first + st * QT;
+      char* cur = smem + buf * 2 * St::kBytes;
+      const bool more = st + 1 < stages;
+      if (more) load(q0 + QT);
+#pragma unroll
+      for (int x = 0; x < TILES; ++x) {
+        const int p0 = start + q0 + 32 * x;        // position of the tile's first query
+        const int live = a.nq - q0 - 32 * x;       // queries of the tile
+        if (!any || live <= 0) continue;
+        // queries whose position reaches this lane's key
+        const uint32_t bits = a.causal ? ~low_bits(j - p0) : ~0u;
+        if (__ballot(bits != 0) == 0) continue;
+        const float* nlr = rows + buf * 2 * QT + 32 * x + 4 * hf;
+        f32x16 c;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const f32x4 v = *reinterpret_cast<const f32x4*>(nlr + QT + 8 * q);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) c[4 * q + e] = v[e];
+        }
+        char *qtile = cur + x * kTileBytes<D>, *gtile = cur + St::kBytes + x * kTileBytes<D>;
+        f32x16 s = product<NP, D>(at, qtile, STEP, kf, splat16(0.0f));
+        const f32x16 dp = product<NP, D>(at, gtile, STEP, vf, c);
+        float mul = a.scale_log2, add = 0.0f;
+        if constexpr (BIAS) {
+          const int d0 = k0 - p0;
+          const BiasKind kind = bias_kind(d0, a.far);
+          if (kind == kBiasNear) {
+            const float* wp = win + (d0 + a.far + kWinPad + (lane & 31) - 4 * hf);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.scale_log2, wp[-reg_row(r)]);
+            mul = 1.0f;
+          } else {
+            add = kind == kBiasLow ? lo : hi;
+          }
+        }
+        if (__ballot(bits != ~0u) != 0) select_rows(s, bits, -INFINITY);
+        float p[16];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const f32x4 v = *reinterpret_cast<const f32x4*>(nlr + 8 * q);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) p[4 * q + e] = __builtin_amdgcn_exp2f(fmaf(s[4 * q + e], mul, v[e] + add));
+        }
+        accumulate_t<NP, D>(at, gtile, STEP, pack_weights<NP>(p), dv);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) p[r] *= dp[r];
+        accumulate_t<NP, D>(at, qtile, STEP, pack_weights<NP>(p), dk);
+      }
+      if (more) store(buf ^ 1, q0 + QT);
+      __syncthreads();
+    }
+  }
+  // a key that does not count has no gradient (its column of P is not one)
+  if (!counts) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t) dk[t] = dv[t] = splat16(0.0f);
+  }
+  store_rows<NP, D>(dk, a.scale, g.dk.p + b * g.dk.sb + hk * g.dk.sh + jc * g.dk.sn, j < a.nk);
+  store_rows<NP, D>(dv, 1.0f, g.dv.p + b * g.dv.sb + hk * g.dv.sh + jc * g.dv.sn, j < a.nk);
+}
+
+// dbias: a workgroup per head. Threads (entry, part group) sum the diagonal sums of
+// the head's blocks in double, then a thread per bucket collects the entries that
+// the map sends there, ascending.
+constexpr int kBiasThreads = 1024;
+constexpr int kMaxEntries = window_entries(MRA_EXACT_MAX_FAR) + 2;
+__global__ __launch_bounds__(kBiasThreads) void exact_bias_kernel(ExactArgs a, const float* __restrict__ diag, int parts,
+                                                                  void* __restrict__ dbias) {
+  __shared__ double tot[kMaxEntries];
+  __shared__ int bucket[kMaxEntries];
+  __shared__ double part[kBiasThreads];
+  const int h = blockIdx.x, tid = threadIdx.x, entries = window_entries(a.far) + 2;
+  const float* src = diag + (long long)h * parts * entries;
+  int cols = 64;                                   // entries at a time
+  while (cols < entries && cols < kBiasThreads) cols *= 2;
+  const int groups = kBiasThreads / cols, grp = tid / cols;
+  for (int e0 = 0; e0 < entries; e0 += cols) {
+    const int e = e0 + tid % cols;
+    double t = 0.0;
+    if (e < entries)
+      for (int p = grp; p < parts; p += groups) t += (double)src[(long long)p * entries + e];
+    part[tid] = t;
+    __syncthreads();
+    if (grp == 0 && e < entries) {
+      for (int q = 1; q < groups; ++q) t += part[q * cols + tid];
+      tot[e] = t;
+      const int d = e < entries - 2 ? min(max(e - kWinPad, 0), 2 * a.far) : (e == entries - 2 ? 0 : 2 * a.far);
+      bucket[e] = a.map[d];
+    }
+    __syncthreads();
+  }
+  for (int c = tid; c < a.buckets; c += kBiasThreads) {
+    double t = 0.0;
+    for (int e = 0; e < entries; ++e)
+      if (bucket[e] == c) t += tot[e];
+    const long long at = (long long)c * a.H + h;
+    if (a.bias_bf16) static_cast<uint16_t*>(dbias)[at] = (uint16_t)f32_to_bf16_rne((float)t);
+    else static_cast<float*>(dbias)[at] = (float)t;
+  }
+}
+
+template <class Kernel>
+static hipError_t allow_lds(Kernel kernel, size_t smem) {
+  if (smem <= 65536) return hipSuccess;
+  return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+}
+
+template <int NP, int D, bool BIAS>
+static hipError_t backward_case(const ExactArgs& a, const ExactGrads& g, hipStream_t stream) {
+  constexpr size_t stage = 4 * Stage<NP, D, kStageRows<NP, D>, kExactThreads>::kBytes;
+  const size_t entries = BIAS ? window_entries(a.far) : 0;
+  const int qblocks = exact_dq_blocks(a.nq);
+  if (a.nq > 0) {
+    const size_t smem = stage + (1 + 2 * kExactWaves) * entries * sizeof(float);
+    auto kernel = exact_dq_kernel<NP, D, BIAS>;
+    hipError_t e = allow_lds(kernel, smem);
+    if (e != hipSuccess) return e;
+    kernel<<<(unsigned)((long long)a.B * a.H * qblocks), kExactThreads, smem, stream>>>(a, g, qblocks);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  if (a.nk > 0) {
+    const size_t smem = stage + (4 * kStageRows<NP, D> + entries) * sizeof(float);
+    auto kernel = exact_dkv_kernel<NP, D, BIAS>;
+    hipError_t e = allow_lds(kernel, smem);
+    if (e != hipSuccess) return e;
+    const int kblocks = (a.nk + kExactWaves * 32 - 1) / (kExactWaves * 32);
+    kernel<<<(unsigned)((long long)a.B * a.Hkv * kblocks), kExactThreads, smem, stream>>>(a, g, kblocks);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+hipError_t launch_exact_backward(const ExactArgs& a, const ExactGrads& g, int d, int dtype, hipStream_t stream) {
+  auto pick = [&](auto np, auto dd) {
+    constexpr int NP = decltype(np)::value, D = decltype(dd)::value;
+    return a.bias != nullptr ? backward_case<NP, D, true>(a, g, stream) : backward_case<NP, D, false>(a, g, stream);
+  };
+  auto width = [&](auto np) {
+    if (d == 32) return pick(np, std::integral_constant<int, 32>{});
+    if (d == 64) return pick(np, std::integral_constant<int, 64>{});
+    return pick(np, std::integral_constant<int, 128>{});
+  };
+  if (a.B > 0 && a.H > 0) {
+    const hipError_t e = dtype == BF16 ? width(std::integral_constant<int, 1>{}) : width(std::integral_constant<int, 3>{});
+    if (e != hipSuccess) return e;
+  }
+  if (g.dbias != nullptr && a.H > 0)
+    exact_bias_kernel<<<a.H, kBiasThreads, 0, stream>>>(a, g.diag, a.B * exact_dq_blocks(a.nq), g.dbias);
+  return hipGetLastError();
+}
+
+}  // namespace mra

@@ -1,0 +1,453 @@
+// Exact softmax attention, forward (mra_exact.h): Z = softmax(S) V with
+// S = scale Q K^T + position bias over the keys that count, in one pass over the
+// keys with a running reference and sum per query.
+//
+// As in the tile pass of MRA-2 (tile.hip) S is formed transposed, S^T = K Q^T, so
+// a lane holds 16 key scores of one query, which are already the B operand of
+// O^T += V^T P^T: weights never move between lanes.
+//
+// exact_fwd_kernel: a workgroup's four waves take 32 QT queries each of one
+// head and walk the keys together, a stage of K and V rows in LDS at a time (two
+// buffers, one barrier per stage); the next stage's rows are on their way to
+// registers meanwhile.
+//
+// exact_split_kernel: few rows. The workgroup's four waves share 32 rows (the
+// queries of all heads of one key head, so a token's heads are one tile) and take
+// every fourth tile of 32 keys; several workgroups may share the rows too, each
+// with a contiguous part of the keys, and leave partial sums that
+// exact_join_kernel adds.
+#include "exact_tile.h"
+
+namespace mra {
+
+// Reference of a query's weights exp2(S - ref) (log2 units), as in tile.hip: any
+// works that keeps weights and sums finite. It is the max of the first tile that
+// has a key plus kMargin. A tile whose weights sum to more than kCap in some lane
+// moves the references of its queries to its own max plus kMargin and forms its
+// weights again, so an ordinary tile has no max, no exchange between lanes and no
+// rescaling. The largest weight of a query stays above 2^-(kMargin + 1).
+constexpr float kMargin = 16.0f;
+constexpr float kCap = 0x1p32f;
+
+template <int NP, int D>
+struct FwdRow {
+  static constexpr int NT = D / 32, KC = D / 16;
+  u32x4 qf[NP][KC];
+  f32x16 o[NT];
+  float ref, sum;
+
+  __device__ __forceinline__ void init() {
+#pragma unroll
+    for (int t = 0; t < NT; ++t) o[t] = splat16(0.0f);
+    ref = -INFINITY;
+    sum = 0.0f;
+  }
+
+  // weights exp2(s mul + c) and their sum (bfloat16: of the rounded weights)
+  __device__ __forceinline__ float weights(const f32x16& s, float mul, float c, Packed<NP>& w) const {
+    float p[16], t = 0.0f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(fmaf(s[r], mul, c));
+    w = pack_weights<NP>(p);
+    if constexpr (NP == 1) {
+      const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          t = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, (uint32_t)w.w[0][u][e]), ones, t, false);
+    } else {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) t += p[r];
+    }
+    return t;
+  }
+
+  // Scores s of a tile in units where s mul + add are log2 logits (-inf: does not count)
+  __device__ __forceinline__ void add_tile(f32x16 s, float mul, float add, const TileAddr<D>& at, char* vtile, int vstep) {
+    Packed<NP> w;
+    float t = weights(s, mul, add - ref, w);
+    if (__ballot(!(t <= kCap)) != 0) {             // also a query's first tile (ref -inf)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], mul, add);
+      float mx = s[0];
+#pragma unroll
+      for (int r = 1; r < 16; ++r) mx = __builtin_elementwise_maximum(mx, s[r]);
+      mx = halves_max(mx);
+      const float next = mx > ref ? mx + kMargin : ref;
+      const float f = next == ref ? 1.0f : __builtin_amdgcn_exp2f(ref - next);
+#pragma unroll
+      for (int x = 0; x < NT; ++x)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[x][r] *= f;
+      sum *= f;
+      ref = next;
+      t = weights(s, 1.0f, ref == -INFINITY ? 0.0f : -ref, w);
+    }
+    sum += t;
+    accumulate_t<NP, D>(at, vtile, vstep, w, o);
+  }
+};
+
+// The scores of a tile with bias and masks: s, mul and add of add_tile. d0: the
+// distance of the tile's first key and this wave's first query; dq: this lane's
+// query behind that one; bits: this lane's keys that count; lo, hi: the outer biases.
+template <bool BIAS>
+__device__ __forceinline__ void finish_scores(f32x16& s, float& mul, float& add, float sl2, uint32_t bits, int d0,
+                                              int far, const float* win, float lo, float hi) {
+  mul = sl2;
+  add = 0.0f;
+  if constexpr (BIAS) {
+    const BiasKind kind = bias_kind(d0, far);      // wave-uniform
+    if (kind == kBiasNear) {
+      const int lane = lane_id();
+      const float* w = win + (d0 + far + kWinPad - (lane & 31) + 4 * (lane >> 5));
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], sl2, w[reg_row(r)]);
+      mul = 1.0f;
+    } else {
+      add = kind == kBiasLow ? lo : hi;
+    }
+  }
+  if (__ballot(bits != ~0u) != 0) select_rows(s, bits, -INFINITY);
+}
+
+template <int NP, int D, int QT, bool BIAS>
+__global__ __launch_bounds__(kExactThreads) void exact_fwd_kernel(ExactArgs a, float* __restrict__ lse, int qblocks) {
+  constexpr int KT = kStageRows<NP, D>, TILES = KT / 32;
+  using St = Stage<NP, D, KT, kExactThreads>;
+  constexpr int STEP = TILES * kTileBytes<D>;      // bytes from one plane to the next
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  float* win = reinterpret_cast<float*>(smem + 4 * St::kBytes);
+  const int tid = threadIdx.x, lane = lane_id(), w = wave_uniform(tid / kWave);
+  const int g = xcd_remap(blockIdx.x, gridDim.x);
+  // causal rows take the longer the later they are: the last blocks of a head first
+  const int bh = g / qblocks, qb = qblocks - 1 - (g - bh * qblocks);
+  const int b = bh / a.H, h = bh - b * a.H, hk = h / a.group;
+  const int row0 = (qb * kExactWaves + w) * 32 * QT;
+  const int limit = key_limit(a, b), start = first_position(a, b);
+  const int last = min((qb + 1) * kExactWaves * 32 * QT, a.nq) - 1;   // the block's last query
+  const int kend = a.causal ? min(limit, start + last + 1) : limit;
+  const int stages = kend > 0 ? (kend + KT - 1) / KT : 0;
+  const char* kp = a.k.p + b * a.k.sb + hk * a.k.sh;
+  const char* vp = a.v.p + b * a.v.sb + hk * a.v.sh;
+
+  TileAddr<D> at;
+  at.init();
+  FwdRow<NP, D> row[QT];
+  int pos0[QT];
+#pragma unroll
+  for (int x = 0; x < QT; ++x) {
+    const int i = row0 + 32 * x + (lane & 31);
+    load_operand<NP, D>(a.q.p + b * a.q.sb + h * a.q.sh + min(i, a.nq - 1) * a.q.sn, i < a.nq, row[x].qf);
+    row[x].init();
+    pos0[x] = start + row0 + 32 * x;
+  }
+  float lo = 0.0f, hi = 0.0f;
+  if constexpr (BIAS) {
+    fill_window(a, h, win, tid, kExactThreads);
+    lo = bias_value(a, h, 0) * kLog2e;
+    hi = bias_value(a, h, 2 * a.far) * kLog2e;
+  }
+
+  St ks, vs;
+  uint64_t ok = 0;
+  if (stages > 0) {
+    ks.load(kp, a.k.sn, 0, limit, tid);
+    vs.load(vp, a.v.sn, 0, limit, tid);
+    ok = key_bits<KT>(mask_byte(a, b, 0), 0, limit);
+    ks.store(smem, ok, tid);
+    vs.store(smem + St::kBytes, ok, tid);
+  }
+  __syncthreads();
+  for (int st = 0; st < stages; ++st) {
+    char* cur = smem + (st & 1) * 2 * St::kBytes;
+    const bool more = st + 1 < stages;
+    uint32_t byte = 0;
+    if (more) {
+      ks.load(kp, a.k.sn, (st + 1) * KT, limit, tid);
+      vs.load(vp, a.v.sn, (st + 1) * KT, limit, tid);
+      byte = mask_byte(a, b, (st + 1) * KT);
+    }
+#pragma unroll
+    for (int i = 0; i < TILES; ++i) {
+      const uint32_t kb = (uint32_t)(ok >> (32 * i));
+      const int k0 = st * KT + 32 * i;
+      if (kb == 0) continue;
+#pragma unroll
+      for (int x = 0; x < QT; ++x) {
+        // keys up to this lane's position
+        const uint32_t bits = a.causal ? kb & low_bits(pos0[x] + (lane & 31) - k0 + 1) : kb;
+        if (__ballot(bits != 0) == 0) continue;
+        f32x16 s = product<NP, D>(at, cur + i * kTileBytes<D>, STEP, row[x].qf, splat16(0.0f));
+        float mul, add;
+        finish_scores<BIAS>(s, mul, add, a.scale_log2, bits, k0 - pos0[x], a.far, win, lo, hi);
+        row[x].add_tile(s, mul, add, at, cur + St::kBytes + i * kTileBytes<D>, STEP);
+      }
+    }
+    if (more) {
+      char* nxt = smem + ((st + 1) & 1) * 2 * St::kBytes;
+      ok = key_bits<KT>(byte, (st + 1) * KT, limit);
+      ks.store(nxt, ok, tid);
+      vs.store(nxt + St::kBytes, ok, tid);
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int x = 0; x < QT; ++x) {
+    const int i = row0 + 32 * x + (lane & 31);
+    const float den = halves_sum(row[x].sum);
+    store_rows<NP, D>(row[x].o, den > 0.0f ? 1.0f / den : 0.0f,
+                      a.out.p + b * a.out.sb + h * a.out.sh + min(i, a.nq - 1) * a.out.sn, i < a.nq);
+    if (lse != nullptr && lane < 32 && i < a.nq)
+      lse[(long long)bh * a.nq + i] = den > 0.0f ? (log2f(den) + row[x].ref) * kLn2 : -INFINITY;
+  }
+}
+
+// Row m of a key head's queries: query m / group of head hk group + m % group.
+template <int NP, int D, bool BIAS>
+__global__ __launch_bounds__(kExactThreads) void exact_split_kernel(ExactArgs a, float* __restrict__ lse, int mtiles,
+                                                                    int splits, float* __restrict__ part_o,
+                                                                    float* __restrict__ part_l) {
+  using St = Stage<NP, D, 32, kWave>;
+  constexpr int NT = D / 32;
+  constexpr int SLOT = St::kBytes;                 // a wave's tile: K, then V
+  constexpr int MERGE = 32 * D * 4;                // a wave's accumulators
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  __shared__ float refs[kExactWaves][kWave], sums[kExactWaves][kWave];
+  const int lane = lane_id(), w = wave_uniform(threadIdx.x / kWave);
+  const int g = xcd_remap(blockIdx.x, gridDim.x);
+  const int sp = g % splits, mt = g / splits % mtiles, bk = g / splits / mtiles;
+  const int b = bk / a.Hkv, hk = bk - b * a.Hkv;
+  const int rows = a.nq * a.group;
+  const int m = mt * 32 + (lane & 31), mc = min(m, rows - 1);
+  const int i = mc / a.group, h = hk * a.group + (mc - i * a.group);
+  const int limit = key_limit(a, b), start = first_position(a, b);
+  const int pos = start + i, last = start + min(mt * 32 + 31, rows - 1) / a.group;
+  const int kend = a.causal ? min(limit, last + 1) : limit;
+  const int tiles = kend > 0 ? (kend + 31) / 32 : 0;
+  const int t0 = (int)((long long)tiles * sp / splits), t1 = (int)((long long)tiles * (sp + 1) / splits);
+  const char* kp = a.k.p + b * a.k.sb + hk * a.k.sh;
+  const char* vp = a.v.p + b * a.v.sb + hk * a.v.sh;
+  char* slot = smem + w * SLOT;
+
+  TileAddr<D> at;
+  at.init();
+  FwdRow<NP, D> row;
+  load_operand<NP, D>(a.q.p + b * a.q.sb + h * a.q.sh + i * a.q.sn, m < rows, row.qf);
+  row.init();
+  float lo = 0.0f, hi = 0.0f;
+  if constexpr (BIAS) {
+    lo = bias_value(a, h, 0) * kLog2e;
+    hi = bias_value(a, h, 2 * a.far) * kLog2e;
+  }
+  St ks, vs;
+  uint32_t byte = 0;
+  int t = t0 + w;
+  if (t < t1) {
+    ks.load(kp, a.k.sn, t * 32, limit, lane);
+    vs.load(vp, a.v.sn, t * 32, limit, lane);
+    byte = mask_byte(a, b, t * 32);
+  }
+  for (; t < t1; t += kExactWaves) {
+    const int k0 = t * 32;
+    const uint64_t ok = key_bits<32>(byte, k0, limit);
+    ks.store(slot, ok, lane);
+    wave_lds_sync();
+    const bool more = t + kExactWaves < t1;
+    if (more) ks.load(kp, a.k.sn, k0 + 32 * kExactWaves, limit, lane);
+    f32x16 s = product<NP, D>(at, slot, kTileBytes<D>, row.qf, splat16(0.0f));
+    wave_lds_sync();
+    vs.store(slot, ok, lane);
+    wave_lds_sync();
+    if (more) {
+      vs.load(vp, a.v.sn, k0 + 32 * kExactWaves, limit, lane);
+      byte = mask_byte(a, b, k0 + 32 * kExactWaves);
+    }
+    const uint32_t kb = (uint32_t)ok, bits = a.causal ? kb & low_bits(pos - k0 + 1) : kb;
+    if (__ballot(bits != 0) != 0) {
+      float mul = a.scale_log2, add = 0.0f;
+      if constexpr (BIAS) {
+        // rows of several heads and queries: every lane has its own distances, d of its first key
+        const int d = k0 - pos, r4 = 4 * (lane >> 5);
+        const bool below = d + 31 <= -a.far, above = d >= a.far;
+        if (__ballot(!(below || above)) == 0) {
+          add = below ? lo : hi;
+        } else {
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            s[r] = fmaf(s[r], a.scale_log2,
+                        bias_value(a, h, min(max(d + r4 + reg_row(r), -a.far), a.far) + a.far) * kLog2e);
+          mul = 1.0f;
+        }
+      }
+      if (__ballot(bits != ~0u) != 0) select_rows(s, bits, -INFINITY);
+      row.add_tile(s, mul, add, at, slot, kTileBytes<D>);
+    }
+    wave_lds_sync();
+  }
+  // the waves' sums relative to the largest reference, added in wave order
+  float sum = halves_sum(row.sum);
+  refs[w][lane] = row.ref;
+  sums[w][lane] = sum;
+  __syncthreads();                                 // the slots are idle
+  float top = refs[0][lane];
+#pragma unroll
+  for (int x = 1; x < kExactWaves; ++x) top = fmaxf(top, refs[x][lane]);
+  auto factor = [&](float ref) { return ref == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ref - top); };
+  const float f = factor(row.ref);
+#pragma unroll
+  for (int x = 0; x < NT; ++x)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) row.o[x][r] *= f;
+  if (w != 0) {
+    f32x4* to = reinterpret_cast<f32x4*>(smem + (w - 1) * MERGE) + lane;
+#pragma unroll
+    for (int x = 0; x < NT; ++x)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        to[(4 * x + q) * kWave] = f32x4{row.o[x][4 * q], row.o[x][4 * q + 1], row.o[x][4 * q + 2], row.o[x][4 * q + 3]};
+  }
+  __syncthreads();
+  if (w != 0) return;
+  sum *= f;
+#pragma unroll
+  for (int p = 1; p < kExactWaves; ++p) {
+    sum += sums[p][lane] * factor(refs[p][lane]);
+    const f32x4* from = reinterpret_cast<const f32x4*>(smem + (p - 1) * MERGE) + lane;
+#pragma unroll
+    for (int x = 0; x < NT; ++x)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const f32x4 v = from[(4 * x + q) * kWave];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) row.o[x][4 * q + e] += v[e];
+      }
+  }
+  if (splits == 1) {
+    store_rows<NP, D>(row.o, sum > 0.0f ? 1.0f / sum : 0.0f, a.out.p + b * a.out.sb + h * a.out.sh + i * a.out.sn,
+                      m < rows);
+    if (lse != nullptr && lane < 32 && m < rows)
+      lse[((long long)b * a.H + h) * a.nq + i] = sum > 0.0f ? (log2f(sum) + top) * kLn2 : -INFINITY;
+    return;
+  }
+  const long long pr = ((long long)sp * a.B * a.Hkv + bk) * rows + mc;   // the partial row
+  store_rows<3, D>(row.o, 1.0f, reinterpret_cast<char*>(part_o + pr * D), m < rows);
+  if (lane < 32 && m < rows) {
+    part_l[2 * pr] = top;
+    part_l[2 * pr + 1] = sum;
+  }
+}
+
+// Adds the partial rows of `splits` workgroups, in their order: a thread per
+// four columns of a row.
+template <int NP, int D>
+__global__ __launch_bounds__(256) void exact_join_kernel(ExactArgs a, float* __restrict__ lse, int splits,
+                                                         const float* __restrict__ part_o,
+                                                         const float* __restrict__ part_l) {
+  constexpr int L = D / 4;
+  const int rows = a.nq * a.group;
+  const long long all = (long long)a.B * a.Hkv * rows;
+  const long long pr = (long long)blockIdx.x * (256 / L) + threadIdx.x / L;
+  const int c = threadIdx.x % L;
+  if (pr >= all) return;
+  float top = -INFINITY;
+  for (int s = 0; s < splits; ++s) top = fmaxf(top, part_l[2 * (s * all + pr)]);
+  float sum = 0.0f;
+  f32x4 z = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+  for (int s = 0; s < splits; ++s) {
+    const float ref = part_l[2 * (s * all + pr)], l = part_l[2 * (s * all + pr) + 1];
+    const f32x4 o = *reinterpret_cast<const f32x4*>(part_o + (s * all + pr) * D + 4 * c);
+    const float f = ref == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ref - top);
+    sum += l * f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) z[e] = fmaf(o[e], f, z[e]);
+  }
+  const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+  const long long bk = pr / rows;
+  const int m = (int)(pr - bk * rows), i = m / a.group, b = (int)(bk / a.Hkv);
+  const int h = (int)(bk - (long long)b * a.Hkv) * a.group + (m - i * a.group);
+  const float out[4] = {z[0] * inv, z[1] * inv, z[2] * inv, z[3] * inv};
+  store4<NP>(a.out.p + b * a.out.sb + h * a.out.sh + i * a.out.sn + 4 * c * (NP == 1 ? 2 : 4), out);
+  if (lse != nullptr && c == 0)
+    lse[((long long)b * a.H + h) * a.nq + i] = sum > 0.0f ? (log2f(sum) + top) * kLn2 : -INFINITY;
+}
+
+// The split kernel serves calls whose 128-row workgroups would leave most of the
+// chip idle; its workgroups are at least two per CU where the keys allow, each
+// with at least two tiles per wave.
+SplitPlan exact_split_plan(const mra_exact_problem_t& p) {
+  SplitPlan s{};
+  const long long heads = (long long)p.B * p.H, kheads = (long long)p.B * p.H_kv;
+  const long long blocks = heads * ((p.n_q + 127) / 128);
+  const long long rows = (long long)p.n_q * (p.H / p.H_kv);
+  s.mtiles = (int)((rows + 31) / 32);
+  s.splits = 1;
+  s.use = blocks < kCus && rows < (1 << 20);
+  if (s.use) {
+    const long long wgs = kheads * s.mtiles, most = (p.n_k + 255) / 256;
+    long long want = (2 * kCus + wgs - 1) / wgs;
+    if (want > most) want = most;
+    if (want > 64) want = 64;
+    if (want > 1) s.splits = (int)want;
+    if (s.splits > 1) s.bytes = (size_t)s.splits * kheads * rows * (p.d + 2) * sizeof(float);
+  }
+  return s;
+}
+
+template <int NP, int D, bool BIAS>
+static hipError_t forward_case(const ExactArgs& a, float* lse, const SplitPlan& plan, void* ws, hipStream_t stream) {
+  if (plan.use) {
+    using St = Stage<NP, D, 32, kWave>;
+    constexpr int slots = kExactWaves * St::kBytes, merge = (kExactWaves - 1) * 32 * D * 4;
+    constexpr size_t smem = slots > merge ? slots : merge;
+    const long long rows = (long long)a.B * a.Hkv * a.nq * a.group;
+    float* part_o = static_cast<float*>(ws);
+    float* part_l = part_o + (plan.splits > 1 ? plan.splits * rows * D : 0);
+    const unsigned wgs = (unsigned)((long long)a.B * a.Hkv * plan.mtiles * plan.splits);
+    auto kernel = exact_split_kernel<NP, D, BIAS>;
+    if (smem > 65536) {
+      const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                                               hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+      if (e != hipSuccess) return e;
+    }
+    kernel<<<wgs, kExactThreads, smem, stream>>>(a, lse, plan.mtiles, plan.splits, part_o, part_l);
+    if (plan.splits > 1) {
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+      constexpr int per = 256 / (D / 4);
+      exact_join_kernel<NP, D><<<(unsigned)((rows + per - 1) / per), 256, 0, stream>>>(a, lse, plan.splits, part_o, part_l);
+    }
+    return hipGetLastError();
+  }
+  constexpr int QT = 1;
+  const int qblocks = (a.nq + kExactWaves * 32 * QT - 1) / (kExactWaves * 32 * QT);
+  const size_t smem = 4 * Stage<NP, D, kStageRows<NP, D>, kExactThreads>::kBytes +
+                      (BIAS ? window_entries(a.far) * sizeof(float) : 0);
+  auto kernel = exact_fwd_kernel<NP, D, QT, BIAS>;
+  if (smem > 65536) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                                             hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != hipSuccess) return e;
+  }
+  kernel<<<(unsigned)((long long)a.B * a.H * qblocks), kExactThreads, smem, stream>>>(a, lse, qblocks);
+  return hipGetLastError();
+}
+
+hipError_t launch_exact_forward(const ExactArgs& a, int d, int dtype, float* lse, const SplitPlan& plan, void* ws,
+                                hipStream_t stream) {
+  auto pick = [&](auto np, auto dd) {
+    constexpr int NP = decltype(np)::value, D = decltype(dd)::value;
+    return a.bias != nullptr ? forward_case<NP, D, true>(a, lse, plan, ws, stream)
+                             : forward_case<NP, D, false>(a, lse, plan, ws, stream);
+  };
+  auto width = [&](auto np) {
+    if (d == 32) return pick(np, std::integral_constant<int, 32>{});
+    if (d == 64) return pick(np, std::integral_constant<int, 64>{});
+    return pick(np, std::integral_constant<int, 128>{});
+  };
+  return dtype == BF16 ? width(std::integral_constant<int, 1>{}) : width(std::integral_constant<int, 3>{});
+}
+
+}  // namespace mra

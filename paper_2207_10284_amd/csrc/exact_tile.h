@@ -1,0 +1,332 @@
+// Device code shared by the exact-attention kernels: staging of 32-row tiles
+// in LDS, matrix-core operands and products, masks and the position bias.
+//
+// Operands are NP bfloat16 planes: one for bfloat16 tensors, three whose sum
+// the value is for float32 ones (tile_ops.h). A tile is 32 rows x D of one plane,
+// row-major under the swizzle of the gradient passes, which serves row and
+// transposed reads without bank conflicts. Rows go from global memory through
+// registers, where rows that do not count become zero (what they hold may be
+// anything) and float32 values are split, once per workgroup instead of once per
+// wave that reads them.
+#pragma once
+
+#include "common.h"
+#include "exact_kernels.h"
+#include "tile_ops.h"
+
+namespace mra {
+
+constexpr int kExactWaves = 4;                     // waves per workgroup
+constexpr int kExactThreads = kExactWaves * kWave;
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) char* lds_ptr;
+
+template <int D>
+__host__ __device__ constexpr int exact_swz(int r) {
+  return D == 128 ? 4 * (r & 3) + ((r >> 2) & 3) : (D == 64 ? 4 * ((r >> 1) & 1) + ((r >> 2) & 3) : (r >> 2) & 3);
+}
+
+template <int D>
+constexpr int kTileBytes = 64 * D;                 // 32 rows of one plane
+
+// Rows per stage of the workgroup's shared loops.
+template <int NP, int D>
+constexpr int kStageRows = NP == 1 || D == 32 ? 64 : 32;
+
+// R rows of D elements moved by T threads from global memory to LDS tiles: plane
+// p of rows 32 i .. 32 i + 31 at (p R/32 + i) kTileBytes. Loads go to registers
+// (load), so that their latency passes during the previous stage's products;
+// store() writes them.
+template <int NP, int D, int R, int T>
+struct Stage {
+  static constexpr int CPR = D / 8;                // units of eight elements per row
+  static constexpr int N = R * CPR / T;
+  static constexpr int LB = NP == 1 ? 1 : 2;       // 16-byte loads per unit
+  static constexpr int kBytes = NP * R * D * 2;
+  static_assert(N >= 1 && R * CPR % T == 0, "whole units per thread");
+  u32x4 v[N][LB];
+
+  // rows row0 .. row0 + R - 1; those at or past limit (> 0) repeat row limit - 1
+  __device__ __forceinline__ void load(const char* base, long long sn, int row0, int limit, int tid) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int u = i * T + tid, r = min(row0 + u / CPR, limit - 1);
+      const u32x4* src = reinterpret_cast<const u32x4*>(base + (long long)r * sn) + (u % CPR) * LB;
+#pragma unroll
+      for (int e = 0; e < LB; ++e) v[i][e] = src[e];
+    }
+  }
+
+  // bit r of `ok`: row r counts (others become zero)
+  __device__ __forceinline__ void store(char* lds, uint64_t ok, int tid) {
+    constexpr uint64_t all = R == 64 ? ~uint64_t(0) : (uint64_t(1) << (R & 63)) - 1;
+    if (ok != all) {                               // wave-uniform
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int r = (i * T + tid) / CPR;
+        const uint32_t keep = (ok >> r) & 1 ? ~0u : 0u;
+#pragma unroll
+        for (int e = 0; e < LB; ++e)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) v[i][e][x] &= keep;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int u = i * T + tid, r = u / CPR;
+      char* dst = lds + (r >> 5) * kTileBytes<D> + raw_offset<D, exact_swz<D>>(r & 31, 8 * (u % CPR));
+      if constexpr (NP == 1) {
+        *reinterpret_cast<u32x4*>(dst) = v[i][0];
+      } else {
+        float f[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(v[i][e / 4][e % 4]);
+        u32x4 pl[3];
+        split8(f, pl);
+#pragma unroll
+        for (int p = 0; p < 3; ++p) *reinterpret_cast<u32x4*>(dst + p * (R / 32) * kTileBytes<D>) = pl[p];
+      }
+    }
+  }
+};
+
+// This lane's operand addresses within a tile.
+template <int D>
+struct TileAddr {
+  static constexpr int KC = D / 16, NT = D / 32;
+  int rr[KC];                                      // row-layout chunk c: row l%32, columns (D/2)(l/32) + 8c ..
+  int tr[NT][2];                                   // transposed column tile t, rows + 0 and + 8
+  __device__ __forceinline__ void init() {
+    const int lane = lane_id(), h = lane >> 5, j = lane & 31, i16 = lane & 15;
+#pragma unroll
+    for (int c = 0; c < KC; ++c) rr[c] = raw_offset<D, exact_swz<D>>(j, (D / 2) * h + 8 * c);
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        tr[t][e] = raw_offset<D, exact_swz<D>>(4 * h + i16 / 4 + 8 * e, 32 * t + 16 * ((lane >> 4) & 1) + 4 * (i16 & 3));
+  }
+  __device__ __forceinline__ u32x4 row(const char* tile, int c) const {
+    return *reinterpret_cast<const u32x4*>(tile + rr[c]);
+  }
+  // transposed chunk (u, t): rows 16u + 8(s/4) + 4(l/32) + s%4 (s = 0..7) of column 32t + l%32
+  __device__ __forceinline__ u32x4 trans(char* tile, int u, int t) const {
+    u32x2 x[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+      x[e] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                           (__attribute__((address_space(3))) s16x4*)(tile + tr[t][e] + 16 * u * 2 * D)));
+    return u32x4{x[0][0], x[0][1], x[1][0], x[1][1]};
+  }
+};
+
+__device__ __forceinline__ f32x16 mfma16(const u32x4& a, const u32x4& b, const f32x16& c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+__device__ __forceinline__ f32x16 splat16(float x) {
+  f32x16 s;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) s[r] = x;
+  return s;
+}
+
+// A row of D elements as this lane's part of a B operand (row l%32's half l/32),
+// in planes; `on` false: zeros.
+template <int NP, int D>
+__device__ __forceinline__ void load_operand(const char* row, bool on, u32x4 (&f)[NP][D / 16]) {
+  constexpr int KC = D / 16;
+  const char* p = row + (lane_id() >> 5) * (D / 2) * (NP == 1 ? 2 : 4);
+  if constexpr (NP == 1) {
+#pragma unroll
+    for (int c = 0; c < KC; ++c) f[0][c] = on ? reinterpret_cast<const u32x4*>(p)[c] : u32x4{0, 0, 0, 0};
+  } else {
+    u32x4 raw[2 * KC];
+#pragma unroll
+    for (int c = 0; c < 2 * KC; ++c) raw[c] = on ? reinterpret_cast<const u32x4*>(p)[c] : u32x4{0, 0, 0, 0};
+    split_chunks(raw, f);
+  }
+}
+
+// c + A B^T over the D columns: A the rows of the staged tile (plane 0 at `tile`,
+// planes `step` bytes apart), B this lane's operand; the smallest plane products first.
+template <int NP, int D>
+__device__ __forceinline__ f32x16 product(const TileAddr<D>& at, const char* tile, int step, const u32x4 (&b)[NP][D / 16],
+                                          f32x16 c) {
+#pragma unroll
+  for (int p = NP - 1; p >= 0; --p)
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) {
+      const u32x4 a = at.row(tile + p * step, k);
+#pragma unroll
+      for (int q = NP - 1 - p; q >= 0; --q) c = mfma16(a, b[q][k], c);
+    }
+  return c;
+}
+
+// The 16 weights of a lane as the planes of the next product's B operand.
+template <int NP>
+struct Packed {
+  u32x4 w[NP][2];
+};
+template <int NP>
+__device__ __forceinline__ Packed<NP> pack_weights(const float (&p)[16]) {
+  Packed<NP> k;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    if constexpr (NP == 1) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        bf16x2 b;
+        b[0] = (__bf16)p[8 * u + 2 * e];
+        b[1] = (__bf16)p[8 * u + 2 * e + 1];
+        k.w[0][u][e] = __builtin_bit_cast(uint32_t, b);
+      }
+    } else {
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = p[8 * u + e];
+      u32x4 pl[3];
+      split8(v, pl);
+#pragma unroll
+      for (int q = 0; q < 3; ++q) k.w[q][u] = pl[q];
+    }
+  }
+  return k;
+}
+
+// o (D rows x 32 columns) += X^T W: X the staged tile, W packed weights.
+template <int NP, int D>
+__device__ __forceinline__ void accumulate_t(const TileAddr<D>& at, char* tile, int step, const Packed<NP>& w,
+                                             f32x16 (&o)[D / 32]) {
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+      for (int p = NP - 1; p >= 0; --p) {
+        const u32x4 x = at.trans(tile + p * step, u, t);
+#pragma unroll
+        for (int q = NP - 1 - p; q >= 0; --q) o[t] = mfma16(x, w.w[q][u], o[t]);
+      }
+}
+
+// Register r of a product holds row 8(r/4) + 4(l/32) + r%4 of its 32.
+__device__ __forceinline__ constexpr int reg_row(int r) { return 8 * (r >> 2) + (r & 3); }
+
+// s where this lane's bit of the row is set, else x; `bits` by row.
+__device__ __forceinline__ void select_rows(f32x16& s, uint32_t bits, float x) {
+  const uint32_t m = bits >> (4 * (lane_id() >> 5));
+#pragma unroll
+  for (int r = 0; r < 16; ++r) s[r] = (m >> reg_row(r)) & 1 ? s[r] : x;
+}
+
+// The lowest n bits (n may be negative or above 32).
+__device__ __forceinline__ uint32_t low_bits(int n) {
+  return n >= 32 ? ~0u : (n <= 0 ? 0u : (1u << n) - 1);
+}
+
+__device__ __forceinline__ int key_limit(const ExactArgs& a, int b) {
+  return a.lengths == nullptr ? a.nk : min(max(a.lengths[b], 0), a.nk);
+}
+
+// Position of query 0 of batch b.
+__device__ __forceinline__ int first_position(const ExactArgs& a, int b) {
+  constexpr int kFar = 1 << 29;
+  return a.q_start == nullptr ? a.nk - a.nq : min(max(a.q_start[b], -kFar), kFar);
+}
+
+// This lane's byte of the mask of the R keys from k0 on (nonzero: counts); a
+// lane past them repeats a valid one.
+__device__ __forceinline__ uint32_t mask_byte(const ExactArgs& a, int b, int k0) {
+  if (a.key_mask == nullptr) return 1;
+  return a.key_mask[(long long)b * a.mask_stride + min(k0 + lane_id(), a.nk - 1)];
+}
+
+// Bits of the keys k0 .. k0 + R - 1 that count.
+template <int R>
+__device__ __forceinline__ uint64_t key_bits(uint32_t byte, int k0, int limit) {
+  const int lane = lane_id();
+  return __ballot(lane < R && k0 + lane < limit && byte != 0);
+}
+
+__device__ __forceinline__ float bias_value(const ExactArgs& a, int h, int entry) {
+  const int e = a.map[entry];
+  if ((unsigned)e >= (unsigned)a.buckets) return 0.0f;
+  const long long at = (long long)e * a.H + h;
+  return a.bias_bf16 ? bf16_to_f32(static_cast<const uint16_t*>(a.bias)[at]) : static_cast<const float*>(a.bias)[at];
+}
+
+// The position bias of a 32 x 32 tile depends on key - position only, 63
+// distances. Where all of them are at most -far or at least far it is one
+// number (one of the outer entries); the rest read it from a window in LDS: entry
+// far + kWinPad + distance, which such a tile never leaves.
+constexpr int kWinPad = 64;
+__host__ __device__ constexpr int window_entries(int far) { return 2 * far + 2 * kWinPad; }
+
+// Fills the window (log2 units) with T threads; the caller synchronises.
+__device__ __forceinline__ void fill_window(const ExactArgs& a, int h, float* win, int tid, int threads) {
+  for (int i = tid; i < window_entries(a.far); i += threads)
+    win[i] = bias_value(a, h, min(max(i - kWinPad, 0), 2 * a.far)) * kLog2e;
+}
+
+enum BiasKind { kBiasNear = 0, kBiasLow = 1, kBiasHigh = 2 };
+
+// d0: the distance of the tile's first key and first query.
+__device__ __forceinline__ BiasKind bias_kind(int d0, int far) {
+  if (d0 + 31 <= -far) return kBiasLow;
+  if (d0 - 31 >= far) return kBiasHigh;
+  return kBiasNear;
+}
+
+// bfloat16 or float32 elements of four consecutive columns
+template <int NP>
+__device__ __forceinline__ void store4(char* dst, const float (&z)[4]) {
+  if constexpr (NP == 1) {
+    bf16x2 lo, hi;
+    lo[0] = (__bf16)z[0]; lo[1] = (__bf16)z[1];
+    hi[0] = (__bf16)z[2]; hi[1] = (__bf16)z[3];
+    *reinterpret_cast<u32x2*>(dst) = u32x2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+  } else {
+    *reinterpret_cast<f32x4*>(dst) = f32x4{z[0], z[1], z[2], z[3]};
+  }
+}
+
+// Stores the transposed accumulators o (column l%32 = a row of the result), times
+// f, to the row at `row` if `on` (every lane takes part in the exchange: lanes l
+// and l^32 hold four columns of two groups each and store eight of one, 16 bytes).
+template <int NP, int D>
+__device__ __forceinline__ void store_rows(const f32x16 (&o)[D / 32], float f, char* row, bool on) {
+  const int h = lane_id() >> 5;
+#pragma unroll
+  for (int t = 0; t < D / 32; ++t) {
+    if constexpr (NP == 1) {
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        u32x2 pr[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          bf16x2 lo, hi;
+          lo[0] = (__bf16)(o[t][8 * g + 4 * e] * f); lo[1] = (__bf16)(o[t][8 * g + 4 * e + 1] * f);
+          hi[0] = (__bf16)(o[t][8 * g + 4 * e + 2] * f); hi[1] = (__bf16)(o[t][8 * g + 4 * e + 3] * f);
+          pr[e] = u32x2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+        }
+        const u32x2 send = h ? pr[0] : pr[1];
+        u32x2 recv;
+        recv[0] = (uint32_t)__shfl_xor((int)send[0], 32);
+        recv[1] = (uint32_t)__shfl_xor((int)send[1], 32);
+        const u32x4 st = h ? u32x4{recv[0], recv[1], pr[1][0], pr[1][1]} : u32x4{pr[0][0], pr[0][1], recv[0], recv[1]};
+        if (on) *reinterpret_cast<u32x4*>(row + 2 * (32 * t + 16 * g + 8 * h)) = st;
+      }
+    } else {
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const float z[4] = {o[t][4 * g] * f, o[t][4 * g + 1] * f, o[t][4 * g + 2] * f, o[t][4 * g + 3] * f};
+        if (on) store4<3>(row + 4 * (32 * t + 8 * g + 4 * h), z);
+      }
+    }
+  }
+}
+
+}  // namespace mra

@@ -9,10 +9,16 @@ library is not built, ``load`` raises, and these calls do if the binding is not.
 
 Shapes: q, k, v are [B, H, n, d] tensors on a ROCm device, float32 or
 bfloat16, contiguous; n is a multiple of 32 and d is 32, 64 or 128.
+
+``exact_attention`` and its parts are the softmax attention that MRA-2
+approximates (C ABI in include/mra_exact.h, a library of its own): any lengths,
+strided tensors, padded and causal batches, shared key heads, a learned
+position bias, single tokens.
 """
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import torch
@@ -485,3 +491,283 @@ def mra_attention(q, k, v, budget: int, variant: str = "mra2", prior_diagonal: b
             and not torch.compiler.is_compiling()):
         return bind().mra_attention(q, k, v, budget, _VARIANTS.index(variant), bool(prior_diagonal))
     return MraAttention.apply(q, k, v, budget, variant, prior_diagonal)
+
+
+# ---------------------------------------------------------------------------
+# Exact softmax attention (include/mra_exact.h)
+EXACT_LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libmra_exact.so")
+MAX_FAR = 512                 # distances with a bucket of their own on either side
+MAX_BUCKETS = 1024
+
+
+class _Strided(ctypes.Structure):
+    _fields_ = [("data", _P), ("stride_b", ctypes.c_int64), ("stride_h", ctypes.c_int64),
+                ("stride_n", ctypes.c_int64)]
+
+
+class _Problem(ctypes.Structure):
+    _fields_ = [("B", _I), ("H", _I), ("H_kv", _I), ("n_q", _I), ("n_k", _I), ("d", _I), ("dtype", _I),
+                ("scale", ctypes.c_float), ("causal", _I), ("lengths", _P), ("q_start", _P), ("key_mask", _P),
+                ("key_mask_stride", ctypes.c_int64), ("bias", _P), ("bias_dtype", _I), ("buckets", _I),
+                ("bucket_map", _P), ("far", _I)]
+
+
+# name -> (restype, argtypes); mirrors include/mra_exact.h
+EXACT_SIGNATURES = {
+    "mra_exact_forward_workspace_bytes": (_Z, [_P]),
+    "mra_exact_forward": (_I, [_P] * 7 + [_Z, _P]),
+    "mra_exact_backward_workspace_bytes": (_Z, [_P]),
+    "mra_exact_backward": (_I, [_P] * 12 + [_Z, _P]),
+    "mra_exact_last_hip_error": (_I, []),
+}
+
+_exact_lib = None
+
+
+class _ExactStatus:
+    """What MraError asks of a library: the shared status texts, this library's HIP error."""
+
+    def mra_status_str(self, status):
+        return load().mra_status_str(status)
+
+    def mra_last_hip_error(self):
+        return load_exact().mra_exact_last_hip_error()
+
+
+def load_exact(path: str = EXACT_LIB_PATH):
+    """Open libmra_exact.so once and declare its signatures. Raises if it is missing."""
+    global _exact_lib
+    if _exact_lib is None:
+        if not os.path.exists(path):
+            raise RuntimeError(f"{path} is not built; run `python -m paper_2207_10284_amd.build` "
+                               "(hipcc, gfx950) first")
+        lib = ctypes.CDLL(path)
+        for name, (res, args) in EXACT_SIGNATURES.items():
+            fn = getattr(lib, name)
+            fn.restype, fn.argtypes = res, args
+        _exact_lib = lib
+    return _exact_lib
+
+
+def _call_exact(name: str, *args):
+    st = getattr(load_exact(), name)(*args)
+    if st != 0:
+        raise MraError(name, st, _ExactStatus())
+
+
+@functools.lru_cache(maxsize=64)
+def _bucket_row(num_buckets: int, max_distance: int, bidirectional: bool):
+    if num_buckets < (4 if bidirectional else 2) or (bidirectional and num_buckets % 2) or num_buckets > MAX_BUCKETS:
+        raise ValueError(f"num_buckets must be 2 to {MAX_BUCKETS} (4 or more, and even, for both directions)")
+    n = num_buckets // 2 if bidirectional else num_buckets
+    e = n // 2
+    if max_distance <= e:
+        raise ValueError(f"max_distance must be above {e}, the distances with a bucket of their own")
+    # floor((n - e) log(r / e) / log(max_distance / e)) >= t as a comparison of whole
+    # numbers, so that distances on a border fall where the formula says
+    lefts = [max_distance ** t * e ** (n - e) for t in range(n - e)]
+
+    def bucket(r):
+        if r < e:
+            return r
+        t = 0
+        while t < n - e - 1 and r ** (n - e) * e ** (t + 1) >= lefts[t + 1]:
+            t += 1
+        return e + t
+
+    side = []
+    while not side or side[-1] != n - 1:
+        side.append(bucket(len(side)))
+        if len(side) > MAX_FAR + 1:
+            raise ValueError(f"the last bucket may begin at distance {MAX_FAR} at most")
+    back = side[:0:-1]                                       # keys before the query, the farthest first
+    return tuple(back + [0] + ([n + x for x in side[1:]] if bidirectional else [0] * len(back)))
+
+
+def distance_buckets(num_buckets: int, max_distance: int, bidirectional: bool = True, device="cuda"):
+    """The map of a learned position bias: int32 [2 far + 1], the bucket of each
+    distance key - query from -far to far; beyond, the outer buckets hold. Each
+    direction has num_buckets / 2 of them (one direction: all; later keys then
+    share bucket 0 with distance 0). Half of a direction's buckets hold one
+    distance each; from there on the width grows by a constant factor: distance
+    r >= e has bucket e + floor((n - e) log(r / e) / log(max_distance / e)), at
+    most n - 1. Any other map of whole numbers in this form serves as well."""
+    return torch.tensor(_bucket_row(int(num_buckets), int(max_distance), bool(bidirectional)), dtype=torch.int32,
+                        device=device)
+
+
+def _strides(t):
+    """Element strides of the outer three axes (0 where an axis has at most one entry)."""
+    return tuple(st if n > 1 else 0 for st, n in zip(t.stride()[:3], t.shape[:3]))
+
+
+def _dense_rows(t) -> bool:
+    per = 16 // t.element_size()
+    return (t.stride(3) == 1 and t.data_ptr() % 16 == 0 and all(st % per == 0 for st in _strides(t))) or t.numel() == 0
+
+
+def _check_rows(t, ref, shape, name):
+    if not t.is_cuda:
+        raise ValueError("tensors must be on a ROCm device")
+    if tuple(t.shape) != tuple(shape) or t.dtype != ref.dtype or t.device != ref.device:
+        raise ValueError(f"{name} must be a {ref.dtype} tensor of shape {tuple(shape)} on {ref.device}")
+    if not _dense_rows(t):
+        raise ValueError(f"{name} must have dense rows, 16-byte aligned")
+
+
+def _view(t):
+    return _Strided(t.data_ptr(), *_strides(t))
+
+
+def _rows_like(t):
+    """An output for t: its layout where that has dense rows."""
+    o = torch.empty_like(t)
+    return o if _dense_rows(o) else torch.empty(t.shape, dtype=t.dtype, device=t.device)
+
+
+def _check_int(t, shape, name, device):
+    if t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"{name} must be a contiguous int32 tensor of shape {shape} on {device}")
+
+
+def _exact_problem(q, k, v, scale, causal, lengths, key_mask, q_start, bias, buckets):
+    if not (q.is_cuda and k.is_cuda and v.is_cuda):
+        raise ValueError("tensors must be on a ROCm device")
+    if q.dim() != 4 or k.dim() != 4 or v.dim() != 4:
+        raise ValueError("q, k, v must have shape [B, heads, n, d]")
+    code = _dtype_code(q)
+    B, H, nq, d = q.shape
+    Hkv, nk = k.shape[1], k.shape[2]
+    if k.shape != (B, Hkv, nk, d) or v.shape != k.shape or (H % Hkv if Hkv else H):
+        raise ValueError("k, v must share shape [B, H_kv, n_k, d] with q's B and d, H a multiple of H_kv")
+    for t, name in ((q, "q"), (k, "k"), (v, "v")):
+        _check_rows(t, q, t.shape, name)
+    dev = q.device
+    if lengths is not None:
+        _check_int(lengths, (B,), "lengths", dev)
+    if q_start is not None:
+        _check_int(q_start, (B,), "q_start", dev)
+    if key_mask is not None and (key_mask.dtype not in (torch.bool, torch.uint8) or key_mask.shape != (B, nk)
+                                 or (nk > 1 and key_mask.stride(1) != 1) or key_mask.device != dev):
+        raise ValueError(f"key_mask must be a bool or uint8 tensor of shape {(B, nk)} with dense rows on {dev}")
+    if (bias is None) != (buckets is None):
+        raise ValueError("bias and buckets go together")
+    far = num = 0
+    if bias is not None:
+        if bias.dim() != 2 or bias.shape[1] != H or bias.dtype not in (q.dtype, torch.float32) \
+                or not bias.is_contiguous() or bias.device != dev:
+            raise ValueError(f"bias must be a contiguous tensor of shape [buckets, {H}], float32 or q's dtype, on {dev}")
+        if buckets.dim() != 1 or buckets.numel() % 2 != 1:
+            raise ValueError("buckets must be int32 of odd length (see distance_buckets)")
+        _check_int(buckets, tuple(buckets.shape), "buckets", dev)
+        num, far = bias.shape[0], buckets.numel() // 2
+    return _Problem(B, H, Hkv, nq, nk, d, code, d ** -0.5 if scale is None else float(scale), int(bool(causal)),
+                    _ptr(lengths), _ptr(q_start), _ptr(key_mask),
+                    key_mask.stride(0) if key_mask is not None and B > 1 else 0, _ptr(bias),
+                    _dtype_code(bias) if bias is not None else 0, num, _ptr(buckets), far)
+
+
+def _exact_workspace(name, p, workspace, device):
+    need = int(getattr(load_exact(), name)(ctypes.byref(p)))
+    if workspace is None and need:
+        workspace = torch.empty(need, device=device, dtype=torch.uint8)
+    return workspace, 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def exact_attention_forward(q, k, v, *, scale=None, causal: bool = False, lengths=None, key_mask=None, q_start=None,
+                            bias=None, buckets=None, out=None, lse_out=None, workspace=None):
+    """Softmax attention softmax(scale q k^T + bias) v, [B, H, n_q, d]; query head
+    h reads key head h // (H / H_kv).
+
+    q: [B, H, n_q, d]; k, v: [B, H_kv, n_k, d], any strides with dense 16-byte
+    aligned rows. ``scale``: 1 / sqrt(d) if not given; positive. Query i stands
+    at position ``q_start[b] + i`` (int32 [B]; n_k - n_q + i if not given). A key j
+    counts if j < ``lengths[b]`` (int32 [B]), ``key_mask[b, j]`` (bool or uint8
+    [B, n_k]) and, with ``causal``, j is at most the position; each only where
+    given. What lies at other keys may be anything; a query for which no key
+    counts gives zeros. ``bias`` ([buckets, H], float32 or q's dtype) adds
+    bias[buckets[distance], h] for the distance j - position (``buckets``: see
+    ``distance_buckets``). ``lse_out`` (float32 [B, H, n_q]) receives the log
+    normalisers. A call whose ``workspace`` (uint8) a graph captured must not run
+    beside another with the same one."""
+    p = _exact_problem(q, k, v, scale, causal, lengths, key_mask, q_start, bias, buckets)
+    if out is None:
+        out = _rows_like(q)
+    else:
+        _check_rows(out, q, q.shape, "out")
+    if lse_out is not None:
+        _check_f32(lse_out, q.shape[:3], "lse_out")
+        if lse_out.device != q.device:
+            raise ValueError(f"lse_out must be on {q.device}")
+    with torch.cuda.device(q.device):
+        workspace, size = _exact_workspace("mra_exact_forward_workspace_bytes", p, workspace, q.device)
+        _call_exact("mra_exact_forward", ctypes.byref(p), *(ctypes.byref(_view(t)) for t in (q, k, v, out)),
+                    _ptr(lse_out), _ptr(workspace), size, _stream(q.device))
+    return out
+
+
+def exact_attention_backward(q, k, v, out, dout, lse, *, scale=None, causal: bool = False, lengths=None,
+                             key_mask=None, q_start=None, bias=None, buckets=None, dq=None, dk=None, dv=None,
+                             dbias=None, workspace=None):
+    """Gradients (dq, dk, dv, dbias; the last None without a bias) of one
+    ``exact_attention_forward`` with the same arguments: ``out`` and ``lse`` are
+    its results, ``dout`` the gradient of the output. The probabilities are formed
+    again from the log normalisers. The same bits every time."""
+    p = _exact_problem(q, k, v, scale, causal, lengths, key_mask, q_start, bias, buckets)
+    _check_rows(out, q, q.shape, "out")
+    _check_rows(dout, q, q.shape, "dout")
+    _check_f32(lse, q.shape[:3], "lse")
+    if lse.device != q.device:
+        raise ValueError(f"lse must be on {q.device}")
+    grads = []
+    for t, g, name in ((q, dq, "dq"), (k, dk, "dk"), (v, dv, "dv")):
+        if g is None:
+            g = _rows_like(t)
+        else:
+            _check_rows(g, t, t.shape, name)
+        grads.append(g)
+    if bias is None and dbias is not None:
+        raise ValueError("dbias without a bias")
+    if bias is not None:
+        if dbias is None:
+            dbias = torch.empty_like(bias)
+        elif dbias.shape != bias.shape or dbias.dtype != bias.dtype or dbias.device != bias.device \
+                or not dbias.is_contiguous():
+            raise ValueError("dbias must be like bias")
+    with torch.cuda.device(q.device):
+        workspace, size = _exact_workspace("mra_exact_backward_workspace_bytes", p, workspace, q.device)
+        _call_exact("mra_exact_backward", ctypes.byref(p), *(ctypes.byref(_view(t)) for t in (q, k, v, out, dout)),
+                    _ptr(lse), *(ctypes.byref(_view(t)) for t in grads), _ptr(dbias), _ptr(workspace), size,
+                    _stream(q.device))
+    return (*grads, dbias)
+
+
+class ExactAttention(torch.autograd.Function):
+    """``exact_attention_forward`` as a differentiable op of q, k, v and bias."""
+
+    @staticmethod
+    def forward(ctx, q, k, v, bias, buckets, lengths, key_mask, q_start, scale, causal):
+        lse = torch.empty(q.shape[:3], device=q.device, dtype=torch.float32)
+        out = exact_attention_forward(q, k, v, scale=scale, causal=causal, lengths=lengths, key_mask=key_mask,
+                                      q_start=q_start, bias=bias, buckets=buckets, lse_out=lse)
+        ctx.save_for_backward(q, k, v, out, lse, bias, buckets, lengths, key_mask, q_start)
+        ctx.scale, ctx.causal = scale, causal
+        return out
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dout):
+        q, k, v, out, lse, bias, buckets, lengths, key_mask, q_start = ctx.saved_tensors
+        if not _dense_rows(dout):
+            dout = dout.contiguous()
+        dq, dk, dv, dbias = exact_attention_backward(q, k, v, out, dout, lse, scale=ctx.scale, causal=ctx.causal,
+                                                     lengths=lengths, key_mask=key_mask, q_start=q_start, bias=bias,
+                                                     buckets=buckets)
+        return dq, dk, dv, dbias, None, None, None, None, None, None
+
+
+def exact_attention(q, k, v, *, scale=None, causal: bool = False, lengths=None, key_mask=None, q_start=None,
+                    bias=None, buckets=None):
+    """Differentiable exact softmax attention (arguments and result as
+    ``exact_attention_forward``), with gradients of q, k, v and bias."""
+    return ExactAttention.apply(q, k, v, bias, buckets, lengths, key_mask, q_start, scale, causal)
