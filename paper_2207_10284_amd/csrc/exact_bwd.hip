@@ -13,13 +13,15 @@
 // S and dP are formed in both: seven products instead of five, but no atomic sums
 // and no partial dQ of n_k / 32 times the size.
 //
-// exact_bias_kernel: the diagonal sums of a head's blocks, added and then collected
-// by bucket, in a fixed order.
+// exact_bias_kernel: the diagonal sums of a head's blocks, added by bucket in a fixed
+// order.
 #include "exact_tile.h"
 
 namespace mra {
 
 constexpr int kDqRows = kExactWaves * 32;
+// floats of a wave's skewed tile (32 rows of 64: see exact_dq_kernel)
+constexpr int kSkew = 32 * 64;
 
 int exact_dq_blocks(int nq) { return (nq + kDqRows - 1) / kDqRows; }
 // the window's entries, then the sums of the tiles below and above it
@@ -33,8 +35,7 @@ __global__ __launch_bounds__(kExactThreads) void exact_dq_kernel(ExactArgs a, Ex
   extern __shared__ __attribute__((aligned(16))) char smem[];
   float* win = reinterpret_cast<float*>(smem + 4 * St::kBytes);
   const int entries = BIAS ? window_entries(a.far) : 0;
-  // a window of diagonal sums per wave and half wave (the halves' keys are four apart)
-  float* acc = win + entries;
+  float* acc = win + entries;                      // a window of diagonal sums per wave
   const int tid = threadIdx.x, lane = lane_id(), w = wave_uniform(tid / kWave), hf = lane >> 5;
   const int gi = xcd_remap(blockIdx.x, gridDim.x);
   const int bh = gi / qblocks, qb = qblocks - 1 - (gi - bh * qblocks);   // causal: the longest first
@@ -84,13 +85,40 @@ __global__ __launch_bounds__(kExactThreads) void exact_dq_kernel(ExactArgs a, Ex
   const float nl = none ? -INFINITY : -L * kLog2e;
   if (none) delta = 0.0f;
   float lo = 0.0f, hi = 0.0f, sum_lo = 0.0f, sum_hi = 0.0f;
-  float* mine = acc + (w * 2 + hf) * entries;
+  float* mine = acc + w * entries;
+  float* skew = acc + kExactWaves * entries + w * kSkew;
   if constexpr (BIAS) {
     fill_window(a, h, win, tid, kExactThreads);
-    for (int x = tid; x < 2 * kExactWaves * entries; x += kExactThreads) acc[x] = 0.0f;
+    for (int x = tid; x < kExactWaves * (entries + kSkew); x += kExactThreads) acc[x] = 0.0f;
     lo = bias_value(a, h, 0) * kLog2e;
     hi = bias_value(a, h, 2 * a.far) * kLog2e;
   }
+
+  // G V^T - delta. The matrix cores' additions fall a little below the exact sum (5e-8 on
+  // average where the sum is about 11), and an offset common to a query's keys does not
+  // vanish in the bias gradient, where the D of many queries meet, whose sums over all keys
+  // are 0. With a bias, float32 takes half of the columns with the opposite sign (gf holds
+  // them so) and subtracts; delta is subtracted last, so that both halves start alike. Error of
+  // dbias (2-norm), 2 heads x 1503 x 128, buckets (32, 128): 5.7e-6 -> 1.3e-6.
+  constexpr bool kTwoSigns = BIAS && NP == 3;
+  if constexpr (kTwoSigns) {
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+#pragma unroll
+      for (int c = KC / 2; c < KC; ++c) gf[p][c] ^= 0x80008000u;
+  }
+  auto values_product = [&](const char* vtile) -> f32x16 {
+    if constexpr (kTwoSigns) {
+      const f32x16 x = product_part<NP, D, 0, KC / 2>(at, vtile, STEP, gf, splat16(0.0f));
+      const f32x16 y = product_part<NP, D, KC / 2, KC>(at, vtile, STEP, gf, splat16(0.0f));
+      f32x16 z;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) z[r] = (x[r] - y[r]) - delta;
+      return z;
+    } else {
+      return product<NP, D>(at, vtile, STEP, gf, splat16(-delta));
+    }
+  };
 
   St ks, vs;
   uint64_t ok = 0;
@@ -119,7 +147,7 @@ __global__ __launch_bounds__(kExactThreads) void exact_dq_kernel(ExactArgs a, Ex
       if (__ballot(bits != 0) == 0) continue;
       char* ktile = cur + x * kTileBytes<D>;
       f32x16 s = product<NP, D>(at, ktile, STEP, qf, splat16(0.0f));
-      f32x16 dp = product<NP, D>(at, cur + St::kBytes + x * kTileBytes<D>, STEP, gf, splat16(-delta));
+      const f32x16 dp = values_product(cur + St::kBytes + x * kTileBytes<D>);
       float mul = a.scale_log2, add = nl;
       const int d0 = k0 - pos0;
       BiasKind kind = kBiasNear;
@@ -140,11 +168,16 @@ __global__ __launch_bounds__(kExactThreads) void exact_dq_kernel(ExactArgs a, Ex
       for (int r = 0; r < 16; ++r) ds[r] = __builtin_amdgcn_exp2f(fmaf(s[r], mul, add)) * dp[r];
       if constexpr (BIAS) {
         if (kind == kBiasNear) {
-          // each lane of a half its own diagonal, so no two lanes of an addition meet; the
-          // additions of one wave are made in their order
+          // row query, column key - query + 31: the diagonals are columns, a lane each
+          float* to = skew + 63 * (lane & 31) + 31 + 4 * hf;
 #pragma unroll
-          for (int r = 0; r < 16; ++r)
-            __hip_atomic_fetch_add(&mine[at_win + reg_row(r)], ds[r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+          for (int r = 0; r < 16; ++r) to[reg_row(r)] = ds[r];
+          wave_lds_sync();
+          float t[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+          for (int q = 0; q < 32; ++q) t[q & 3] += skew[64 * q + lane];
+          mine[d0 + a.far + kWinPad - 31 + lane] += (t[0] + t[1]) + (t[2] + t[3]);
+          wave_lds_sync();
         } else {
           float t = 0.0f;
 #pragma unroll
@@ -178,7 +211,7 @@ __global__ __launch_bounds__(kExactThreads) void exact_dq_kernel(ExactArgs a, Ex
     for (int x = tid; x < entries; x += kExactThreads) {
       float t = 0.0f;
 #pragma unroll
-      for (int p = 0; p < 2 * kExactWaves; ++p) t += acc[p * entries + x];
+      for (int p = 0; p < kExactWaves; ++p) t += acc[p * entries + x];
       out[x] = t;
     }
     if (tid < 2) out[entries + tid] = win[tid] + win[2 + tid] + win[4 + tid] + win[6 + tid];
@@ -313,43 +346,54 @@ __global__ __launch_bounds__(kExactThreads) void exact_dkv_kernel(ExactArgs a, E
   store_rows<NP, D>(dv, 1.0f, g.dv.p + b * g.dv.sb + hk * g.dv.sh + jc * g.dv.sn, j < a.nk);
 }
 
-// dbias: a workgroup per head. Threads (entry, part group) sum the diagonal sums of
-// the head's blocks in double, then a thread per bucket collects the entries that
-// the map sends there, ascending.
-constexpr int kBiasThreads = 1024;
+// dbias: a workgroup per head and bucket. It lists the window's entries that the map
+// sends to its bucket, and its threads sum them over the head's blocks in double.
+constexpr int kBiasThreads = 256;
 constexpr int kMaxEntries = window_entries(MRA_EXACT_MAX_FAR) + 2;
 __global__ __launch_bounds__(kBiasThreads) void exact_bias_kernel(ExactArgs a, const float* __restrict__ diag, int parts,
                                                                   void* __restrict__ dbias) {
-  __shared__ double tot[kMaxEntries];
-  __shared__ int bucket[kMaxEntries];
-  __shared__ double part[kBiasThreads];
-  const int h = blockIdx.x, tid = threadIdx.x, entries = window_entries(a.far) + 2;
+  __shared__ uint16_t list[kMaxEntries];
+  __shared__ int count;
+  __shared__ double sums[kBiasThreads];
+  const int h = blockIdx.x, c = blockIdx.y, tid = threadIdx.x, entries = window_entries(a.far) + 2;
   const float* src = diag + (long long)h * parts * entries;
-  int cols = 64;                                   // entries at a time
-  while (cols < entries && cols < kBiasThreads) cols *= 2;
-  const int groups = kBiasThreads / cols, grp = tid / cols;
-  for (int e0 = 0; e0 < entries; e0 += cols) {
-    const int e = e0 + tid % cols;
-    double t = 0.0;
-    if (e < entries)
-      for (int p = grp; p < parts; p += groups) t += (double)src[(long long)p * entries + e];
-    part[tid] = t;
-    __syncthreads();
-    if (grp == 0 && e < entries) {
-      for (int q = 1; q < groups; ++q) t += part[q * cols + tid];
-      tot[e] = t;
-      const int d = e < entries - 2 ? min(max(e - kWinPad, 0), 2 * a.far) : (e == entries - 2 ? 0 : 2 * a.far);
-      bucket[e] = a.map[d];
+  if (tid < kWave) {                               // ascending: one wave, its lanes' hits in order
+    int n = 0;
+    for (int e0 = 0; e0 < entries; e0 += kWave) {
+      const int e = e0 + tid;
+      int d = min(max(e - kWinPad, 0), 2 * a.far);
+      if (e == entries - 2) d = 0;                 // the tiles below the window, and above it
+      if (e == entries - 1) d = 2 * a.far;
+      const bool hit = e < entries && a.map[d] == c;
+      const uint64_t hits = __ballot(hit);
+      if (hit) list[n + bits_below(hits)] = (uint16_t)e;
+      n += __popcll(hits);
     }
+    if (tid == 0) count = n;
+  }
+  __syncthreads();
+  const int n = count;
+  double t = 0.0;
+  if (n > 0) {
+    // threads side by side take entries side by side of a block, whole blocks where they fit
+    const int cols = min(n, kBiasThreads), per = kBiasThreads / cols, col = tid % cols, first = tid / cols;
+    if (first < per)
+      for (int e = col; e < n; e += cols) {
+        const float* at = src + list[e];
+#pragma unroll 8
+        for (int p = first; p < parts; p += per) t += (double)at[(long long)p * entries];
+      }
+  }
+  sums[tid] = t;
+  __syncthreads();
+  for (int half = kBiasThreads / 2; half > 0; half /= 2) {
+    if (tid < half) sums[tid] += sums[tid + half];
     __syncthreads();
   }
-  for (int c = tid; c < a.buckets; c += kBiasThreads) {
-    double t = 0.0;
-    for (int e = 0; e < entries; ++e)
-      if (bucket[e] == c) t += tot[e];
+  if (tid == 0) {
     const long long at = (long long)c * a.H + h;
-    if (a.bias_bf16) static_cast<uint16_t*>(dbias)[at] = (uint16_t)f32_to_bf16_rne((float)t);
-    else static_cast<float*>(dbias)[at] = (float)t;
+    if (a.bias_bf16) static_cast<uint16_t*>(dbias)[at] = (uint16_t)f32_to_bf16_rne((float)sums[0]);
+    else static_cast<float*>(dbias)[at] = (float)sums[0];
   }
 }
 
@@ -365,7 +409,7 @@ static hipError_t backward_case(const ExactArgs& a, const ExactGrads& g, hipStre
   const size_t entries = BIAS ? window_entries(a.far) : 0;
   const int qblocks = exact_dq_blocks(a.nq);
   if (a.nq > 0) {
-    const size_t smem = stage + (1 + 2 * kExactWaves) * entries * sizeof(float);
+    const size_t smem = stage + ((1 + kExactWaves) * entries + (BIAS ? kExactWaves * kSkew : 0)) * sizeof(float);
     auto kernel = exact_dq_kernel<NP, D, BIAS>;
     hipError_t e = allow_lds(kernel, smem);
     if (e != hipSuccess) return e;
@@ -399,7 +443,7 @@ hipError_t launch_exact_backward(const ExactArgs& a, const ExactGrads& g, int d,
     if (e != hipSuccess) return e;
   }
   if (g.dbias != nullptr && a.H > 0)
-    exact_bias_kernel<<<a.H, kBiasThreads, 0, stream>>>(a, g.diag, a.B * exact_dq_blocks(a.nq), g.dbias);
+    exact_bias_kernel<<<dim3(a.H, a.buckets), kBiasThreads, 0, stream>>>(a, g.diag, a.B * exact_dq_blocks(a.nq), g.dbias);
   return hipGetLastError();
 }
 

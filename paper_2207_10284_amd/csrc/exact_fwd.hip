@@ -339,32 +339,51 @@ __global__ __launch_bounds__(kExactThreads) void exact_split_kernel(ExactArgs a,
   }
 }
 
-// Adds the partial rows of `splits` workgroups, in their order: a thread per
-// four columns of a row.
+// Adds the partial rows of `splits` workgroups: a workgroup per row, D / 4 threads
+// across the columns, the others across the splits; their sums are added in order.
 template <int NP, int D>
 __global__ __launch_bounds__(256) void exact_join_kernel(ExactArgs a, float* __restrict__ lse, int splits,
                                                          const float* __restrict__ part_o,
                                                          const float* __restrict__ part_l) {
-  constexpr int L = D / 4;
-  const int rows = a.nq * a.group;
-  const long long all = (long long)a.B * a.Hkv * rows;
-  const long long pr = (long long)blockIdx.x * (256 / L) + threadIdx.x / L;
-  const int c = threadIdx.x % L;
-  if (pr >= all) return;
-  float top = -INFINITY;
-  for (int s = 0; s < splits; ++s) top = fmaxf(top, part_l[2 * (s * all + pr)]);
-  float sum = 0.0f;
-  f32x4 z = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
-  for (int s = 0; s < splits; ++s) {
-    const float ref = part_l[2 * (s * all + pr)], l = part_l[2 * (s * all + pr) + 1];
-    const f32x4 o = *reinterpret_cast<const f32x4*>(part_o + (s * all + pr) * D + 4 * c);
-    const float f = ref == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ref - top);
-    sum += l * f;
+  constexpr int L = D / 4, G = 256 / L;
+  __shared__ float refs[64], ls[64];
+  __shared__ __attribute__((aligned(16))) f32x4 zs[G][L];
+  const int rows = a.nq * a.group, tid = threadIdx.x, c = tid % L, grp = tid / L;
+  const long long all = (long long)a.B * a.Hkv * rows, pr = blockIdx.x;
+  f32x4 o[64 / G];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) z[e] = fmaf(o[e], f, z[e]);
+  for (int x = 0; x < 64 / G; ++x) {
+    const int s = min(grp + x * G, splits - 1);
+    o[x] = *reinterpret_cast<const f32x4*>(part_o + (s * all + pr) * D + 4 * c);
   }
-  const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+  if (tid < 64) {
+    const bool on = tid < splits;
+    const float ref = on ? part_l[2 * (tid * all + pr)] : -INFINITY;
+    const float top = wave_max(ref);
+    const float f = ref == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ref - top);
+    refs[tid] = f;
+    const float sum = wave_sum(on ? part_l[2 * (tid * all + pr) + 1] * f : 0.0f);
+    if (tid == 0) {
+      ls[0] = top;
+      ls[1] = sum;
+    }
+  }
+  __syncthreads();
+  f32x4 z = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int x = 0; x < 64 / G; ++x) {
+    const float f = refs[grp + x * G];             // 0 past the splits
+#pragma unroll
+    for (int e = 0; e < 4; ++e) z[e] = f == 0.0f ? z[e] : fmaf(o[x][e], f, z[e]);
+  }
+  zs[grp][c] = z;
+  __syncthreads();
+  if (grp != 0) return;
+#pragma unroll
+  for (int x = 1; x < G; ++x)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) z[e] += zs[x][c][e];
+  const float top = ls[0], sum = ls[1], inv = sum > 0.0f ? 1.0f / sum : 0.0f;
   const long long bk = pr / rows;
   const int m = (int)(pr - bk * rows), i = m / a.group, b = (int)(bk / a.Hkv);
   const int h = (int)(bk - (long long)b * a.Hkv) * a.group + (m - i * a.group);
@@ -375,8 +394,9 @@ __global__ __launch_bounds__(256) void exact_join_kernel(ExactArgs a, float* __r
 }
 
 // The split kernel serves calls whose 128-row workgroups would leave most of the
-// chip idle; its workgroups are at least two per CU where the keys allow, each
-// with at least two tiles per wave.
+// chip idle, and those whose rows would leave most of each workgroup idle; its
+// workgroups are at least two per CU where the keys allow, each with at least two
+// tiles per wave.
 SplitPlan exact_split_plan(const mra_exact_problem_t& p) {
   SplitPlan s{};
   const long long heads = (long long)p.B * p.H, kheads = (long long)p.B * p.H_kv;
@@ -384,7 +404,7 @@ SplitPlan exact_split_plan(const mra_exact_problem_t& p) {
   const long long rows = (long long)p.n_q * (p.H / p.H_kv);
   s.mtiles = (int)((rows + 31) / 32);
   s.splits = 1;
-  s.use = blocks < kCus && rows < (1 << 20);
+  s.use = (blocks < kCus || rows <= 64) && rows < (1 << 20);
   if (s.use) {
     const long long wgs = kheads * s.mtiles, most = (p.n_k + 255) / 256;
     long long want = (2 * kCus + wgs - 1) / wgs;
@@ -416,8 +436,7 @@ static hipError_t forward_case(const ExactArgs& a, float* lse, const SplitPlan& 
     if (plan.splits > 1) {
       const hipError_t e = hipGetLastError();
       if (e != hipSuccess) return e;
-      constexpr int per = 256 / (D / 4);
-      exact_join_kernel<NP, D><<<(unsigned)((rows + per - 1) / per), 256, 0, stream>>>(a, lse, plan.splits, part_o, part_l);
+      exact_join_kernel<NP, D><<<(unsigned)rows, 256, 0, stream>>>(a, lse, plan.splits, part_o, part_l);
     }
     return hipGetLastError();
   }

@@ -149,20 +149,26 @@ __device__ __forceinline__ void load_operand(const char* row, bool on, u32x4 (&f
   }
 }
 
-// c + A B^T over the D columns: A the rows of the staged tile (plane 0 at `tile`,
+// c + A B^T over the column chunks K0 .. K1 - 1 (16 columns each): A the rows of the staged tile (plane 0 at `tile`,
 // planes `step` bytes apart), B this lane's operand; the smallest plane products first.
-template <int NP, int D>
-__device__ __forceinline__ f32x16 product(const TileAddr<D>& at, const char* tile, int step, const u32x4 (&b)[NP][D / 16],
-                                          f32x16 c) {
+template <int NP, int D, int K0, int K1>
+__device__ __forceinline__ f32x16 product_part(const TileAddr<D>& at, const char* tile, int step,
+                                               const u32x4 (&b)[NP][D / 16], f32x16 c) {
 #pragma unroll
   for (int p = NP - 1; p >= 0; --p)
 #pragma unroll
-    for (int k = 0; k < D / 16; ++k) {
+    for (int k = K0; k < K1; ++k) {
       const u32x4 a = at.row(tile + p * step, k);
 #pragma unroll
       for (int q = NP - 1 - p; q >= 0; --q) c = mfma16(a, b[q][k], c);
     }
   return c;
+}
+
+template <int NP, int D>
+__device__ __forceinline__ f32x16 product(const TileAddr<D>& at, const char* tile, int step, const u32x4 (&b)[NP][D / 16],
+                                          const f32x16& c) {
+  return product_part<NP, D, 0, D / 16>(at, tile, step, b, c);
 }
 
 // The 16 weights of a lane as the planes of the next product's B operand.

@@ -243,6 +243,16 @@ def test_bias_window_covers_every_near_tile(far):
                 assert min(max(x - PAD, 0), 2 * far) == min(max(x - far - PAD, -far), far) + far
 
 
+def test_skewed_tile():
+    """Query q's key k goes to row q, column k - q + 31 of 32 x 64 floats; the
+    addresses of a near tile's 64 columns in the window stay inside it."""
+    seen = {63 * q + 31 + k: (q, k) for q in range(32) for k in range(32)}
+    assert len(seen) == 1024 and all(divmod(x, 64) == (q, k - q + 31) for x, (q, k) in seen.items())
+    for far in (0, 1, 91, 512):
+        for d0 in range(-far - 30, far + 31):
+            assert 0 <= d0 + far + PAD - 31 and d0 + far + PAD - 31 + 63 < 2 * far + 2 * PAD
+
+
 @pytest.mark.parametrize("d", [32, 64, 128])
 @pytest.mark.parametrize("rows,threads", [(64, 256), (32, 256), (32, 64)])
 def test_stage_writes_each_chunk_once(d, rows, threads):
@@ -275,6 +285,6 @@ def test_lds_fits():
         rows = 64 if planes == 1 or d == 32 else 32
         stage = 4 * planes * rows * d * 2
         win = (2 * 512 + 2 * PAD) * 4
-        assert stage + 9 * win <= 160 * 1024                        # dQ: the bias and eight windows of sums
+        assert stage + 5 * win + 4 * 32 * 64 * 4 <= 160 * 1024      # dQ: the bias, four windows of sums and skewed tiles
         assert stage + 16 * rows + win <= 160 * 1024                # dK, dV
         assert max(4 * planes * 32 * d * 2, 3 * 32 * d * 4) + 2048 <= 160 * 1024
