@@ -1,5 +1,6 @@
 """Build libmra.so and libmra_exact.so (the HIP kernels and their C ABIs, gfx950)
-and _binding.so (the torch binding of ops.py's calls, host code) in-tree.
+and _binding.so and _binding_exact.so (the torch bindings of ops.py's calls, host
+code) in-tree.
 
     python -m paper_2207_10284_amd.build
 
@@ -23,6 +24,7 @@ BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libmra.so")
 LIB_EXACT = os.path.join(PKG, "libmra_exact.so")
 BINDING = os.path.join(PKG, "_binding.so")
+BINDING_EXACT = os.path.join(PKG, "_binding_exact.so")
 SOURCES = ["api.cpp", "pool.hip", "coarse.hip", "select.hip", "select_global.hip", "tile.hip",
            "bwd.hip", "multilevel.hip", "noalloc.hip"]
 EXACT_SOURCES = ["exact_api.cpp", "exact_fwd.hip", "exact_bwd.hip"]
@@ -50,22 +52,22 @@ def _compile(src: str) -> str:
     return obj
 
 
-def _build_binding() -> str:
-    """The torch binding: host code against the installed torch's headers; it
-    takes libmra's entry points by address, so it does not link to it."""
+def _build_binding(source: str, binding: str) -> str:
+    """A torch binding: host code against the installed torch's headers; it
+    takes its library's entry points by address, so it does not link to it."""
     torch = os.path.dirname(importlib.util.find_spec("torch").origin)
     inc = [os.path.join(torch, "include"), os.path.join(torch, "include", "torch", "csrc", "api", "include"),
            "/opt/rocm/include", sysconfig.get_paths()["include"]]
-    tmp = BINDING + ".tmp"
+    tmp = binding + ".tmp"
     cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-D__HIP_PLATFORM_AMD__=1",
-           "-DUSE_ROCM", "-I", INCLUDE, *(f for d in inc for f in ("-isystem", d)), os.path.join(CSRC, "binding.cpp"),
+           "-DUSE_ROCM", "-I", INCLUDE, *(f for d in inc for f in ("-isystem", d)), os.path.join(CSRC, source),
            "-L", os.path.join(torch, "lib"), "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch", "-ltorch_python",
            "-o", tmp]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"compile failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
-    os.replace(tmp, BINDING)
-    return BINDING
+    os.replace(tmp, binding)
+    return binding
 
 
 def _link(objs, lib: str) -> None:
@@ -80,15 +82,17 @@ def _link(objs, lib: str) -> None:
 def build(verbose: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
     with cf.ThreadPoolExecutor(max_workers=8) as ex:
-        binding = ex.submit(_build_binding)
+        bindings = [ex.submit(_build_binding, "binding.cpp", BINDING),
+                    ex.submit(_build_binding, "exact_binding.cpp", BINDING_EXACT)]
         exact = [ex.submit(_compile, s) for s in EXACT_SOURCES]
         objs = list(ex.map(_compile, SOURCES))
         exact = [f.result() for f in exact]
-        binding.result()
+        for b in bindings:
+            b.result()
     _link(objs, LIB)
     _link(exact, LIB_EXACT)
     if verbose:
-        print(f"built {LIB}, {LIB_EXACT} and {BINDING}")
+        print(f"built {LIB}, {LIB_EXACT}, {BINDING} and {BINDING_EXACT}")
     return LIB
 
 

@@ -10,17 +10,11 @@
 // rest mostly on the autograd engine's thread; with this node it takes 58 in a
 // bare loop and 91 among other work. A forward call's host time fell from 19 to
 // 12 us, which is its three launches.
-#include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_like.h>
-#include <c10/hip/HIPStream.h>
-#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/custom_function.h>
-#include <torch/csrc/utils/pybind.h>
 
-#include "mra.h"
-
-namespace py = pybind11;
+#include "binding_common.h"
 
 namespace {
 
@@ -42,43 +36,12 @@ Api api{};
 
 enum Variant { kMra2 = 0, kSparse = 1, kGlobal = 2 };
 
-// ops.py's MraError factory; never destroyed (the interpreter ends first)
-py::object& status_error = *new py::object();
-
-// What fails here is raised as the Python function of ops.py raises it, also from
-// the backward, whose errors reach the caller through the autograd engine: a
-// refusal by the library as MraError, one by the checks as c10's ValueError and
-// TypeError, which torch turns into Python's (as it does its own, an exhausted
-// allocator's, and a saved-tensor hook's exception).
-void ok(const char* fn, mra_status_t st) {
-  if (st == MRA_OK) return;
-  py::gil_scoped_acquire gil;
-  const py::object err = status_error(fn, (int)st);
-  PyErr_SetObject(reinterpret_cast<PyObject*>(Py_TYPE(err.ptr())), err.ptr());
-  python_error e;
-  e.persist();
-  throw e;
-}
-
-mra_dtype_t dtype_code(const at::Tensor& t) {
-  if (t.scalar_type() == at::kFloat) return MRA_F32;
-  if (t.scalar_type() == at::kBFloat16) return MRA_BF16;
-  TORCH_CHECK_TYPE(false, "unsupported dtype ", c10::toString(t.scalar_type()), "; expected float32 or bfloat16");
-}
-
 void check_like(const at::Tensor& t, const at::Tensor& ref) {
   TORCH_CHECK_VALUE(t.is_cuda(), "tensors must be on a ROCm device");
   TORCH_CHECK_VALUE(t.dim() == 4 && t.sizes() == ref.sizes() && t.scalar_type() == ref.scalar_type() &&
                         t.device() == ref.device(),
                     "q, k, v must share shape [B, H, n, d], dtype and device");
   TORCH_CHECK_VALUE(t.is_contiguous(), "q, k, v must be contiguous");
-}
-
-// A shape as Python writes it.
-std::string tuple_of(at::IntArrayRef shape) {
-  std::string s = "(";
-  for (size_t i = 0; i < shape.size(); ++i) s += (i ? ", " : "") + std::to_string(shape[i]);
-  return s + (shape.size() == 1 ? ",)" : ")");
 }
 
 void check_f32(const at::Tensor& t, at::IntArrayRef shape, const char* name) {
@@ -91,14 +54,10 @@ void check_idx(const at::Tensor& t, at::IntArrayRef shape, const at::Device& dev
                     "idx must be a contiguous int32 tensor of shape ", tuple_of(shape));
 }
 
-void* ptr(const std::optional<at::Tensor>& t) { return t ? t->data_ptr() : nullptr; }
-
 struct Dims {
   int B, H, n, d;
 };
 Dims dims(const at::Tensor& t) { return {(int)t.size(0), (int)t.size(1), (int)t.size(2), (int)t.size(3)}; }
-
-void* stream_of(const at::Tensor& t) { return c10::hip::getCurrentHIPStream(t.device().index()).stream(); }
 
 size_t workspace_bytes(int variant, const Dims& s, int64_t budget, mra_dtype_t dt) {
   return variant == kGlobal ? api.global_ws(s.B, s.H, s.n, s.d, kBlock, dt)
@@ -228,11 +187,6 @@ struct Attention : torch::autograd::Function<Attention> {
 at::Tensor mra_attention(const at::Tensor& q, const at::Tensor& k, const at::Tensor& v, int64_t budget, int64_t variant,
                          bool prior) {
   return Attention::apply(q, k, v, budget, variant, prior);
-}
-
-template <class F>
-void bind_one(const py::dict& a, const char* name, F& f) {
-  f = reinterpret_cast<F>(a[name].cast<uintptr_t>());
 }
 
 void bind(const py::dict& a) {

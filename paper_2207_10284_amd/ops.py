@@ -522,6 +522,7 @@ EXACT_SIGNATURES = {
 }
 
 _exact_lib = None
+_exact_native = None    # csrc/exact_binding.cpp, bound to _exact_lib by the first call that needs it
 
 
 class _ExactStatus:
@@ -547,6 +548,22 @@ def load_exact(path: str = EXACT_LIB_PATH):
             fn.restype, fn.argtypes = res, args
         _exact_lib = lib
     return _exact_lib
+
+
+def bind_exact():
+    """The native binding of the exact-attention calls (as ``bind``)."""
+    global _exact_native
+    if _exact_native is None:
+        lib = load_exact()
+        try:
+            from paper_2207_10284_amd import _binding_exact
+        except ImportError as e:
+            raise RuntimeError(f"the torch binding is not built ({e}); run `python -m paper_2207_10284_amd.build` "
+                               "first") from e
+        _binding_exact.bind({name: ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in EXACT_SIGNATURES},
+                            lambda fn, status: MraError(fn, status, _ExactStatus()))
+        _exact_native = _binding_exact
+    return _exact_native
 
 
 def _call_exact(name: str, *args):
@@ -630,6 +647,9 @@ def _check_int(t, shape, name, device):
         raise ValueError(f"{name} must be a contiguous int32 tensor of shape {shape} on {device}")
 
 
+_EXACT_KEYS = ("scale", "causal", "lengths", "key_mask", "q_start", "bias", "buckets")
+
+
 def _exact_problem(q, k, v, scale, causal, lengths, key_mask, q_start, bias, buckets):
     if not (q.is_cuda and k.is_cuda and v.is_cuda):
         raise ValueError("tensors must be on a ROCm device")
@@ -667,11 +687,16 @@ def _exact_problem(q, k, v, scale, causal, lengths, key_mask, q_start, bias, buc
                     _dtype_code(bias) if bias is not None else 0, num, _ptr(buckets), far)
 
 
-def _exact_workspace(name, p, workspace, device):
-    need = int(getattr(load_exact(), name)(ctypes.byref(p)))
-    if workspace is None and need:
-        workspace = torch.empty(need, device=device, dtype=torch.uint8)
-    return workspace, 0 if workspace is None else workspace.numel() * workspace.element_size()
+def exact_forward_workspace_bytes(q, k, v, **kw) -> int:
+    """Workspace of ``exact_attention_forward`` for these arguments (0: none)."""
+    p = _exact_problem(q, k, v, *(kw.get(n) for n in _EXACT_KEYS))
+    return int(load_exact().mra_exact_forward_workspace_bytes(ctypes.byref(p)))
+
+
+def exact_backward_workspace_bytes(q, k, v, **kw) -> int:
+    """Workspace of ``exact_attention_backward`` for these arguments."""
+    p = _exact_problem(q, k, v, *(kw.get(n) for n in _EXACT_KEYS))
+    return int(load_exact().mra_exact_backward_workspace_bytes(ctypes.byref(p)))
 
 
 def exact_attention_forward(q, k, v, *, scale=None, causal: bool = False, lengths=None, key_mask=None, q_start=None,
@@ -690,20 +715,8 @@ def exact_attention_forward(q, k, v, *, scale=None, causal: bool = False, length
     ``distance_buckets``). ``lse_out`` (float32 [B, H, n_q]) receives the log
     normalisers. A call whose ``workspace`` (uint8) a graph captured must not run
     beside another with the same one."""
-    p = _exact_problem(q, k, v, scale, causal, lengths, key_mask, q_start, bias, buckets)
-    if out is None:
-        out = _rows_like(q)
-    else:
-        _check_rows(out, q, q.shape, "out")
-    if lse_out is not None:
-        _check_f32(lse_out, q.shape[:3], "lse_out")
-        if lse_out.device != q.device:
-            raise ValueError(f"lse_out must be on {q.device}")
-    with torch.cuda.device(q.device):
-        workspace, size = _exact_workspace("mra_exact_forward_workspace_bytes", p, workspace, q.device)
-        _call_exact("mra_exact_forward", ctypes.byref(p), *(ctypes.byref(_view(t)) for t in (q, k, v, out)),
-                    _ptr(lse_out), _ptr(workspace), size, _stream(q.device))
-    return out
+    return bind_exact().forward(q, k, v, scale, causal, lengths, key_mask, q_start, bias, buckets, _result(q, out),
+                                lse_out, workspace)
 
 
 def exact_attention_backward(q, k, v, out, dout, lse, *, scale=None, causal: bool = False, lengths=None,
@@ -735,10 +748,12 @@ def exact_attention_backward(q, k, v, out, dout, lse, *, scale=None, causal: boo
                 or not dbias.is_contiguous():
             raise ValueError("dbias must be like bias")
     with torch.cuda.device(q.device):
-        workspace, size = _exact_workspace("mra_exact_backward_workspace_bytes", p, workspace, q.device)
+        if workspace is None:
+            workspace = torch.empty(max(int(load_exact().mra_exact_backward_workspace_bytes(ctypes.byref(p))), 1),
+                                    device=q.device, dtype=torch.uint8)
         _call_exact("mra_exact_backward", ctypes.byref(p), *(ctypes.byref(_view(t)) for t in (q, k, v, out, dout)),
-                    _ptr(lse), *(ctypes.byref(_view(t)) for t in grads), _ptr(dbias), _ptr(workspace), size,
-                    _stream(q.device))
+                    _ptr(lse), *(ctypes.byref(_view(t)) for t in grads), _ptr(dbias), _ptr(workspace),
+                    workspace.numel() * workspace.element_size(), _stream(q.device))
     return (*grads, dbias)
 
 
@@ -769,5 +784,11 @@ class ExactAttention(torch.autograd.Function):
 def exact_attention(q, k, v, *, scale=None, causal: bool = False, lengths=None, key_mask=None, q_start=None,
                     bias=None, buckets=None):
     """Differentiable exact softmax attention (arguments and result as
-    ``exact_attention_forward``), with gradients of q, k, v and bias."""
+    ``exact_attention_forward``), with gradients of q, k, v and bias; native where
+    ``mra_attention`` is."""
+    tensors = (q, k, v, lengths, key_mask, q_start, bias, buckets)
+    if (all(t is None or type(t) in _PLAIN for t in tensors)
+            and not torch._C._are_functorch_transforms_active() and torch._C._get_tracing_state() is None
+            and not torch.compiler.is_compiling()):
+        return bind_exact().exact_attention(q, k, v, scale, causal, lengths, key_mask, q_start, bias, buckets)
     return ExactAttention.apply(q, k, v, bias, buckets, lengths, key_mask, q_start, scale, causal)
