@@ -130,8 +130,10 @@ __global__ __launch_bounds__(kExactThreads) void exact_dq_kernel(ExactArgs a, Ex
     vs.store(smem + St::kBytes, ok, tid);
   }
   __syncthreads();
-  for (int st = 0; st < stages; ++st) {
-    char* cur = smem + (st & 1) * 2 * St::kBytes;
+  wait_loads<0>();                                 // the operands too: no wait for them beside the loads in flight below
+  // stage st in buffer BUF (known at compile time: its part of an LDS address is an offset)
+  auto stage = [&](int st, auto BUF) {
+    char* cur = smem + BUF * 2 * St::kBytes;
     const bool more = st + 1 < stages;
     uint32_t byte = 0;
     if (more) {
@@ -189,12 +191,16 @@ __global__ __launch_bounds__(kExactThreads) void exact_dq_kernel(ExactArgs a, Ex
       accumulate_t<NP, D>(at, ktile, STEP, pack_weights<NP>(ds), dq);
     }
     if (more) {
-      char* nxt = smem + ((st + 1) & 1) * 2 * St::kBytes;
+      char* nxt = smem + (1 - BUF) * 2 * St::kBytes;
       ok = key_bits<KT>(byte, (st + 1) * KT, limit);
       ks.store(nxt, ok, tid);
       vs.store(nxt + St::kBytes, ok, tid);
     }
     __syncthreads();
+  };
+  for (int st = 0; st < stages; st += 2) {
+    stage(st, std::integral_constant<int, 0>{});
+    if (st + 1 < stages) stage(st + 1, std::integral_constant<int, 1>{});
   }
   store_rows<NP, D>(dq, a.scale, g.dq.p + b * g.dq.sb + h * g.dq.sh + ic * g.dq.sn, i < a.nq);
   if constexpr (BIAS) {
@@ -283,8 +289,10 @@ __global__ __launch_bounds__(kExactThreads) void exact_dkv_kernel(ExactArgs a, E
     load(first);
     store(0, first);
     __syncthreads();
-    for (int st = 0; st < stages; ++st) {
-      const int buf = st & 1, q0 = first + st * QT;
+    wait_loads<0>();                               // the operands too: no wait for them beside the loads in flight below
+    auto stage = [&](int st, auto BUF) {
+      constexpr int buf = BUF;
+      const int q0 = first + st * QT;
       char* cur = smem + buf * 2 * St::kBytes;
       const bool more = st + 1 < stages;
       if (more) load(q0 + QT);
@@ -335,6 +343,10 @@ __global__ __launch_bounds__(kExactThreads) void exact_dkv_kernel(ExactArgs a, E
       }
       if (more) store(buf ^ 1, q0 + QT);
       __syncthreads();
+    };
+    for (int st = 0; st < stages; st += 2) {
+      stage(st, std::integral_constant<int, 0>{});
+      if (st + 1 < stages) stage(st + 1, std::integral_constant<int, 1>{});
     }
   }
   // a key that does not count has no gradient (its column of P is not one)

@@ -66,23 +66,23 @@ struct FwdRow {
   // Scores s of a tile in units where s mul + add are log2 logits (-inf: does not count)
   __device__ __forceinline__ void add_tile(f32x16 s, float mul, float add, const TileAddr<D>& at, char* vtile, int vstep) {
     Packed<NP> w;
-    float t = weights(s, mul, add - ref, w);
-    if (__ballot(!(t <= kCap)) != 0) {             // also a query's first tile (ref -inf)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], mul, add);
+    float t;
+    bool again = false;
+    // once, or again after the references moved
+    while (true) {
+      t = weights(s, mul, ref == -INFINITY && again ? 0.0f : add - ref, w);
+      if (again || __ballot(!(t <= kCap)) == 0) break;
       float mx = s[0];
 #pragma unroll
       for (int r = 1; r < 16; ++r) mx = __builtin_elementwise_maximum(mx, s[r]);
-      mx = halves_max(mx);
+      mx = fmaf(halves_max(mx), mul, add);
       const float next = mx > ref ? mx + kMargin : ref;
       const float f = next == ref ? 1.0f : __builtin_amdgcn_exp2f(ref - next);
 #pragma unroll
-      for (int x = 0; x < NT; ++x)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) o[x][r] *= f;
+      for (int x = 0; x < NT; ++x) o[x] *= f;
       sum *= f;
       ref = next;
-      t = weights(s, 1.0f, ref == -INFINITY ? 0.0f : -ref, w);
+      again = true;
     }
     sum += t;
     accumulate_t<NP, D>(at, vtile, vstep, w, o);
@@ -160,8 +160,10 @@ __global__ __launch_bounds__(kExactThreads) void exact_fwd_kernel(ExactArgs a, f
     vs.store(smem + St::kBytes, ok, tid);
   }
   __syncthreads();
-  for (int st = 0; st < stages; ++st) {
-    char* cur = smem + (st & 1) * 2 * St::kBytes;
+  wait_loads<0>();                                 // Q too: no wait for it beside the loads in flight below
+  // stage st in buffer BUF (known at compile time: its part of an LDS address is an offset)
+  auto stage = [&](int st, auto BUF) {
+    char* cur = smem + BUF * 2 * St::kBytes;
     const bool more = st + 1 < stages;
     uint32_t byte = 0;
     if (more) {
@@ -186,12 +188,16 @@ __global__ __launch_bounds__(kExactThreads) void exact_fwd_kernel(ExactArgs a, f
       }
     }
     if (more) {
-      char* nxt = smem + ((st + 1) & 1) * 2 * St::kBytes;
+      char* nxt = smem + (1 - BUF) * 2 * St::kBytes;
       ok = key_bits<KT>(byte, (st + 1) * KT, limit);
       ks.store(nxt, ok, tid);
       vs.store(nxt + St::kBytes, ok, tid);
     }
     __syncthreads();
+  };
+  for (int st = 0; st < stages; st += 2) {
+    stage(st, std::integral_constant<int, 0>{});
+    if (st + 1 < stages) stage(st + 1, std::integral_constant<int, 1>{});
   }
 #pragma unroll
   for (int x = 0; x < QT; ++x) {
@@ -249,6 +255,7 @@ __global__ __launch_bounds__(kExactThreads) void exact_split_kernel(ExactArgs a,
     vs.load(vp, a.v.sn, t * 32, limit, lane);
     byte = mask_byte(a, b, t * 32);
   }
+  wait_loads<0>();                                 // Q too: no wait for it beside the loads in flight below
   for (; t < t1; t += kExactWaves) {
     const int k0 = t * 32;
     const uint64_t ok = key_bits<32>(byte, k0, limit);

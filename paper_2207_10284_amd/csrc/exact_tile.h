@@ -106,6 +106,11 @@ struct TileAddr {
 #pragma unroll
       for (int e = 0; e < 2; ++e)
         tr[t][e] = raw_offset<D, exact_swz<D>>(4 * h + i16 / 4 + 8 * e, 32 * t + 16 * ((lane >> 4) & 1) + 4 * (i16 & 3));
+    // kept as they are, not put together again at each read
+#pragma unroll
+    for (int c = 0; c < KC; ++c) asm("" : "+v"(rr[c]));
+#pragma unroll
+    for (int t = 0; t < NT; ++t) asm("" : "+v"(tr[t][0]), "+v"(tr[t][1]));
   }
   __device__ __forceinline__ u32x4 row(const char* tile, int c) const {
     return *reinterpret_cast<const u32x4*>(tile + rr[c]);
