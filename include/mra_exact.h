@@ -56,7 +56,7 @@ typedef struct {
   int B, H, H_kv;             /* batches, query heads, key heads; H a multiple of H_kv */
   int n_q, n_k, d;
   mra_dtype_t dtype;          /* of q, k, v, out and their gradients */
-  float scale;                /* positive and finite */
+  float scale;                /* 2^-64 to 2^64 */
   int causal;                 /* 0 or 1 */
   const int32_t* lengths;     /* device [B], or NULL: every key */
   const int32_t* q_start;     /* device [B], or NULL: n_k - n_q */

@@ -5,7 +5,6 @@
 
 #include <hip/hip_runtime.h>
 
-#include <cmath>
 #include <cstdint>
 
 #include "exact_kernels.h"
@@ -40,7 +39,7 @@ mra_status_t check_problem(const mra_exact_problem_t* p) {
   if (p->B < 0 || p->H < 0 || p->H_kv < 0 || p->n_q < 0 || p->n_k < 0 || p->d <= 0) return MRA_ERR_INVALID_ARG;
   if (p->H > 0 && (p->H_kv == 0 || p->H % p->H_kv != 0)) return MRA_ERR_INVALID_ARG;
   if (p->H == 0 && p->H_kv != 0) return MRA_ERR_INVALID_ARG;
-  if (!(p->scale > 0.0f) || !std::isfinite(p->scale)) return MRA_ERR_INVALID_ARG;
+  if (!(p->scale >= 0x1p-64f && p->scale <= 0x1p64f)) return MRA_ERR_INVALID_ARG;
   if (p->causal != 0 && p->causal != 1) return MRA_ERR_INVALID_ARG;
   if (p->d != 32 && p->d != 64 && p->d != 128) return MRA_ERR_UNSUPPORTED;
   if (p->n_q > kMaxLen || p->n_k > kMaxLen) return MRA_ERR_UNSUPPORTED;

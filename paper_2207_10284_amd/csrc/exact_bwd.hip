@@ -37,8 +37,8 @@ __global__ __launch_bounds__(kExactThreads) void exact_dq_kernel(ExactArgs a, Ex
   const int entries = BIAS ? window_entries(a.far) : 0;
   float* acc = win + entries;                      // a window of diagonal sums per wave
   const int tid = threadIdx.x, lane = lane_id(), w = wave_uniform(tid / kWave), hf = lane >> 5;
-  const int gi = xcd_remap(blockIdx.x, gridDim.x);
-  const int bh = gi / qblocks, qb = qblocks - 1 - (gi - bh * qblocks);   // causal: the longest first
+  const HeadBlock hb = head_block(blockIdx.x, a.B * a.H, qblocks, a.causal);
+  const int bh = hb.head, qb = qblocks - 1 - hb.block;             // causal: the longest first
   const int b = bh / a.H, h = bh - b * a.H, hk = h / a.group;
   const int row0 = qb * kDqRows + w * 32, i = row0 + (lane & 31), ic = min(i, a.nq - 1);
   const int limit = key_limit(a, b), start = first_position(a, b);
@@ -49,7 +49,7 @@ __global__ __launch_bounds__(kExactThreads) void exact_dq_kernel(ExactArgs a, Ex
   const int pos0 = start + row0;
 
   TileAddr<D> at;
-  at.init();
+  at.init(smem);
   u32x4 qf[NP][KC], gf[NP][KC];
   f32x16 dq[NT];
 #pragma unroll
@@ -107,7 +107,7 @@ __global__ __launch_bounds__(kExactThreads) void exact_dq_kernel(ExactArgs a, Ex
 #pragma unroll
       for (int c = KC / 2; c < KC; ++c) gf[p][c] ^= 0x80008000u;
   }
-  auto values_product = [&](const char* vtile) -> f32x16 {
+  auto values_product = [&](int vtile) -> f32x16 {
     if constexpr (kTwoSigns) {
       const f32x16 x = product_part<NP, D, 0, KC / 2>(at, vtile, STEP, gf, splat16(0.0f));
       const f32x16 y = product_part<NP, D, KC / 2, KC>(at, vtile, STEP, gf, splat16(0.0f));
@@ -121,39 +121,56 @@ __global__ __launch_bounds__(kExactThreads) void exact_dq_kernel(ExactArgs a, Ex
   };
 
   St ks, vs;
-  uint64_t ok = 0;
+  MaskBytes<KT> bytes;
+  RowBits<KT> ok{};
   if (stages > 0) {
     ks.load(kp, a.k.sn, 0, limit, tid);
     vs.load(vp, a.v.sn, 0, limit, tid);
-    ok = key_bits<KT>(mask_byte(a, b, 0), 0, limit);
+    bytes.load(a, b, 0);
+    ok = bytes.bits(0, limit);
     ks.store(smem, ok, tid);
     vs.store(smem + St::kBytes, ok, tid);
   }
   __syncthreads();
   wait_loads<0>();                                 // the operands too: no wait for them beside the loads in flight below
-  // stage st in buffer BUF (known at compile time: its part of an LDS address is an offset)
-  auto stage = [&](int st, auto BUF) {
-    char* cur = smem + BUF * 2 * St::kBytes;
+  // stage st in buffer BUF (known at compile time: its part of an LDS address is an
+  // offset); PLAIN: every key counts for every query, no bias
+  auto stage = [&](int st, auto BUF, auto PLAIN) {
+    constexpr int cur = BUF * 2 * St::kBytes;
     const bool more = st + 1 < stages;
-    uint32_t byte = 0;
     if (more) {
       ks.load(kp, a.k.sn, (st + 1) * KT, limit, tid);
       vs.load(vp, a.v.sn, (st + 1) * KT, limit, tid);
-      byte = mask_byte(a, b, (st + 1) * KT);
+      bytes.load(a, b, (st + 1) * KT);
     }
 #pragma unroll
     for (int x = 0; x < TILES; ++x) {
-      const uint32_t kb = (uint32_t)(ok >> (32 * x));
-      const int k0 = st * KT + 32 * x;
-      const uint32_t bits = a.causal ? kb & low_bits(pos0 + (lane & 31) - k0 + 1) : kb;
-      if (__ballot(bits != 0) == 0) continue;
-      char* ktile = cur + x * kTileBytes<D>;
-      f32x16 s = product<NP, D>(at, ktile, STEP, qf, splat16(0.0f));
-      const f32x16 dp = values_product(cur + St::kBytes + x * kTileBytes<D>);
+      const uint32_t kb = PLAIN ? ~0u : ok.tile(x);
+      const int k0 = st * KT + 32 * x, ktile = cur + x * kTileBytes<D>, vtile = cur + St::kBytes + x * kTileBytes<D>;
+      if (!PLAIN && (kb == 0 || (a.causal && k0 > pos0 + 31))) continue;
+      f32x16 s, dp;
+      u32x4 kt[2][NT];
+      if constexpr (NP == 1) {
+        u32x4 kr[KC], vr[KC];
+        read_rows<D>(at, ktile, kr);
+        read_rows<D>(at, vtile, vr);
+        __builtin_amdgcn_sched_barrier(0);
+        s = splat16(0.0f);
+        dp = splat16(-delta);
+#pragma unroll
+        for (int c = 0; c < KC; ++c) {
+          s = mfma16(kr[c], qf[0][c], s);
+          dp = mfma16(vr[c], gf[0][c], dp);
+        }
+        read_trans<D>(at, ktile, kt);
+        __builtin_amdgcn_sched_barrier(0);
+      } else {
+        s = product<NP, D>(at, ktile, STEP, qf, splat16(0.0f));
+        dp = values_product(vtile);
+      }
       float mul = a.scale_log2, add = nl;
-      const int d0 = k0 - pos0;
+      const int d0 = k0 - pos0, at_win = d0 + a.far + kWinPad - (lane & 31) + 4 * hf;
       BiasKind kind = kBiasNear;
-      const int at_win = d0 + a.far + kWinPad - (lane & 31) + 4 * hf;
       if constexpr (BIAS) {
         kind = bias_kind(d0, a.far);
         if (kind == kBiasNear) {
@@ -164,7 +181,8 @@ __global__ __launch_bounds__(kExactThreads) void exact_dq_kernel(ExactArgs a, Ex
           add = nl + (kind == kBiasLow ? lo : hi);
         }
       }
-      if (__ballot(bits != ~0u) != 0) select_rows(s, bits, -INFINITY);
+      if (!PLAIN && (kb != ~0u || (a.causal && k0 + 31 > pos0)))
+        select_rows(s, a.causal ? kb & low_bits(pos0 + (lane & 31) - k0 + 1) : kb, -INFINITY);
       float ds[16];
 #pragma unroll
       for (int r = 0; r < 16; ++r) ds[r] = __builtin_amdgcn_exp2f(fmaf(s[r], mul, add)) * dp[r];
@@ -188,19 +206,33 @@ __global__ __launch_bounds__(kExactThreads) void exact_dq_kernel(ExactArgs a, Ex
           else sum_hi += t;
         }
       }
-      accumulate_t<NP, D>(at, ktile, STEP, pack_weights<NP>(ds), dq);
+      const Packed<NP> dw = pack_weights<NP>(ds);
+      if constexpr (NP == 1) accumulate_chunks<D>(kt, dw, dq);
+      else accumulate_t<NP, D>(at, ktile, STEP, dw, dq);
     }
     if (more) {
       char* nxt = smem + (1 - BUF) * 2 * St::kBytes;
-      ok = key_bits<KT>(byte, (st + 1) * KT, limit);
+      ok = bytes.bits((st + 1) * KT, limit);
       ks.store(nxt, ok, tid);
       vs.store(nxt + St::kBytes, ok, tid);
     }
     __syncthreads();
   };
-  for (int st = 0; st < stages; st += 2) {
-    stage(st, std::integral_constant<int, 0>{});
-    if (st + 1 < stages) stage(st + 1, std::integral_constant<int, 1>{});
+  constexpr std::integral_constant<int, 0> b0{};
+  constexpr std::integral_constant<int, 1> b1{};
+  // the stages whose keys all count for all of the block's queries, in pairs, then the others
+  int st = 0;
+  if constexpr (!BIAS) {
+    const int all = a.causal ? min(limit, start + qb * kDqRows + 1) : limit;
+    const int plain = a.key_mask != nullptr ? 0 : max(all, 0) / KT & ~1;
+    for (; st < plain; st += 2) {
+      stage(st, b0, std::true_type{});
+      stage(st + 1, b1, std::true_type{});
+    }
+  }
+  for (; st < stages; st += 2) {
+    stage(st, b0, std::false_type{});
+    if (st + 1 < stages) stage(st + 1, b1, std::false_type{});
   }
   store_rows<NP, D>(dq, a.scale, g.dq.p + b * g.dq.sb + h * g.dq.sh + ic * g.dq.sn, i < a.nq);
   if constexpr (BIAS) {
@@ -229,12 +261,12 @@ __global__ __launch_bounds__(kExactThreads) void exact_dkv_kernel(ExactArgs a, E
   constexpr int QT = kStageRows<NP, D>, TILES = QT / 32, KC = D / 16, NT = D / 32;
   using St = Stage<NP, D, QT, kExactThreads>;
   constexpr int STEP = TILES * kTileBytes<D>;
+  constexpr int NUMS = 4 * St::kBytes;             // [2 buffers][-L / scale, -delta][QT] chunks of 16 bytes
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  float* rows = reinterpret_cast<float*>(smem + 4 * St::kBytes);   // [2][2][QT]: -L (log2 units), -delta
-  float* win = rows + 4 * QT;
+  float* win = reinterpret_cast<float*>(smem + NUMS + 64 * QT);
   const int tid = threadIdx.x, lane = lane_id(), w = wave_uniform(tid / kWave), hf = lane >> 5;
-  const int gi = xcd_remap(blockIdx.x, gridDim.x);
-  const int bk = gi / kblocks, kblk = gi - bk * kblocks;
+  const HeadBlock hb = head_block(blockIdx.x, a.B * a.Hkv, kblocks, a.causal);
+  const int bk = hb.head, kblk = hb.block;                         // causal: the longest first
   const int b = bk / a.Hkv, hk = bk - b * a.Hkv;
   const int block0 = kblk * kExactWaves * 32, k0 = block0 + w * 32, j = k0 + (lane & 31), jc = min(j, a.nk - 1);
   const int limit = key_limit(a, b), start = first_position(a, b);
@@ -242,17 +274,24 @@ __global__ __launch_bounds__(kExactThreads) void exact_dkv_kernel(ExactArgs a, E
   const bool any = __ballot(counts) != 0;          // of the wave's keys
 
   TileAddr<D> at;
-  at.init();
+  at.init(smem);
   u32x4 kf[NP][KC], vf[NP][KC];
   load_operand<NP, D>(a.k.p + b * a.k.sb + hk * a.k.sh + jc * a.k.sn, counts, kf);
   load_operand<NP, D>(a.v.p + b * a.v.sb + hk * a.v.sh + jc * a.v.sn, counts, vf);
   f32x16 dk[NT], dv[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t) dk[t] = dv[t] = splat16(0.0f);
+  // three ones against the first number of a query (half 0's chunk) and its second (half 1's)
+  const u32x4 three = {0x3F803F80u, 0x00003F80u, 0u, 0u}, none4 = {0u, 0u, 0u, 0u};
+  const u32x4 ones_l = hf == 0 ? three : none4, ones_d = hf == 0 ? none4 : three;
+  const uint32_t nums = lds_addr(smem) + NUMS + 16 * (hf * QT + (lane & 31));
+  const float inv_scale = 1.0f / a.scale;
 
-  // causal: the first query whose position reaches the block's first key
+  // causal: the first query whose position reaches the block's first key, and the
+  // first stage that all of the block's keys are behind
   const int first = a.causal ? min(max(block0 - start, 0), a.nq) / QT * QT : 0;
   const int stages = block0 < limit ? (a.nq - first + QT - 1) / QT : 0;   // per head
+  const int clear = a.causal ? max(block0 + kExactWaves * 32 - 1 - start - first + QT - 1, 0) / QT : 0;
   for (int hg = 0; hg < a.group && stages > 0; ++hg) {
     const int h = hk * a.group + hg;
     const char* qp = a.q.p + b * a.q.sb + h * a.q.sh;
@@ -272,81 +311,111 @@ __global__ __launch_bounds__(kExactThreads) void exact_dkv_kernel(ExactArgs a, E
       if (tid < QT) {
         const int q = min(q0 + tid, a.nq - 1);
         const float L = g.lse[lrow + q];
-        const bool none = q0 + tid >= a.nq || L == -INFINITY;
-        nl = none ? -INFINITY : -L * kLog2e;
-        nd = none ? 0.0f : -g.delta[lrow + q];
+        const bool off = q0 + tid >= a.nq || L == -INFINITY;   // no weight: finite, as it meets zeros too
+        nl = off ? -3e38f : -L * inv_scale;
+        nd = off ? 0.0f : -g.delta[lrow + q];
       }
     };
     auto store = [&](int buf, int q0) {
-      const uint64_t ok = key_bits<QT>(1, q0, a.nq);
+      const RowBits<QT> ok = row_bits<QT>(q0, a.nq);
       qs.store(smem + buf * 2 * St::kBytes, ok, tid);
       gs.store(smem + buf * 2 * St::kBytes + St::kBytes, ok, tid);
       if (tid < QT) {
-        rows[buf * 2 * QT + tid] = nl;
-        rows[buf * 2 * QT + QT + tid] = nd;
+        u32x4* to = reinterpret_cast<u32x4*>(smem + NUMS) + 2 * QT * buf + tid;
+        to[0] = number_chunk(nl);
+        to[QT] = number_chunk(nd);
       }
     };
     load(first);
     store(0, first);
     __syncthreads();
     wait_loads<0>();                               // the operands too: no wait for them beside the loads in flight below
-    auto stage = [&](int st, auto BUF) {
-      constexpr int buf = BUF;
+    // S - L / scale and dP - delta of a tile
+    auto logits = [&](int qtile, int gtile, int num, f32x16& s, f32x16& dp) {
+      const u32x4 n = *(const __attribute__((address_space(3))) u32x4*)(lds_ptr)(nums + num);
+      if constexpr (NP == 1) {
+        u32x4 qr[KC], gr[KC];
+        read_rows<D>(at, qtile, qr);
+        read_rows<D>(at, gtile, gr);
+        __builtin_amdgcn_sched_barrier(0);
+        s = dp = splat16(0.0f);
+#pragma unroll
+        for (int c = 0; c < KC; ++c) {
+          s = mfma16(qr[c], kf[0][c], s);
+          dp = mfma16(gr[c], vf[0][c], dp);
+        }
+      } else {
+        s = product<NP, D>(at, qtile, STEP, kf, splat16(0.0f));
+        dp = product<NP, D>(at, gtile, STEP, vf, splat16(0.0f));
+      }
+      s = mfma16(n, ones_l, s);
+      dp = mfma16(n, ones_d, dp);
+    };
+    // a stage in buffer BUF; PLAIN: every query reaches every key, one bias
+    auto stage = [&](int st, auto BUF, auto PLAIN) {
+      constexpr int cur = BUF * 2 * St::kBytes;
       const int q0 = first + st * QT;
-      char* cur = smem + buf * 2 * St::kBytes;
       const bool more = st + 1 < stages;
       if (more) load(q0 + QT);
 #pragma unroll
       for (int x = 0; x < TILES; ++x) {
         const int p0 = start + q0 + 32 * x;        // position of the tile's first query
-        const int live = a.nq - q0 - 32 * x;       // queries of the tile
-        if (!any || live <= 0) continue;
-        // queries whose position reaches this lane's key
-        const uint32_t bits = a.causal ? ~low_bits(j - p0) : ~0u;
-        if (__ballot(bits != 0) == 0) continue;
-        const float* nlr = rows + buf * 2 * QT + 32 * x + 4 * hf;
-        f32x16 c;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const f32x4 v = *reinterpret_cast<const f32x4*>(nlr + QT + 8 * q);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) c[4 * q + e] = v[e];
+        if (!any || a.nq <= q0 + 32 * x) continue;
+        if (!PLAIN && a.causal && p0 + 31 < k0) continue;       // no query reaches a key
+        const int qtile = cur + x * kTileBytes<D>, gtile = cur + St::kBytes + x * kTileBytes<D>;
+        f32x16 s, dp;
+        logits(qtile, gtile, 32 * QT * BUF + 512 * x, s, dp);
+        u32x4 gt[2][NT], qt[2][NT];
+        if constexpr (NP == 1) {
+          read_trans<D>(at, gtile, gt);
+          read_trans<D>(at, qtile, qt);
+          __builtin_amdgcn_sched_barrier(0);
         }
-        char *qtile = cur + x * kTileBytes<D>, *gtile = cur + St::kBytes + x * kTileBytes<D>;
-        f32x16 s = product<NP, D>(at, qtile, STEP, kf, splat16(0.0f));
-        const f32x16 dp = product<NP, D>(at, gtile, STEP, vf, c);
         float mul = a.scale_log2, add = 0.0f;
-        if constexpr (BIAS) {
-          const int d0 = k0 - p0;
-          const BiasKind kind = bias_kind(d0, a.far);
-          if (kind == kBiasNear) {
-            const float* wp = win + (d0 + a.far + kWinPad + (lane & 31) - 4 * hf);
+        if constexpr (!PLAIN) {
+          if constexpr (BIAS) {
+            const int d0 = k0 - p0;
+            const BiasKind kind = bias_kind(d0, a.far);
+            if (kind == kBiasNear) {
+              const float* wp = win + (d0 + a.far + kWinPad + (lane & 31) - 4 * hf);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.scale_log2, wp[-reg_row(r)]);
-            mul = 1.0f;
-          } else {
-            add = kind == kBiasLow ? lo : hi;
+              for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.scale_log2, wp[-reg_row(r)]);
+              mul = 1.0f;
+            } else {
+              add = kind == kBiasLow ? lo : hi;
+            }
           }
+          if (a.causal && p0 < k0 + 31) select_rows(s, ~low_bits(j - p0), -INFINITY);
         }
-        if (__ballot(bits != ~0u) != 0) select_rows(s, bits, -INFINITY);
         float p[16];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const f32x4 v = *reinterpret_cast<const f32x4*>(nlr + 8 * q);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) p[4 * q + e] = __builtin_amdgcn_exp2f(fmaf(s[4 * q + e], mul, v[e] + add));
-        }
-        accumulate_t<NP, D>(at, gtile, STEP, pack_weights<NP>(p), dv);
+        for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(!PLAIN && BIAS ? fmaf(s[r], mul, add) : s[r] * mul);
+        const Packed<NP> pw = pack_weights<NP>(p);
+        if constexpr (NP == 1) accumulate_chunks<D>(gt, pw, dv);
+        else accumulate_t<NP, D>(at, gtile, STEP, pw, dv);
 #pragma unroll
         for (int r = 0; r < 16; ++r) p[r] *= dp[r];
-        accumulate_t<NP, D>(at, qtile, STEP, pack_weights<NP>(p), dk);
+        const Packed<NP> dw = pack_weights<NP>(p);
+        if constexpr (NP == 1) accumulate_chunks<D>(qt, dw, dk);
+        else accumulate_t<NP, D>(at, qtile, STEP, dw, dk);
       }
-      if (more) store(buf ^ 1, q0 + QT);
+      if (more) store(1 - BUF, q0 + QT);
       __syncthreads();
     };
-    for (int st = 0; st < stages; st += 2) {
-      stage(st, std::integral_constant<int, 0>{});
-      if (st + 1 < stages) stage(st + 1, std::integral_constant<int, 1>{});
+    constexpr std::integral_constant<int, 0> b0{};
+    constexpr std::integral_constant<int, 1> b1{};
+    // stages on the causal border (or with a bias, all), in pairs, then the others
+    int st = 0;
+    const int border = BIAS ? stages : min(clear, stages);
+    for (; st < border; st += 2) {
+      stage(st, b0, std::false_type{});
+      if (st + 1 < stages) stage(st + 1, b1, std::false_type{});
+    }
+    if constexpr (!BIAS) {
+      for (; st < stages; st += 2) {
+        stage(st, b0, std::true_type{});
+        if (st + 1 < stages) stage(st + 1, b1, std::true_type{});
+      }
     }
   }
   // a key that does not count has no gradient (its column of P is not one)
@@ -409,12 +478,6 @@ __global__ __launch_bounds__(kBiasThreads) void exact_bias_kernel(ExactArgs a, c
   }
 }
 
-template <class Kernel>
-static hipError_t allow_lds(Kernel kernel, size_t smem) {
-  if (smem <= 65536) return hipSuccess;
-  return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-}
-
 template <int NP, int D, bool BIAS>
 static hipError_t backward_case(const ExactArgs& a, const ExactGrads& g, hipStream_t stream) {
   constexpr size_t stage = 4 * Stage<NP, D, kStageRows<NP, D>, kExactThreads>::kBytes;
@@ -429,7 +492,7 @@ static hipError_t backward_case(const ExactArgs& a, const ExactGrads& g, hipStre
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   if (a.nk > 0) {
-    const size_t smem = stage + (4 * kStageRows<NP, D> + entries) * sizeof(float);
+    const size_t smem = stage + 64 * kStageRows<NP, D> + entries * sizeof(float);
     auto kernel = exact_dkv_kernel<NP, D, BIAS>;
     hipError_t e = allow_lds(kernel, smem);
     if (e != hipSuccess) return e;

@@ -63,37 +63,52 @@ struct FwdRow {
     return t;
   }
 
-  // Scores s of a tile in units where s mul + add are log2 logits (-inf: does not count)
-  __device__ __forceinline__ void add_tile(f32x16 s, float mul, float add, const TileAddr<D>& at, char* vtile, int vstep) {
-    Packed<NP> w;
-    float t;
-    bool again = false;
-    // once, or again after the references moved
-    while (true) {
-      t = weights(s, mul, ref == -INFINITY && again ? 0.0f : add - ref, w);
-      if (again || __ballot(!(t <= kCap)) == 0) break;
-      float mx = s[0];
+  // Moves the reference to this tile's max, if that is larger.
+  __device__ __forceinline__ void move(const f32x16& s, float mul, float add) {
+    float mx = s[0];
 #pragma unroll
-      for (int r = 1; r < 16; ++r) mx = __builtin_elementwise_maximum(mx, s[r]);
-      mx = fmaf(halves_max(mx), mul, add);
-      const float next = mx > ref ? mx + kMargin : ref;
-      const float f = next == ref ? 1.0f : __builtin_amdgcn_exp2f(ref - next);
+    for (int r = 1; r < 16; ++r) mx = __builtin_elementwise_maximum(mx, s[r]);
+    mx = fmaf(halves_max(mx), mul, add);
+    const float next = mx > ref ? mx + kMargin : ref;
+    const float f = next == ref ? 1.0f : __builtin_amdgcn_exp2f(ref - next);
 #pragma unroll
-      for (int x = 0; x < NT; ++x) o[x] *= f;
-      sum *= f;
-      ref = next;
-      again = true;
-    }
-    sum += t;
-    accumulate_t<NP, D>(at, vtile, vstep, w, o);
+    for (int x = 0; x < NT; ++x) o[x] *= f;
+    sum *= f;
+    ref = next;
   }
 };
+
+// Weights of the scores s of R tiles of as many rows (log2 logits s mul + add; -inf:
+// does not count) and their sums; references that a tile outgrows are moved. The
+// second turn of the loop, not a branch, forms the weights again: with a branch the
+// accumulators were copied to other registers and back on every tile.
+template <int NP, int D, int R>
+__device__ __forceinline__ void tile_weights(FwdRow<NP, D> (&row)[R], const f32x16 (&s)[R], const float (&mul)[R],
+                                             const float (&add)[R], Packed<NP> (&w)[R]) {
+  float t[R];
+  bool again = false;
+  while (true) {
+    bool fits = true;
+#pragma unroll
+    for (int x = 0; x < R; ++x) {
+      // moved and still without a key: every s is -inf
+      t[x] = row[x].weights(s[x], mul[x], again && row[x].ref == -INFINITY ? 0.0f : add[x] - row[x].ref, w[x]);
+      fits = fits && t[x] <= kCap;                 // not so for a query's first tile (ref -inf)
+    }
+    if (again || __ballot(!fits) == 0) break;
+#pragma unroll
+    for (int x = 0; x < R; ++x) row[x].move(s[x], mul[x], add[x]);
+    again = true;
+  }
+#pragma unroll
+  for (int x = 0; x < R; ++x) row[x].sum += t[x];
+}
 
 // The scores of a tile with bias and masks: s, mul and add of add_tile. d0: the
 // distance of the tile's first key and this wave's first query; dq: this lane's
 // query behind that one; bits: this lane's keys that count; lo, hi: the outer biases.
 template <bool BIAS>
-__device__ __forceinline__ void finish_scores(f32x16& s, float& mul, float& add, float sl2, uint32_t bits, int d0,
+__device__ __forceinline__ void finish_scores(f32x16& s, float& mul, float& add, float sl2, bool masked, uint32_t bits, int d0,
                                               int far, const float* win, float lo, float hi) {
   mul = sl2;
   add = 0.0f;
@@ -109,7 +124,45 @@ __device__ __forceinline__ void finish_scores(f32x16& s, float& mul, float& add,
       add = kind == kBiasLow ? lo : hi;
     }
   }
-  if (__ballot(bits != ~0u) != 0) select_rows(s, bits, -INFINITY);
+  if (masked) select_rows(s, bits, -INFINITY);
+}
+
+// s[x] = K Q_x^T for all rows of a wave, each K chunk read once.
+template <int NP, int D, int R>
+__device__ __forceinline__ void products(const TileAddr<D>& at, int tile, int step, const FwdRow<NP, D> (&row)[R],
+                                         f32x16 (&s)[R]) {
+#pragma unroll
+  for (int x = 0; x < R; ++x) s[x] = splat16(0.0f);
+#pragma unroll
+  for (int p = NP - 1; p >= 0; --p) {
+    u32x4 k[D / 16];
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) k[c] = at.row(tile + p * step, c);
+#pragma unroll
+    for (int x = 0; x < R; ++x)
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c)
+#pragma unroll
+        for (int q = NP - 1 - p; q >= 0; --q) s[x] = mfma16(k[c], row[x].qf[q][c], s[x]);
+  }
+}
+
+// o[x] += V^T W_x for all rows of a wave, each V chunk read once.
+template <int NP, int D, int R>
+__device__ __forceinline__ void accumulate_rows(const TileAddr<D>& at, int tile, int step, const Packed<NP> (&w)[R],
+                                                FwdRow<NP, D> (&row)[R]) {
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+      for (int p = NP - 1; p >= 0; --p) {
+        const u32x4 v = at.trans(tile + p * step, u, t);
+#pragma unroll
+        for (int x = 0; x < R; ++x)
+#pragma unroll
+          for (int q = NP - 1 - p; q >= 0; --q) row[x].o[t] = mfma16(v, w[x].w[q][u], row[x].o[t]);
+      }
 }
 
 template <int NP, int D, int QT, bool BIAS>
@@ -120,9 +173,9 @@ __global__ __launch_bounds__(kExactThreads) void exact_fwd_kernel(ExactArgs a, f
   extern __shared__ __attribute__((aligned(16))) char smem[];
   float* win = reinterpret_cast<float*>(smem + 4 * St::kBytes);
   const int tid = threadIdx.x, lane = lane_id(), w = wave_uniform(tid / kWave);
-  const int g = xcd_remap(blockIdx.x, gridDim.x);
+  const HeadBlock hb = head_block(blockIdx.x, a.B * a.H, qblocks, a.causal);
   // causal rows take the longer the later they are: the last blocks of a head first
-  const int bh = g / qblocks, qb = qblocks - 1 - (g - bh * qblocks);
+  const int bh = hb.head, qb = qblocks - 1 - hb.block;
   const int b = bh / a.H, h = bh - b * a.H, hk = h / a.group;
   const int row0 = (qb * kExactWaves + w) * 32 * QT;
   const int limit = key_limit(a, b), start = first_position(a, b);
@@ -133,7 +186,7 @@ __global__ __launch_bounds__(kExactThreads) void exact_fwd_kernel(ExactArgs a, f
   const char* vp = a.v.p + b * a.v.sb + hk * a.v.sh;
 
   TileAddr<D> at;
-  at.init();
+  at.init(smem);
   FwdRow<NP, D> row[QT];
   int pos0[QT];
 #pragma unroll
@@ -151,11 +204,13 @@ __global__ __launch_bounds__(kExactThreads) void exact_fwd_kernel(ExactArgs a, f
   }
 
   St ks, vs;
-  uint64_t ok = 0;
+  MaskBytes<KT> bytes;
+  RowBits<KT> ok{};
   if (stages > 0) {
     ks.load(kp, a.k.sn, 0, limit, tid);
     vs.load(vp, a.v.sn, 0, limit, tid);
-    ok = key_bits<KT>(mask_byte(a, b, 0), 0, limit);
+    bytes.load(a, b, 0);
+    ok = bytes.bits(0, limit);
     ks.store(smem, ok, tid);
     vs.store(smem + St::kBytes, ok, tid);
   }
@@ -163,33 +218,49 @@ __global__ __launch_bounds__(kExactThreads) void exact_fwd_kernel(ExactArgs a, f
   wait_loads<0>();                                 // Q too: no wait for it beside the loads in flight below
   // stage st in buffer BUF (known at compile time: its part of an LDS address is an offset)
   auto stage = [&](int st, auto BUF) {
-    char* cur = smem + BUF * 2 * St::kBytes;
+    constexpr int kbuf = BUF * 2 * St::kBytes, vbuf = kbuf + St::kBytes;
     const bool more = st + 1 < stages;
-    uint32_t byte = 0;
     if (more) {
       ks.load(kp, a.k.sn, (st + 1) * KT, limit, tid);
       vs.load(vp, a.v.sn, (st + 1) * KT, limit, tid);
-      byte = mask_byte(a, b, (st + 1) * KT);
+      bytes.load(a, b, (st + 1) * KT);
     }
 #pragma unroll
     for (int i = 0; i < TILES; ++i) {
-      const uint32_t kb = (uint32_t)(ok >> (32 * i));
-      const int k0 = st * KT + 32 * i;
-      if (kb == 0) continue;
+      const uint32_t kb = ok.tile(i);
+      const int k0 = st * KT + 32 * i, ktile = kbuf + i * kTileBytes<D>, vtile = vbuf + i * kTileBytes<D>;
+      if (kb == 0 || (a.causal && k0 > pos0[QT - 1] + 31)) continue;      // no key counts for the wave
+      f32x16 s[QT];
+      products<NP, D, QT>(at, ktile, STEP, row, s);
+      float mul[QT], add[QT];
 #pragma unroll
       for (int x = 0; x < QT; ++x) {
         // keys up to this lane's position
         const uint32_t bits = a.causal ? kb & low_bits(pos0[x] + (lane & 31) - k0 + 1) : kb;
-        if (__ballot(bits != 0) == 0) continue;
-        f32x16 s = product<NP, D>(at, cur + i * kTileBytes<D>, STEP, row[x].qf, splat16(0.0f));
-        float mul, add;
-        finish_scores<BIAS>(s, mul, add, a.scale_log2, bits, k0 - pos0[x], a.far, win, lo, hi);
-        row[x].add_tile(s, mul, add, at, cur + St::kBytes + i * kTileBytes<D>, STEP);
+        const bool masked = kb != ~0u || (a.causal && k0 + 31 > pos0[x]);
+        finish_scores<BIAS>(s[x], mul[x], add[x], a.scale_log2, masked, bits, k0 - pos0[x], a.far, win, lo, hi);
+      }
+      Packed<NP> pw[QT];
+      if constexpr (NP == 1) {
+        u32x4 v[2][D / 32];                        // on their way while the weights are formed
+        read_trans<D>(at, vtile, v);
+        __builtin_amdgcn_sched_barrier(0);
+        tile_weights<NP, D, QT>(row, s, mul, add, pw);
+        // ahead of the SIMD's other wave while it forms weights: 8 heads x 12 x 4096 x 64: 432 -> 428 us
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int x = 0; x < QT; ++x) accumulate_chunks<D>(v, pw[x], row[x].o);
+        __builtin_amdgcn_s_setprio(0);
+      } else {
+        tile_weights<NP, D, QT>(row, s, mul, add, pw);
+        __builtin_amdgcn_s_setprio(1);
+        accumulate_rows<NP, D, QT>(at, vtile, STEP, pw, row);
+        __builtin_amdgcn_s_setprio(0);
       }
     }
     if (more) {
       char* nxt = smem + (1 - BUF) * 2 * St::kBytes;
-      ok = key_bits<KT>(byte, (st + 1) * KT, limit);
+      ok = bytes.bits((st + 1) * KT, limit);
       ks.store(nxt, ok, tid);
       vs.store(nxt + St::kBytes, ok, tid);
     }
@@ -238,8 +309,9 @@ __global__ __launch_bounds__(kExactThreads) void exact_split_kernel(ExactArgs a,
   char* slot = smem + w * SLOT;
 
   TileAddr<D> at;
-  at.init();
-  FwdRow<NP, D> row;
+  at.init(slot);
+  FwdRow<NP, D> rows1[1];
+  FwdRow<NP, D>& row = rows1[0];
   load_operand<NP, D>(a.q.p + b * a.q.sb + h * a.q.sh + i * a.q.sn, m < rows, row.qf);
   row.init();
   float lo = 0.0f, hi = 0.0f;
@@ -248,30 +320,31 @@ __global__ __launch_bounds__(kExactThreads) void exact_split_kernel(ExactArgs a,
     hi = bias_value(a, h, 2 * a.far) * kLog2e;
   }
   St ks, vs;
-  uint32_t byte = 0;
+  MaskBytes<32> bytes;
   int t = t0 + w;
   if (t < t1) {
     ks.load(kp, a.k.sn, t * 32, limit, lane);
     vs.load(vp, a.v.sn, t * 32, limit, lane);
-    byte = mask_byte(a, b, t * 32);
+    bytes.load(a, b, t * 32);
   }
   wait_loads<0>();                                 // Q too: no wait for it beside the loads in flight below
   for (; t < t1; t += kExactWaves) {
     const int k0 = t * 32;
-    const uint64_t ok = key_bits<32>(byte, k0, limit);
+    const RowBits<32> ok = bytes.bits(k0, limit);
     ks.store(slot, ok, lane);
     wave_lds_sync();
     const bool more = t + kExactWaves < t1;
     if (more) ks.load(kp, a.k.sn, k0 + 32 * kExactWaves, limit, lane);
-    f32x16 s = product<NP, D>(at, slot, kTileBytes<D>, row.qf, splat16(0.0f));
+    f32x16 s1[1] = {product<NP, D>(at, 0, kTileBytes<D>, row.qf, splat16(0.0f))};
+    f32x16& s = s1[0];
     wave_lds_sync();
     vs.store(slot, ok, lane);
     wave_lds_sync();
     if (more) {
       vs.load(vp, a.v.sn, k0 + 32 * kExactWaves, limit, lane);
-      byte = mask_byte(a, b, k0 + 32 * kExactWaves);
+      bytes.load(a, b, k0 + 32 * kExactWaves);
     }
-    const uint32_t kb = (uint32_t)ok, bits = a.causal ? kb & low_bits(pos - k0 + 1) : kb;
+    const uint32_t kb = ok.tile(0), bits = a.causal ? kb & low_bits(pos - k0 + 1) : kb;
     if (__ballot(bits != 0) != 0) {
       float mul = a.scale_log2, add = 0.0f;
       if constexpr (BIAS) {
@@ -289,7 +362,9 @@ __global__ __launch_bounds__(kExactThreads) void exact_split_kernel(ExactArgs a,
         }
       }
       if (__ballot(bits != ~0u) != 0) select_rows(s, bits, -INFINITY);
-      row.add_tile(s, mul, add, at, slot, kTileBytes<D>);
+      Packed<NP> pw[1];
+      tile_weights<NP, D, 1>(rows1, s1, {mul}, {add}, pw);
+      accumulate_t<NP, D>(at, 0, kTileBytes<D>, pw[0], row.o);
     }
     wave_lds_sync();
   }
@@ -423,6 +498,18 @@ SplitPlan exact_split_plan(const mra_exact_problem_t& p) {
   return s;
 }
 
+template <int NP, int D, int QT, bool BIAS>
+static hipError_t launch_rows(const ExactArgs& a, float* lse, hipStream_t stream) {
+  const int qblocks = (a.nq + kExactWaves * 32 * QT - 1) / (kExactWaves * 32 * QT);
+  const size_t smem = 4 * Stage<NP, D, kStageRows<NP, D>, kExactThreads>::kBytes +
+                      (BIAS ? window_entries(a.far) * sizeof(float) : 0);
+  auto kernel = exact_fwd_kernel<NP, D, QT, BIAS>;
+  const hipError_t e = allow_lds(kernel, smem);
+  if (e != hipSuccess) return e;
+  kernel<<<(unsigned)((long long)a.B * a.H * qblocks), kExactThreads, smem, stream>>>(a, lse, qblocks);
+  return hipGetLastError();
+}
+
 template <int NP, int D, bool BIAS>
 static hipError_t forward_case(const ExactArgs& a, float* lse, const SplitPlan& plan, void* ws, hipStream_t stream) {
   if (plan.use) {
@@ -434,31 +521,23 @@ static hipError_t forward_case(const ExactArgs& a, float* lse, const SplitPlan& 
     float* part_l = part_o + (plan.splits > 1 ? plan.splits * rows * D : 0);
     const unsigned wgs = (unsigned)((long long)a.B * a.Hkv * plan.mtiles * plan.splits);
     auto kernel = exact_split_kernel<NP, D, BIAS>;
-    if (smem > 65536) {
-      const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
-                                               hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-      if (e != hipSuccess) return e;
-    }
+    hipError_t e = allow_lds(kernel, smem);
+    if (e != hipSuccess) return e;
     kernel<<<wgs, kExactThreads, smem, stream>>>(a, lse, plan.mtiles, plan.splits, part_o, part_l);
     if (plan.splits > 1) {
-      const hipError_t e = hipGetLastError();
-      if (e != hipSuccess) return e;
+      if ((e = hipGetLastError()) != hipSuccess) return e;
       exact_join_kernel<NP, D><<<(unsigned)rows, 256, 0, stream>>>(a, lse, plan.splits, part_o, part_l);
     }
     return hipGetLastError();
   }
-  constexpr int QT = 1;
-  const int qblocks = (a.nq + kExactWaves * 32 * QT - 1) / (kExactWaves * 32 * QT);
-  const size_t smem = 4 * Stage<NP, D, kStageRows<NP, D>, kExactThreads>::kBytes +
-                      (BIAS ? window_entries(a.far) * sizeof(float) : 0);
-  auto kernel = exact_fwd_kernel<NP, D, QT, BIAS>;
-  if (smem > 65536) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
-                                             hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != hipSuccess) return e;
+  if constexpr (NP == 1 && D <= 64) {
+    // 64 queries per wave read K and V from LDS half as often (96 heads x 4096 x 64: 475 ->
+    // 428 us) but need the rows to fill their larger blocks, and blocks to fill the chip more than
+    // once (384 heads x 512 x 64, 768 of them: 36 -> 38 us)
+    const long long heads = (long long)a.B * a.H, wide = (a.nq + 255) / 256, narrow = (a.nq + 127) / 128;
+    if (heads * wide >= 4 * kCus && 20 * wide <= 11 * narrow) return launch_rows<NP, D, 2, BIAS>(a, lse, stream);
   }
-  kernel<<<(unsigned)((long long)a.B * a.H * qblocks), kExactThreads, smem, stream>>>(a, lse, qblocks);
-  return hipGetLastError();
+  return launch_rows<NP, D, 1, BIAS>(a, lse, stream);
 }
 
 hipError_t launch_exact_forward(const ExactArgs& a, int d, int dtype, float* lse, const SplitPlan& plan, void* ws,

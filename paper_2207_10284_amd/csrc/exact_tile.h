@@ -34,6 +34,22 @@ constexpr int kTileBytes = 64 * D;                 // 32 rows of one plane
 template <int NP, int D>
 constexpr int kStageRows = NP == 1 || D == 32 ? 64 : 32;
 
+// Which of a stage's R rows count: row r is bit r % 64 of word r / 64.
+template <int R>
+struct RowBits {
+  static constexpr int W = (R + 63) / 64;
+  static constexpr uint64_t kAll = R >= 64 ? ~uint64_t(0) : (uint64_t(1) << (R & 63)) - 1;
+  uint64_t w[W];
+  __device__ __forceinline__ uint32_t tile(int i) const { return (uint32_t)(w[i / 2] >> (32 * (i & 1))); }
+  __device__ __forceinline__ bool all() const {
+    bool y = true;
+#pragma unroll
+    for (int i = 0; i < W; ++i) y = y && w[i] == kAll;
+    return y;
+  }
+  __device__ __forceinline__ bool row(int r) const { return ((W == 2 && r >= 64 ? w[W - 1] : w[0]) >> (r & 63)) & 1; }
+};
+
 // R rows of D elements moved by T threads from global memory to LDS tiles: plane
 // p of rows 32 i .. 32 i + 31 at (p R/32 + i) kTileBytes. Loads go to registers
 // (load), so that their latency passes during the previous stage's products;
@@ -58,14 +74,12 @@ struct Stage {
     }
   }
 
-  // bit r of `ok`: row r counts (others become zero)
-  __device__ __forceinline__ void store(char* lds, uint64_t ok, int tid) {
-    constexpr uint64_t all = R == 64 ? ~uint64_t(0) : (uint64_t(1) << (R & 63)) - 1;
-    if (ok != all) {                               // wave-uniform
+  // rows that do not count become zero
+  __device__ __forceinline__ void store(char* lds, const RowBits<R>& ok, int tid) {
+    if (!ok.all()) {                               // wave-uniform
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const int r = (i * T + tid) / CPR;
-        const uint32_t keep = (ok >> r) & 1 ? ~0u : 0u;
+        const uint32_t keep = ok.row((i * T + tid) / CPR) ? ~0u : 0u;
 #pragma unroll
         for (int e = 0; e < LB; ++e)
 #pragma unroll
@@ -91,37 +105,60 @@ struct Stage {
   }
 };
 
-// This lane's operand addresses within a tile.
+// Head and block of workgroup p of heads x blocks. Workgroups go round the eight XCDs
+// in turn (see xcd_remap): eight heads at a time, an XCD takes one head's blocks in
+// their order, so that they share its L2. The last heads % 8 heads are shared by all
+// XCDs: causal ones block by block, since a head's blocks then differ in length and a
+// range of them per XCD leaves some idle (dK and dV of 4 key heads x 16384 x 128: the
+// first half of a head's blocks has three quarters of the work), others in ranges.
+struct HeadBlock {
+  int head, block;
+};
+__device__ __forceinline__ HeadBlock head_block(int p, int heads, int blocks, bool causal) {
+  const int rest = heads % 8, whole = (heads - rest) * blocks;
+  if (p < whole) {
+    const int q = p / (8 * blocks), r = p - q * 8 * blocks;
+    return {8 * q + r % 8, r / 8};
+  }
+  const int r = p - whole;
+  if (causal) return {heads - rest + r % rest, r / rest};
+  const int x = xcd_remap(r, rest * blocks);
+  return {heads - rest + x / blocks, x % blocks};
+}
+
+// This lane's operand addresses in LDS, of a tile at the start of `base`; a tile
+// `off` bytes further on is read with the same addresses and an offset.
 template <int D>
 struct TileAddr {
   static constexpr int KC = D / 16, NT = D / 32;
-  int rr[KC];                                      // row-layout chunk c: row l%32, columns (D/2)(l/32) + 8c ..
-  int tr[NT][2];                                   // transposed column tile t, rows + 0 and + 8
-  __device__ __forceinline__ void init() {
+  uint32_t rr[KC];                                 // row-layout chunk c: row l%32, columns (D/2)(l/32) + 8c ..
+  uint32_t tr[NT][2];                              // transposed column tile t, rows + 0 and + 8
+  __device__ __forceinline__ void init(const char* base) {
     const int lane = lane_id(), h = lane >> 5, j = lane & 31, i16 = lane & 15;
 #pragma unroll
-    for (int c = 0; c < KC; ++c) rr[c] = raw_offset<D, exact_swz<D>>(j, (D / 2) * h + 8 * c);
+    for (int c = 0; c < KC; ++c) rr[c] = lds_addr(base) + raw_offset<D, exact_swz<D>>(j, (D / 2) * h + 8 * c);
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int e = 0; e < 2; ++e)
-        tr[t][e] = raw_offset<D, exact_swz<D>>(4 * h + i16 / 4 + 8 * e, 32 * t + 16 * ((lane >> 4) & 1) + 4 * (i16 & 3));
+        tr[t][e] = lds_addr(base) +
+                   raw_offset<D, exact_swz<D>>(4 * h + i16 / 4 + 8 * e, 32 * t + 16 * ((lane >> 4) & 1) + 4 * (i16 & 3));
     // kept as they are, not put together again at each read
 #pragma unroll
     for (int c = 0; c < KC; ++c) asm("" : "+v"(rr[c]));
 #pragma unroll
     for (int t = 0; t < NT; ++t) asm("" : "+v"(tr[t][0]), "+v"(tr[t][1]));
   }
-  __device__ __forceinline__ u32x4 row(const char* tile, int c) const {
-    return *reinterpret_cast<const u32x4*>(tile + rr[c]);
+  __device__ __forceinline__ u32x4 row(int off, int c) const {
+    return *(const __attribute__((address_space(3))) u32x4*)(lds_ptr)(rr[c] + off);
   }
   // transposed chunk (u, t): rows 16u + 8(s/4) + 4(l/32) + s%4 (s = 0..7) of column 32t + l%32
-  __device__ __forceinline__ u32x4 trans(char* tile, int u, int t) const {
+  __device__ __forceinline__ u32x4 trans(int off, int u, int t) const {
     u32x2 x[2];
 #pragma unroll
     for (int e = 0; e < 2; ++e)
       x[e] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                           (__attribute__((address_space(3))) s16x4*)(tile + tr[t][e] + 16 * u * 2 * D)));
+                                           (__attribute__((address_space(3))) s16x4*)(lds_ptr)(tr[t][e] + off + 16 * u * 2 * D)));
     return u32x4{x[0][0], x[0][1], x[1][0], x[1][1]};
   }
 };
@@ -157,7 +194,7 @@ __device__ __forceinline__ void load_operand(const char* row, bool on, u32x4 (&f
 // c + A B^T over the column chunks K0 .. K1 - 1 (16 columns each): A the rows of the staged tile (plane 0 at `tile`,
 // planes `step` bytes apart), B this lane's operand; the smallest plane products first.
 template <int NP, int D, int K0, int K1>
-__device__ __forceinline__ f32x16 product_part(const TileAddr<D>& at, const char* tile, int step,
+__device__ __forceinline__ f32x16 product_part(const TileAddr<D>& at, int tile, int step,
                                                const u32x4 (&b)[NP][D / 16], f32x16 c) {
 #pragma unroll
   for (int p = NP - 1; p >= 0; --p)
@@ -171,7 +208,7 @@ __device__ __forceinline__ f32x16 product_part(const TileAddr<D>& at, const char
 }
 
 template <int NP, int D>
-__device__ __forceinline__ f32x16 product(const TileAddr<D>& at, const char* tile, int step, const u32x4 (&b)[NP][D / 16],
+__device__ __forceinline__ f32x16 product(const TileAddr<D>& at, int tile, int step, const u32x4 (&b)[NP][D / 16],
                                           const f32x16& c) {
   return product_part<NP, D, 0, D / 16>(at, tile, step, b, c);
 }
@@ -181,6 +218,45 @@ template <int NP>
 struct Packed {
   u32x4 w[NP][2];
 };
+// All row-layout chunks of a one-plane tile.
+template <int D>
+__device__ __forceinline__ void read_rows(const TileAddr<D>& at, int tile, u32x4 (&f)[D / 16]) {
+#pragma unroll
+  for (int c = 0; c < D / 16; ++c) f[c] = at.row(tile, c);
+}
+
+// All transposed chunks of a one-plane tile.
+template <int D>
+__device__ __forceinline__ void read_trans(const TileAddr<D>& at, int tile, u32x4 (&f)[2][D / 32]) {
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t) f[u][t] = at.trans(tile, u, t);
+}
+
+// o += X^T W of a one-plane tile whose transposed chunks are x.
+template <int D>
+__device__ __forceinline__ void accumulate_chunks(const u32x4 (&x)[2][D / 32], const Packed<1>& w, f32x16 (&o)[D / 32]) {
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t) o[t] = mfma16(x[u][t], w.w[0][u], o[t]);
+}
+
+// A row's number x as an operand chunk: the bfloat16 elements hi, mid, lo of x (each
+// the rest rounded, so their sum is x to 2^-24), then zeros. One more step of a
+// product, with a chunk of three ones on the other side, adds x to the row's results.
+__device__ __forceinline__ u32x4 number_chunk(float x) {
+  bf16x2 a, b;
+  a[0] = (__bf16)x;
+  const float r = x - (float)a[0];
+  a[1] = (__bf16)r;
+  b[0] = (__bf16)(r - (float)a[1]);
+  b[1] = (__bf16)0.0f;
+  return u32x4{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b), 0u, 0u};
+}
+
+// The planes of 16 weights.
 template <int NP>
 __device__ __forceinline__ Packed<NP> pack_weights(const float (&p)[16]) {
   Packed<NP> k;
@@ -209,7 +285,7 @@ __device__ __forceinline__ Packed<NP> pack_weights(const float (&p)[16]) {
 
 // o (D rows x 32 columns) += X^T W: X the staged tile, W packed weights.
 template <int NP, int D>
-__device__ __forceinline__ void accumulate_t(const TileAddr<D>& at, char* tile, int step, const Packed<NP>& w,
+__device__ __forceinline__ void accumulate_t(const TileAddr<D>& at, int tile, int step, const Packed<NP>& w,
                                              f32x16 (&o)[D / 32]) {
 #pragma unroll
   for (int u = 0; u < 2; ++u)
@@ -248,18 +324,40 @@ __device__ __forceinline__ int first_position(const ExactArgs& a, int b) {
   return a.q_start == nullptr ? a.nk - a.nq : min(max(a.q_start[b], -kFar), kFar);
 }
 
-// This lane's byte of the mask of the R keys from k0 on (nonzero: counts); a
-// lane past them repeats a valid one.
-__device__ __forceinline__ uint32_t mask_byte(const ExactArgs& a, int b, int k0) {
-  if (a.key_mask == nullptr) return 1;
-  return a.key_mask[(long long)b * a.mask_stride + min(k0 + lane_id(), a.nk - 1)];
-}
-
-// Bits of the keys k0 .. k0 + R - 1 that count.
+// This lane's bytes of the mask of the R keys from k0 on (nonzero: counts), 64 lanes
+// a word; a lane past the keys repeats the last.
 template <int R>
-__device__ __forceinline__ uint64_t key_bits(uint32_t byte, int k0, int limit) {
-  const int lane = lane_id();
-  return __ballot(lane < R && k0 + lane < limit && byte != 0);
+struct MaskBytes {
+  uint32_t b[RowBits<R>::W];
+  __device__ __forceinline__ void load(const ExactArgs& a, int batch, int k0) {
+#pragma unroll
+    for (int i = 0; i < RowBits<R>::W; ++i)
+      b[i] = a.key_mask == nullptr
+                 ? 1
+                 : a.key_mask[(long long)batch * a.mask_stride + min(k0 + 64 * i + lane_id(), a.nk - 1)];
+  }
+  // the keys k0 .. k0 + R - 1 that count
+  __device__ __forceinline__ RowBits<R> bits(int k0, int limit) const {
+    RowBits<R> ok;
+#pragma unroll
+    for (int i = 0; i < RowBits<R>::W; ++i) {
+      const int r = 64 * i + lane_id();
+      ok.w[i] = __ballot(r < R && k0 + r < limit && b[i] != 0);
+    }
+    return ok;
+  }
+};
+
+// The rows row0 .. row0 + R - 1 below limit.
+template <int R>
+__device__ __forceinline__ RowBits<R> row_bits(int row0, int limit) {
+  RowBits<R> ok;
+#pragma unroll
+  for (int i = 0; i < RowBits<R>::W; ++i) {
+    const int r = 64 * i + lane_id();
+    ok.w[i] = __ballot(r < R && row0 + r < limit);
+  }
+  return ok;
 }
 
 __device__ __forceinline__ float bias_value(const ExactArgs& a, int h, int entry) {
@@ -338,6 +436,13 @@ __device__ __forceinline__ void store_rows(const f32x16 (&o)[D / 32], float f, c
       }
     }
   }
+}
+
+// More than 64 KB of dynamic LDS has to be allowed for.
+template <class Kernel>
+inline hipError_t allow_lds(Kernel kernel, size_t smem) {
+  if (smem <= 65536) return hipSuccess;
+  return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
 }
 
 }  // namespace mra

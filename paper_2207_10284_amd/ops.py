@@ -705,7 +705,7 @@ def exact_attention_forward(q, k, v, *, scale=None, causal: bool = False, length
     h reads key head h // (H / H_kv).
 
     q: [B, H, n_q, d]; k, v: [B, H_kv, n_k, d], any strides with dense 16-byte
-    aligned rows. ``scale``: 1 / sqrt(d) if not given; positive. Query i stands
+    aligned rows. ``scale``: 1 / sqrt(d) if not given; 2^-64 to 2^64. Query i stands
     at position ``q_start[b] + i`` (int32 [B]; n_k - n_q + i if not given). A key j
     counts if j < ``lengths[b]`` (int32 [B]), ``key_mask[b, j]`` (bool or uint8
     [B, n_k]) and, with ``causal``, j is at most the position; each only where
