@@ -304,16 +304,14 @@ __global__ __launch_bounds__(kExactThreads) void exact_dkv_kernel(ExactArgs a, E
       hi = bias_value(a, h, 2 * a.far) * kLog2e;
     }
     St qs, gs;
-    float nl = 0.0f, nd = 0.0f;                    // of query tid of the stage
+    float L = 0.0f, delta = 0.0f;                  // of query tid of the stage
     auto load = [&](int q0) {
       qs.load(qp, a.q.sn, q0, a.nq, tid);
       gs.load(gp, g.dout.sn, q0, a.nq, tid);
-      if (tid < QT) {
-        const int q = min(q0 + tid, a.nq - 1);
-        const float L = g.lse[lrow + q];
-        const bool off = q0 + tid >= a.nq || L == -INFINITY;   // no weight: finite, as it meets zeros too
-        nl = off ? -3e38f : -L * inv_scale;
-        nd = off ? 0.0f : -g.delta[lrow + q];
+      if (tid < QT) {                              // as they are: looked at in store(), when they have arrived
+        const long long at_row = lrow + min(q0 + tid, a.nq - 1);
+        L = g.lse[at_row];
+        delta = g.delta[at_row];
       }
     };
     auto store = [&](int buf, int q0) {
@@ -321,9 +319,10 @@ __global__ __launch_bounds__(kExactThreads) void exact_dkv_kernel(ExactArgs a, E
       qs.store(smem + buf * 2 * St::kBytes, ok, tid);
       gs.store(smem + buf * 2 * St::kBytes + St::kBytes, ok, tid);
       if (tid < QT) {
+        const bool off = q0 + tid >= a.nq || L == -INFINITY;   // no weight: finite, as it meets zeros too
         u32x4* to = reinterpret_cast<u32x4*>(smem + NUMS) + 2 * QT * buf + tid;
-        to[0] = number_chunk(nl);
-        to[QT] = number_chunk(nd);
+        to[0] = number_chunk(off ? -3e38f : -L * inv_scale);
+        to[QT] = number_chunk(off ? 0.0f : -delta);
       }
     };
     load(first);
