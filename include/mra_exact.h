@@ -26,7 +26,7 @@
  *   (the d elements of a row are consecutive). Every stride is >= 0 and a
  *   multiple of 16 bytes. Input strides may be 0 (a broadcast axis). Outputs
  *   must not overlap themselves or another argument.
- * - d is 32, 64 or 128; 0 <= n_q, n_k <= 2^26.
+ * - d is 32, 64 or 128; 0 <= n_q, n_k <= 2^26; row strides below 2^25 bytes.
  * - What lies at a key that does not count for any query of its batch
  *   (j >= lengths[b], key_mask[b][j] == 0) may be anything, also NaN. Results
  *   for other non-finite inputs are unspecified.

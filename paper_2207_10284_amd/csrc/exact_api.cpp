@@ -15,6 +15,7 @@ thread_local int g_last_hip_error = 0;
 
 constexpr int kMaxLen = 1 << 26;
 constexpr long long kMaxGrid = 2147483647LL;
+constexpr int64_t kMaxRowStride = 1 << 25;        // bytes: 64 rows within 32 bits
 
 #define MRA_TRY(expr)                 \
   do {                                \
@@ -68,7 +69,7 @@ mra_status_t check_tensor(const mra_strided_t* t, mra_dtype_t dt) {
   if (!aligned16(t->data)) return MRA_ERR_MISALIGNED;
   const int64_t per = dt == MRA_BF16 ? 8 : 4;
   if (t->stride_b % per || t->stride_h % per || t->stride_n % per) return MRA_ERR_MISALIGNED;
-  return MRA_OK;
+  return t->stride_n < kMaxRowStride / (16 / per) ? MRA_OK : MRA_ERR_UNSUPPORTED;
 }
 
 mra::Rows rows_of(const mra_strided_t* t, mra_dtype_t dt) {

@@ -121,11 +121,13 @@ __global__ __launch_bounds__(kExactThreads) void exact_dq_kernel(ExactArgs a, Ex
   };
 
   St ks, vs;
+  ks.init(a.k.sn, tid);
+  vs.init(a.v.sn, tid);
   MaskBytes<KT> bytes;
   RowBits<KT> ok{};
   if (stages > 0) {
-    ks.load(kp, a.k.sn, 0, limit, tid);
-    vs.load(vp, a.v.sn, 0, limit, tid);
+    ks.load(kp, a.k.sn, 0, limit);
+    vs.load(vp, a.v.sn, 0, limit);
     bytes.load(a, b, 0);
     ok = bytes.bits(0, limit);
     ks.store(smem, ok, tid);
@@ -139,8 +141,8 @@ __global__ __launch_bounds__(kExactThreads) void exact_dq_kernel(ExactArgs a, Ex
     constexpr int cur = BUF * 2 * St::kBytes;
     const bool more = st + 1 < stages;
     if (more) {
-      ks.load(kp, a.k.sn, (st + 1) * KT, limit, tid);
-      vs.load(vp, a.v.sn, (st + 1) * KT, limit, tid);
+      ks.load(kp, a.k.sn, (st + 1) * KT, limit);
+      vs.load(vp, a.v.sn, (st + 1) * KT, limit);
       bytes.load(a, b, (st + 1) * KT);
     }
 #pragma unroll
@@ -304,10 +306,12 @@ __global__ __launch_bounds__(kExactThreads) void exact_dkv_kernel(ExactArgs a, E
       hi = bias_value(a, h, 2 * a.far) * kLog2e;
     }
     St qs, gs;
+    qs.init(a.q.sn, tid);
+    gs.init(g.dout.sn, tid);
     float L = 0.0f, delta = 0.0f;                  // of query tid of the stage
     auto load = [&](int q0) {
-      qs.load(qp, a.q.sn, q0, a.nq, tid);
-      gs.load(gp, g.dout.sn, q0, a.nq, tid);
+      qs.load(qp, a.q.sn, q0, a.nq);
+      gs.load(gp, g.dout.sn, q0, a.nq);
       if (tid < QT) {                              // as they are: looked at in store(), when they have arrived
         const long long at_row = lrow + min(q0 + tid, a.nq - 1);
         L = g.lse[at_row];
@@ -367,7 +371,7 @@ __global__ __launch_bounds__(kExactThreads) void exact_dkv_kernel(ExactArgs a, E
         u32x4 gt[2][NT], qt[2][NT];
         if constexpr (NP == 1) {
           read_trans<D>(at, gtile, gt);
-          read_trans<D>(at, qtile, qt);
+          if constexpr (D < 128) read_trans<D>(at, qtile, qt);
           __builtin_amdgcn_sched_barrier(0);
         }
         float mul = a.scale_log2, add = 0.0f;
@@ -392,6 +396,7 @@ __global__ __launch_bounds__(kExactThreads) void exact_dkv_kernel(ExactArgs a, E
         const Packed<NP> pw = pack_weights<NP>(p);
         if constexpr (NP == 1) accumulate_chunks<D>(gt, pw, dv);
         else accumulate_t<NP, D>(at, gtile, STEP, pw, dv);
+        if constexpr (NP == 1 && D == 128) read_trans<D>(at, qtile, qt);
 #pragma unroll
         for (int r = 0; r < 16; ++r) p[r] *= dp[r];
         const Packed<NP> dw = pack_weights<NP>(p);

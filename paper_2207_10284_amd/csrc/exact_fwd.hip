@@ -204,11 +204,13 @@ __global__ __launch_bounds__(kExactThreads) void exact_fwd_kernel(ExactArgs a, f
   }
 
   St ks, vs;
+  ks.init(a.k.sn, tid);
+  vs.init(a.v.sn, tid);
   MaskBytes<KT> bytes;
   RowBits<KT> ok{};
   if (stages > 0) {
-    ks.load(kp, a.k.sn, 0, limit, tid);
-    vs.load(vp, a.v.sn, 0, limit, tid);
+    ks.load(kp, a.k.sn, 0, limit);
+    vs.load(vp, a.v.sn, 0, limit);
     bytes.load(a, b, 0);
     ok = bytes.bits(0, limit);
     ks.store(smem, ok, tid);
@@ -221,8 +223,8 @@ __global__ __launch_bounds__(kExactThreads) void exact_fwd_kernel(ExactArgs a, f
     constexpr int kbuf = BUF * 2 * St::kBytes, vbuf = kbuf + St::kBytes;
     const bool more = st + 1 < stages;
     if (more) {
-      ks.load(kp, a.k.sn, (st + 1) * KT, limit, tid);
-      vs.load(vp, a.v.sn, (st + 1) * KT, limit, tid);
+      ks.load(kp, a.k.sn, (st + 1) * KT, limit);
+      vs.load(vp, a.v.sn, (st + 1) * KT, limit);
       bytes.load(a, b, (st + 1) * KT);
     }
 #pragma unroll
@@ -320,11 +322,13 @@ __global__ __launch_bounds__(kExactThreads) void exact_split_kernel(ExactArgs a,
     hi = bias_value(a, h, 2 * a.far) * kLog2e;
   }
   St ks, vs;
+  ks.init(a.k.sn, lane);
+  vs.init(a.v.sn, lane);
   MaskBytes<32> bytes;
   int t = t0 + w;
   if (t < t1) {
-    ks.load(kp, a.k.sn, t * 32, limit, lane);
-    vs.load(vp, a.v.sn, t * 32, limit, lane);
+    ks.load(kp, a.k.sn, t * 32, limit);
+    vs.load(vp, a.v.sn, t * 32, limit);
     bytes.load(a, b, t * 32);
   }
   wait_loads<0>();                                 // Q too: no wait for it beside the loads in flight below
@@ -334,14 +338,14 @@ __global__ __launch_bounds__(kExactThreads) void exact_split_kernel(ExactArgs a,
     ks.store(slot, ok, lane);
     wave_lds_sync();
     const bool more = t + kExactWaves < t1;
-    if (more) ks.load(kp, a.k.sn, k0 + 32 * kExactWaves, limit, lane);
+    if (more) ks.load(kp, a.k.sn, k0 + 32 * kExactWaves, limit);
     f32x16 s1[1] = {product<NP, D>(at, 0, kTileBytes<D>, row.qf, splat16(0.0f))};
     f32x16& s = s1[0];
     wave_lds_sync();
     vs.store(slot, ok, lane);
     wave_lds_sync();
     if (more) {
-      vs.load(vp, a.v.sn, k0 + 32 * kExactWaves, limit, lane);
+      vs.load(vp, a.v.sn, k0 + 32 * kExactWaves, limit);
       bytes.load(a, b, k0 + 32 * kExactWaves);
     }
     const uint32_t kb = ok.tile(0), bits = a.causal ? kb & low_bits(pos - k0 + 1) : kb;

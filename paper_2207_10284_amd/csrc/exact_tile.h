@@ -62,15 +62,24 @@ struct Stage {
   static constexpr int kBytes = NP * R * D * 2;
   static_assert(N >= 1 && R * CPR % T == 0, "whole units per thread");
   u32x4 v[N][LB];
+  static constexpr int ROWS = T / CPR;             // rows that the threads' units i cover
+  static_assert(T % CPR == 0, "whole rows");
+  uint32_t off;                                    // of this thread's units from their first row on
 
-  // rows row0 .. row0 + R - 1; those at or past limit (> 0) repeat row limit - 1
-  __device__ __forceinline__ void load(const char* base, long long sn, int row0, int limit, int tid) {
+  __device__ __forceinline__ void init(long long sn, int tid) {
+    off = (uint32_t)(tid / CPR) * (uint32_t)sn + (tid % CPR) * LB * 16;
+  }
+
+  // rows row0 .. row0 + R - 1; those at or past limit are zero. One buffer per unit,
+  // whose range ends with the last row (row strides are below 2^25 bytes), so a load needs no
+  // vector instruction for its address or its bounds.
+  __device__ __forceinline__ void load(const char* base, long long sn, int row0, int limit) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int u = i * T + tid, r = min(row0 + u / CPR, limit - 1);
-      const u32x4* src = reinterpret_cast<const u32x4*>(base + (long long)r * sn) + (u % CPR) * LB;
+      const int r = row0 + i * ROWS, rows = min(limit - r, ROWS);
+      const i32x4 rs = buffer_rsrc(base + (long long)r * sn, rows > 0 ? (unsigned)(rows - 1) * (unsigned)sn + CPR * LB * 16 : 0u);
 #pragma unroll
-      for (int e = 0; e < LB; ++e) v[i][e] = src[e];
+      for (int e = 0; e < LB; ++e) v[i][e] = __builtin_bit_cast(u32x4, mra_raw_buffer_load_f32x4(rs, (int)off + 16 * e, 0, 0));
     }
   }
 

@@ -85,7 +85,7 @@ def test_tensors_refused(lib):
     p = problem()
     assert forward(lib, None) == INVALID and backward(lib, None) == INVALID
     for bad, status in ((tensor(None), INVALID), (tensor(A + 8), MISALIGNED), (tensor(n=-64), INVALID),
-                        (tensor(n=68), MISALIGNED), (tensor(h=4), MISALIGNED), (tensor(b=12), MISALIGNED)):
+                        (tensor(n=68), MISALIGNED), (tensor(n=1 << 24), UNSUPPORTED), (tensor(h=4), MISALIGNED), (tensor(b=12), MISALIGNED)):
         for name in ("q", "k", "v", "out"):
             assert forward(lib, p, **{name: bad}) == status, (name, status)
         for name in ("q", "k", "v", "out", "dout", "dq", "dk", "dv"):
