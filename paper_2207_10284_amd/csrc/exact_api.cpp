@@ -100,17 +100,25 @@ mra::ExactArgs args_of(const mra_exact_problem_t& p) {
   return a;
 }
 
-// Workspace of the backward: delta per query, then (with a bias) the diagonal sums.
+// Workspace of the backward: delta per query, the diagonal sums (with a bias), the
+// partial sums of dq, dk and dv.
 struct WsBackward {
-  size_t diag, total;
+  mra::BackwardPlan plan;
+  size_t diag, q, k, v, total;
 };
 
 WsBackward ws_backward(const mra_exact_problem_t& p) {
   WsBackward w{};
-  w.diag = align256((size_t)p.B * p.H * p.n_q * sizeof(float));
-  w.total = w.diag;
+  w.plan = mra::exact_backward_plan(p);
+  size_t off = align256((size_t)p.B * p.H * p.n_q * sizeof(float));
+  w.diag = off;
   if (p.bias != nullptr)
-    w.total += align256((size_t)p.B * p.H * mra::exact_dq_blocks(p.n_q) * mra::exact_window(p.far) * sizeof(float));
+    off += align256((size_t)p.B * p.H * mra::exact_dq_blocks(p.n_q) * w.plan.dq_parts * mra::exact_window(p.far) *
+                    sizeof(float));
+  w.q = off; off += align256(w.plan.q_floats * sizeof(float));
+  w.k = off; off += align256(w.plan.k_floats * sizeof(float));
+  w.v = off; off += align256(w.plan.k_floats * sizeof(float));
+  w.total = off;
   return w;
 }
 
@@ -188,15 +196,21 @@ mra_status_t mra_exact_backward(const mra_exact_problem_t* p, const mra_strided_
     g.dk = rows_of(dk, p->dtype);
     g.dv = rows_of(dv, p->dtype);
   }
+  mra::BackwardPlan plan{1, 1, 0, 0};
   if (rows) {
     const WsBackward w = ws_backward(*p);
     MRA_TRY(check_workspace(workspace, workspace_bytes, w.total));
-    g.delta = static_cast<float*>(workspace);
-    if (dbias != nullptr) g.diag = reinterpret_cast<float*>(static_cast<char*>(workspace) + w.diag);
+    plan = w.plan;
+    auto at = [&](size_t off) { return reinterpret_cast<float*>(static_cast<char*>(workspace) + off); };
+    g.delta = at(0);
+    if (dbias != nullptr) g.diag = at(w.diag);
+    g.part_q = at(w.q);
+    g.part_k = at(w.k);
+    g.part_v = at(w.v);
   }
   g.dbias = dbias;
   if (!rows && !keys && (dbias == nullptr || p->H == 0)) return MRA_OK;
-  return hip_status(mra::launch_exact_backward(a, g, p->d, (int)p->dtype, static_cast<hipStream_t>(stream)));
+  return hip_status(mra::launch_exact_backward(a, g, plan, p->d, (int)p->dtype, static_cast<hipStream_t>(stream)));
 }
 
 int mra_exact_last_hip_error(void) { return g_last_hip_error; }

@@ -48,12 +48,21 @@ struct ExactGrads {
   Rows dout, dq, dk, dv;
   const float* lse;
   float* delta;                           // [B, H, n_q]: G . Z per query
-  float* diag;                            // [H, parts, window]: sums of dS over diagonals (bias gradient only)
+  float* diag;                            // [H, B, blocks, parts, window]: sums of dS over diagonals (bias gradient only)
   void* dbias;
+  float *part_q, *part_k, *part_v;        // [parts, B, heads, n, d]: see BackwardPlan
 };
+
+// How many workgroups share a block of the passes, and the floats of their partial sums.
+struct BackwardPlan {
+  int dq_parts, dkv_parts;
+  size_t q_floats, k_floats;              // of dq; of dk, and of dv (0: one part)
+};
+BackwardPlan exact_backward_plan(const mra_exact_problem_t& p);
 // Query blocks of the dQ pass per head and floats of a block's diagonal sums.
 int exact_dq_blocks(int nq);
 int exact_window(int far);
-hipError_t launch_exact_backward(const ExactArgs& a, const ExactGrads& g, int d, int dtype, hipStream_t stream);
+hipError_t launch_exact_backward(const ExactArgs& a, const ExactGrads& g, const BackwardPlan& plan, int d, int dtype,
+                                 hipStream_t stream);
 
 }  // namespace mra

@@ -136,30 +136,33 @@ __device__ __forceinline__ HeadBlock head_block(int p, int heads, int blocks, bo
 }
 
 // This lane's operand addresses in LDS, of a tile at the start of `base`; a tile
-// `off` bytes further on is read with the same addresses and an offset.
-template <int D>
+// `off` bytes further on is read with the same addresses and an offset. FEW (D = 128):
+// the chunks and column tiles differ from the first by an exclusive or, made at each
+// read, where registers decide how many waves a SIMD holds.
+template <int D, bool FEW = false>
 struct TileAddr {
   static constexpr int KC = D / 16, NT = D / 32;
-  uint32_t rr[KC];                                 // row-layout chunk c: row l%32, columns (D/2)(l/32) + 8c ..
-  uint32_t tr[NT][2];                              // transposed column tile t, rows + 0 and + 8
+  static_assert(!FEW || D == 128, "eight chunks and four column tiles within the swizzle's blocks");
+  uint32_t rr[FEW ? 1 : KC];                      // row-layout chunk c: row l%32, columns (D/2)(l/32) + 8c ..
+  uint32_t tr[FEW ? 1 : NT][2];                   // transposed column tile t, rows + 0 and + 8
   __device__ __forceinline__ void init(const char* base) {
     const int lane = lane_id(), h = lane >> 5, j = lane & 31, i16 = lane & 15;
 #pragma unroll
-    for (int c = 0; c < KC; ++c) rr[c] = lds_addr(base) + raw_offset<D, exact_swz<D>>(j, (D / 2) * h + 8 * c);
+    for (int c = 0; c < (FEW ? 1 : KC); ++c) rr[c] = lds_addr(base) + raw_offset<D, exact_swz<D>>(j, (D / 2) * h + 8 * c);
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
+    for (int t = 0; t < (FEW ? 1 : NT); ++t)
 #pragma unroll
       for (int e = 0; e < 2; ++e)
         tr[t][e] = lds_addr(base) +
                    raw_offset<D, exact_swz<D>>(4 * h + i16 / 4 + 8 * e, 32 * t + 16 * ((lane >> 4) & 1) + 4 * (i16 & 3));
     // kept as they are, not put together again at each read
 #pragma unroll
-    for (int c = 0; c < KC; ++c) asm("" : "+v"(rr[c]));
+    for (int c = 0; c < (FEW ? 1 : KC); ++c) asm("" : "+v"(rr[c]));
 #pragma unroll
-    for (int t = 0; t < NT; ++t) asm("" : "+v"(tr[t][0]), "+v"(tr[t][1]));
+    for (int t = 0; t < (FEW ? 1 : NT); ++t) asm("" : "+v"(tr[t][0]), "+v"(tr[t][1]));
   }
   __device__ __forceinline__ u32x4 row(int off, int c) const {
-    return *(const __attribute__((address_space(3))) u32x4*)(lds_ptr)(rr[c] + off);
+    return *(const __attribute__((address_space(3))) u32x4*)(lds_ptr)((FEW ? rr[0] ^ 16u * c : rr[FEW ? 0 : c]) + off);
   }
   // transposed chunk (u, t): rows 16u + 8(s/4) + 4(l/32) + s%4 (s = 0..7) of column 32t + l%32
   __device__ __forceinline__ u32x4 trans(int off, int u, int t) const {
@@ -167,7 +170,8 @@ struct TileAddr {
 #pragma unroll
     for (int e = 0; e < 2; ++e)
       x[e] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                           (__attribute__((address_space(3))) s16x4*)(lds_ptr)(tr[t][e] + off + 16 * u * 2 * D)));
+                                           (__attribute__((address_space(3))) s16x4*)(lds_ptr)(
+                                               (FEW ? tr[0][e] ^ 64u * t : tr[FEW ? 0 : t][e]) + off + 16 * u * 2 * D)));
     return u32x4{x[0][0], x[0][1], x[1][0], x[1][1]};
   }
 };
@@ -202,22 +206,28 @@ __device__ __forceinline__ void load_operand(const char* row, bool on, u32x4 (&f
 
 // c + A B^T over the column chunks K0 .. K1 - 1 (16 columns each): A the rows of the staged tile (plane 0 at `tile`,
 // planes `step` bytes apart), B this lane's operand; the smallest plane products first.
-template <int NP, int D, int K0, int K1>
-__device__ __forceinline__ f32x16 product_part(const TileAddr<D>& at, int tile, int step,
+template <int NP, int D, int K0, int K1, class At>
+__device__ __forceinline__ f32x16 product_part(const At& a, int tile, int step,
                                                const u32x4 (&b)[NP][D / 16], f32x16 c) {
+  constexpr int C = K1 - K0 < 2 ? K1 - K0 : 2;     // chunks read together, ahead of their products
 #pragma unroll
   for (int p = NP - 1; p >= 0; --p)
 #pragma unroll
-    for (int k = K0; k < K1; ++k) {
-      const u32x4 a = at.row(tile + p * step, k);
+    for (int k0 = K0; k0 < K1; k0 += C) {
+      u32x4 x[C];
 #pragma unroll
-      for (int q = NP - 1 - p; q >= 0; --q) c = mfma16(a, b[q][k], c);
+      for (int i = 0; i < C; ++i) x[i] = a.row(tile + p * step, k0 + i);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < C; ++i)
+#pragma unroll
+        for (int q = NP - 1 - p; q >= 0; --q) c = mfma16(x[i], b[q][k0 + i], c);
     }
   return c;
 }
 
-template <int NP, int D>
-__device__ __forceinline__ f32x16 product(const TileAddr<D>& at, int tile, int step, const u32x4 (&b)[NP][D / 16],
+template <int NP, int D, class At>
+__device__ __forceinline__ f32x16 product(const At& at, int tile, int step, const u32x4 (&b)[NP][D / 16],
                                           const f32x16& c) {
   return product_part<NP, D, 0, D / 16>(at, tile, step, b, c);
 }
@@ -228,15 +238,15 @@ struct Packed {
   u32x4 w[NP][2];
 };
 // All row-layout chunks of a one-plane tile.
-template <int D>
-__device__ __forceinline__ void read_rows(const TileAddr<D>& at, int tile, u32x4 (&f)[D / 16]) {
+template <int D, class At>
+__device__ __forceinline__ void read_rows(const At& at, int tile, u32x4 (&f)[D / 16]) {
 #pragma unroll
   for (int c = 0; c < D / 16; ++c) f[c] = at.row(tile, c);
 }
 
 // All transposed chunks of a one-plane tile.
-template <int D>
-__device__ __forceinline__ void read_trans(const TileAddr<D>& at, int tile, u32x4 (&f)[2][D / 32]) {
+template <int D, class At>
+__device__ __forceinline__ void read_trans(const At& at, int tile, u32x4 (&f)[2][D / 32]) {
 #pragma unroll
   for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -292,20 +302,23 @@ __device__ __forceinline__ Packed<NP> pack_weights(const float (&p)[16]) {
   return k;
 }
 
-// o (D rows x 32 columns) += X^T W: X the staged tile, W packed weights.
-template <int NP, int D>
-__device__ __forceinline__ void accumulate_t(const TileAddr<D>& at, int tile, int step, const Packed<NP>& w,
+// o (D rows x 32 columns) += X^T W: X the staged tile, W packed weights. A plane's chunks
+// of all column tiles are read together, and their products are independent.
+template <int NP, int D, class At>
+__device__ __forceinline__ void accumulate_t(const At& at, int tile, int step, const Packed<NP>& w,
                                              f32x16 (&o)[D / 32]) {
 #pragma unroll
   for (int u = 0; u < 2; ++u)
 #pragma unroll
-    for (int t = 0; t < D / 32; ++t)
+    for (int p = NP - 1; p >= 0; --p) {
+      u32x4 x[D / 32];
 #pragma unroll
-      for (int p = NP - 1; p >= 0; --p) {
-        const u32x4 x = at.trans(tile + p * step, u, t);
+      for (int t = 0; t < D / 32; ++t) x[t] = at.trans(tile + p * step, u, t);
 #pragma unroll
-        for (int q = NP - 1 - p; q >= 0; --q) o[t] = mfma16(x, w.w[q][u], o[t]);
-      }
+      for (int q = NP - 1 - p; q >= 0; --q)
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t) o[t] = mfma16(x[t], w.w[q][u], o[t]);
+    }
 }
 
 // Register r of a product holds row 8(r/4) + 4(l/32) + r%4 of its 32.

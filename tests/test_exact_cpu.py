@@ -98,7 +98,7 @@ def test_tensors_refused(lib):
 
 
 def test_workspaces_refused(lib):
-    p = problem(n_k=4096)                                           # few rows: the keys are shared
+    p = problem(n_k=4096)                                           # few rows: workgroups share the keys
     need = lib.mra_exact_forward_workspace_bytes(ctypes.byref(p))
     assert need > 0
     assert forward(lib, p, size=need - 1) == WORKSPACE
@@ -107,7 +107,7 @@ def test_workspaces_refused(lib):
     assert need >= 2 * 40 * 4
     assert backward(lib, p, size=need - 1) == WORKSPACE
     assert backward(lib, p, ws=None) == INVALID and backward(lib, p, ws=A + 4) == MISALIGNED
-    wide = problem(bias=A, buckets=8, bucket_map=A, far=20)
+    wide = problem(n_k=4096, bias=A, buckets=8, bucket_map=A, far=20)
     assert lib.mra_exact_backward_workspace_bytes(ctypes.byref(wide)) > need
 
 
