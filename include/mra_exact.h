@@ -27,6 +27,8 @@
  *   multiple of 16 bytes. Input strides may be 0 (a broadcast axis). Outputs
  *   must not overlap themselves or another argument.
  * - d is 32, 64 or 128; 0 <= n_q, n_k <= 2^26; row strides below 2^25 bytes.
+ * - A bias of -infinity (in float32, also one below -2^126) takes its distances
+ *   out: such a key does not count. Other entries are finite.
  * - What lies at a key that does not count for any query of its batch
  *   (j >= lengths[b], key_mask[b][j] == 0) may be anything, also NaN. Results
  *   for other non-finite inputs are unspecified.

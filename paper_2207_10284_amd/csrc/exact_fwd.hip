@@ -25,9 +25,10 @@ namespace mra {
 // has a key plus kMargin. A tile whose weights sum to more than kCap in some lane
 // moves the references of its queries to its own max plus kMargin and forms its
 // weights again, so an ordinary tile has no max, no exchange between lanes and no
-// rescaling. The largest weight of a query stays above 2^-(kMargin + 1).
+// rescaling. No weight exceeds 1, so the accumulators overflow only where the sum of |v|
+// does, and the largest weight of a query stays above 2^-(kMargin + 1).
 constexpr float kMargin = 16.0f;
-constexpr float kCap = 0x1p32f;
+constexpr float kCap = 1.0f;
 
 template <int NP, int D>
 struct FwdRow {
@@ -91,8 +92,8 @@ __device__ __forceinline__ void tile_weights(FwdRow<NP, D> (&row)[R], const f32x
     bool fits = true;
 #pragma unroll
     for (int x = 0; x < R; ++x) {
-      // moved and still without a key: every s is -inf
-      t[x] = row[x].weights(s[x], mul[x], again && row[x].ref == -INFINITY ? 0.0f : add[x] - row[x].ref, w[x]);
+      // moved and still without a key: every s or the bias is -inf
+      t[x] = row[x].weights(s[x], mul[x], again && row[x].ref == -INFINITY ? add[x] : add[x] - row[x].ref, w[x]);
       fits = fits && t[x] <= kCap;                 // not so for a query's first tile (ref -inf)
     }
     if (again || __ballot(!fits) == 0) break;

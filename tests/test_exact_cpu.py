@@ -280,6 +280,92 @@ def test_stage_writes_each_chunk_once(d, rows, threads):
             assert at[off(j, d // 2 * h + 8 * c)] == (j, d // 2 * h + 8 * c)
 
 
+def swz(d, r):
+    return 4 * (r & 3) + ((r >> 2) & 3) if d == 128 else (4 * ((r >> 1) & 1) + ((r >> 2) & 3) if d == 64 else (r >> 2) & 3)
+
+
+def test_few_addresses():
+    """d = 128: a lane's row chunk c and its transposed column tile t sit at the
+    first's address exclusive-or 16 c and 64 t."""
+    off = lambda r, c: r * 256 + (((2 * c >> 4) ^ swz(128, r)) << 4) + (2 * c & 15)
+    for lane in range(64):
+        h, j, i16 = lane >> 5, lane & 31, lane & 15
+        for c in range(8):
+            assert off(j, 64 * h + 8 * c) == off(j, 64 * h) ^ 16 * c
+        for e in range(2):
+            r, c0 = 4 * h + i16 // 4 + 8 * e, 16 * ((lane >> 4) & 1) + 4 * (i16 & 3)
+            for t in range(4):
+                assert off(r, 32 * t + c0) == off(r, c0) ^ 64 * t
+
+
+@pytest.mark.parametrize("elem,d,rows,threads", [(2, 32, 64, 256), (2, 64, 64, 256), (2, 128, 64, 256), (4, 32, 64, 256),
+                                                 (4, 64, 32, 256), (4, 128, 32, 256), (2, 128, 32, 64), (4, 32, 32, 64)])
+def test_stage_buffers_end_with_the_last_row(elem, d, rows, threads):
+    """The loads of a unit's buffer are in its range exactly for the rows that
+    count (range: the last such row's end), for rows side by side and apart."""
+    cpr, loads = d // 8, elem // 2
+    per = threads // cpr
+    for stride in (d * elem, 3 * d * elem, (1 << 25) - 16):
+        for left in (1, 2, 31, 32, 33, 63, 64, 100):
+            for i in range(rows * cpr // threads):
+                n = min(left - i * per, per)
+                size = (n - 1) * stride + cpr * loads * 16 if n > 0 else 0
+                assert size < 1 << 32
+                for tid in {0, 1, cpr - 1, cpr, threads // 2, threads - 1} | {max(0, min(n, per - 1)) * cpr}:
+                    for e in range(loads):
+                        at = tid // cpr * stride + tid % cpr * loads * 16 + 16 * e
+                        assert at + 16 < 1 << 32
+                        assert (at + 16 <= size) == (i * per + tid // cpr < left)
+
+
+def head_block(p, heads, blocks, causal):
+    rest = heads % 8
+    whole = (heads - rest) * blocks
+    if p < whole:
+        q, r = divmod(p, 8 * blocks)
+        return 8 * q + r % 8, r // 8
+    r = p - whole
+    if causal:
+        return heads - rest + r % rest, r // rest
+    total = rest * blocks
+    x, slot, q, m = r % 8, r // 8, total // 8, total % 8
+    x = x * (q + 1) + slot if x < m else m * (q + 1) + (x - m) * q + slot
+    return heads - rest + x // blocks, x % blocks
+
+
+@pytest.mark.parametrize("causal", [False, True])
+def test_head_blocks_are_each_taken_once(causal):
+    for heads in (1, 3, 7, 8, 9, 12, 96):
+        for blocks in (1, 2, 5, 13, 64):
+            got = {head_block(p, heads, blocks, causal) for p in range(heads * blocks)}
+            assert got == {(h, b) for h in range(heads) for b in range(blocks)}
+
+
+def test_parts_cover_every_stage_once():
+    """Ranges of the stages of all heads, head after head (dK, dV)."""
+    for group in (1, 3, 8):
+        for stages in (0, 1, 2, 7, 40):
+            for parts in (1, 2, 6, 8):
+                seen = []
+                for part in range(parts):
+                    t0, t1 = group * stages * part // parts, group * stages * (part + 1) // parts
+                    hg = t0 // stages if stages else group
+                    while hg < group and hg * stages < t1:
+                        seen += [(hg, st) for st in range(max(t0 - hg * stages, 0), min(t1 - hg * stages, stages))]
+                        hg += 1
+                assert seen == [(h, st) for h in range(group) for st in range(stages)]
+
+
+def test_number_chunk():
+    """hi + mid + lo, each the rest rounded to bfloat16, are the number to 2^-24."""
+    x = torch.cat([torch.randn(1000, generator=torch.Generator().manual_seed(1)) * 10.0 ** e for e in range(-3, 6)])
+    x = torch.cat([x, torch.tensor([0.0, -3e38, 1e-20])])
+    hi = x.bfloat16().float()
+    mid = (x - hi).bfloat16().float()
+    lo = (x - hi - mid).bfloat16().float()
+    assert ((hi.double() + mid + lo - x).abs() <= 2.0 ** -24 * x.abs()).all()
+
+
 def test_lds_fits():
     """Dynamic LDS of every launch, at the widest window, within 160 KB."""
     for planes, d in ((p, d) for p in (1, 3) for d in (32, 64, 128)):
