@@ -36,11 +36,13 @@ constexpr bool kDqTwo = NP == 1 && D == 128;
 template <int NP, int D>
 constexpr int kDqStageRows = kDqTwo<NP, D> ? 32 : kStageRows<NP, D>;
 
-template <int NP, int D, bool BIAS>
-__global__ __launch_bounds__(kExactThreads, (kDqTwo<NP, D> ? 2 : 1)) void exact_dq_kernel(ExactArgs a, ExactGrads g, int qblocks) {
+// RT: 32-row tiles of queries per wave
+template <int NP, int D, int RT, bool BIAS>
+__global__ __launch_bounds__(kExactThreads, (kDqTwo<NP, D> || RT == 2 ? 2 : 1)) void exact_dq_kernel(ExactArgs a, ExactGrads g, int qblocks) {
   constexpr int KT = kDqStageRows<NP, D>, TILES = KT / 32, KC = D / 16, NT = D / 32;
   using St = Stage<NP, D, KT, kExactThreads>;
-  constexpr int STEP = TILES * kTileBytes<D>;
+  constexpr int STEP = TILES * kTileBytes<D>, ROWS = kDqRows * RT;
+  static_assert(RT == 1 || (!BIAS && NP == 1), "one bias, one plane");
   extern __shared__ __attribute__((aligned(16))) char smem[];
   float* win = reinterpret_cast<float*>(smem + 4 * St::kBytes);
   const int entries = BIAS ? window_entries(a.far) : 0;
@@ -50,9 +52,9 @@ __global__ __launch_bounds__(kExactThreads, (kDqTwo<NP, D> ? 2 : 1)) void exact_
   const int bh = hb.head, qb = qblocks - 1 - hb.block;             // causal: the longest first
   const int part = blockIdx.y, parts = gridDim.y;
   const int b = bh / a.H, h = bh - b * a.H, hk = h / a.group;
-  const int row0 = qb * kDqRows + w * 32, i = row0 + (lane & 31), ic = min(i, a.nq - 1);
+  const int row0 = qb * ROWS + w * 32 * RT, i0 = row0 + (lane & 31);      // this lane's query of tile y: i0 + 32 y
   const int limit = key_limit(a, b), start = first_position(a, b);
-  const int kend = a.causal ? min(limit, start + min((qb + 1) * kDqRows, a.nq)) : limit;
+  const int kend = a.causal ? min(limit, start + min((qb + 1) * ROWS, a.nq)) : limit;
   const int all_stages = kend > 0 ? (kend + KT - 1) / KT : 0;
   // this workgroup's part of them
   const int begin = parts == 1 ? 0 : (int)((long long)all_stages * part / parts);
@@ -63,40 +65,43 @@ __global__ __launch_bounds__(kExactThreads, (kDqTwo<NP, D> ? 2 : 1)) void exact_
 
   TileAddr<D, kDqTwo<NP, D>> at;
   at.init(smem);
-  u32x4 qf[NP][KC], gf[NP][KC];
-  f32x16 dq[NT];
+  u32x4 qf[RT][NP][KC], gf[RT][NP][KC];
+  f32x16 dq[RT][NT];
+  float delta[RT], nl[RT];
 #pragma unroll
-  for (int t = 0; t < NT; ++t) dq[t] = splat16(0.0f);
-  load_operand<NP, D>(a.q.p + b * a.q.sb + h * a.q.sh + ic * a.q.sn, i < a.nq, qf);
-  float delta = 0.0f;
-  {
+  for (int y = 0; y < RT; ++y) {
+    const int i = i0 + 32 * y, ic = min(i, a.nq - 1);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) dq[y][t] = splat16(0.0f);
+    load_operand<NP, D>(a.q.p + b * a.q.sb + h * a.q.sh + ic * a.q.sn, i < a.nq, qf[y]);
     constexpr int LB = NP == 1 ? KC : 2 * KC;
     const int half = hf * (D / 2) * (NP == 1 ? 2 : 4);
     const u32x4* gr = reinterpret_cast<const u32x4*>(g.dout.p + b * g.dout.sb + h * g.dout.sh + ic * g.dout.sn + half);
     const u32x4* zr = reinterpret_cast<const u32x4*>(a.out.p + b * a.out.sb + h * a.out.sh + ic * a.out.sn + half);
+    float d = 0.0f;
 #pragma unroll
     for (int c = 0; c < LB; ++c) {
-      const u32x4 x = gr[c], y = zr[c];
+      const u32x4 u = gr[c], v = zr[c];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         if constexpr (NP == 1) {
-          delta = fmaf(bf16_to_f32(x[e] & 0xFFFFu), bf16_to_f32(y[e] & 0xFFFFu), delta);
-          delta = fmaf(bf16_to_f32(x[e] >> 16), bf16_to_f32(y[e] >> 16), delta);
+          d = fmaf(bf16_to_f32(u[e] & 0xFFFFu), bf16_to_f32(v[e] & 0xFFFFu), d);
+          d = fmaf(bf16_to_f32(u[e] >> 16), bf16_to_f32(v[e] >> 16), d);
         } else {
-          delta = fmaf(__uint_as_float(x[e]), __uint_as_float(y[e]), delta);
+          d = fmaf(__uint_as_float(u[e]), __uint_as_float(v[e]), d);
         }
       }
     }
-    delta = halves_sum(delta);
+    d = halves_sum(d);
+    load_operand<NP, D>(g.dout.p + b * g.dout.sb + h * g.dout.sh + ic * g.dout.sn, i < a.nq, gf[y]);
+    const long long at_row = (long long)bh * a.nq + ic;
+    const float L = g.lse[at_row];
+    if (part == 0 && lane < 32 && i < a.nq) g.delta[at_row] = d;
+    // no key counts: no weight; the same for rows past the last
+    const bool none = i >= a.nq || L == -INFINITY;
+    nl[y] = none ? -INFINITY : -L * kLog2e;
+    delta[y] = none ? 0.0f : d;
   }
-  load_operand<NP, D>(g.dout.p + b * g.dout.sb + h * g.dout.sh + ic * g.dout.sn, i < a.nq, gf);
-  const long long at_row = (long long)bh * a.nq + ic;
-  const float L = g.lse[at_row];
-  if (part == 0 && lane < 32 && i < a.nq) g.delta[at_row] = delta;
-  // no key counts: no weight; the same for rows past the last
-  const bool none = i >= a.nq || L == -INFINITY;
-  const float nl = none ? -INFINITY : -L * kLog2e;
-  if (none) delta = 0.0f;
   float lo = 0.0f, hi = 0.0f, sum_lo = 0.0f, sum_hi = 0.0f;
   float* mine = acc + w * entries;
   float* skew = acc + kExactWaves * entries + w * kSkew;
@@ -118,18 +123,18 @@ __global__ __launch_bounds__(kExactThreads, (kDqTwo<NP, D> ? 2 : 1)) void exact_
 #pragma unroll
     for (int p = 0; p < NP; ++p)
 #pragma unroll
-      for (int c = KC / 2; c < KC; ++c) gf[p][c] ^= 0x80008000u;
+      for (int c = KC / 2; c < KC; ++c) gf[0][p][c] ^= 0x80008000u;
   }
   auto values_product = [&](int vtile) -> f32x16 {
     if constexpr (kTwoSigns) {
-      const f32x16 x = product_part<NP, D, 0, KC / 2>(at, vtile, STEP, gf, splat16(0.0f));
-      const f32x16 y = product_part<NP, D, KC / 2, KC>(at, vtile, STEP, gf, splat16(0.0f));
+      const f32x16 x = product_part<NP, D, 0, KC / 2>(at, vtile, STEP, gf[0], splat16(0.0f));
+      const f32x16 y = product_part<NP, D, KC / 2, KC>(at, vtile, STEP, gf[0], splat16(0.0f));
       f32x16 z;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) z[r] = (x[r] - y[r]) - delta;
+      for (int r = 0; r < 16; ++r) z[r] = (x[r] - y[r]) - delta[0];
       return z;
     } else {
-      return product<NP, D>(at, vtile, STEP, gf, splat16(-delta));
+      return product<NP, D>(at, vtile, STEP, gf[0], splat16(-delta[0]));
     }
   };
 
@@ -148,6 +153,7 @@ __global__ __launch_bounds__(kExactThreads, (kDqTwo<NP, D> ? 2 : 1)) void exact_
   }
   __syncthreads();
   wait_loads<0>();                                 // the operands too: no wait for them beside the loads in flight below
+  constexpr bool kSub = kDqTwo<NP, D> || RT == 2;  // delta subtracted by the vector ALU: 16 registers fewer
   // stage st in buffer BUF (known at compile time: its part of an LDS address is an
   // offset); PLAIN: every key counts for every query, no bias
   auto stage = [&](int st, auto BUF, auto PLAIN) {
@@ -162,78 +168,86 @@ __global__ __launch_bounds__(kExactThreads, (kDqTwo<NP, D> ? 2 : 1)) void exact_
     for (int x = 0; x < TILES; ++x) {
       const uint32_t kb = PLAIN ? ~0u : ok.tile(x);
       const int k0 = st * KT + 32 * x, ktile = cur + x * kTileBytes<D>, vtile = cur + St::kBytes + x * kTileBytes<D>;
-      if (!PLAIN && (kb == 0 || (a.causal && k0 > pos0 + 31))) continue;
-      f32x16 s, dp;
-      u32x4 kt[2][NT];
+      if (!PLAIN && (kb == 0 || (a.causal && k0 > pos0 + 32 * RT - 1))) continue;
+      u32x4 kr[KC], vr[KC], kt[2][NT];             // one plane only
       if constexpr (NP == 1) {
-        u32x4 kr[KC], vr[KC];
         read_rows<D>(at, ktile, kr);
         if constexpr (D < 128) read_rows<D>(at, vtile, vr);
         __builtin_amdgcn_sched_barrier(0);
-        s = splat16(0.0f);
-        dp = splat16(D < 128 ? -delta : 0.0f);
-        if constexpr (D < 128) {
+      }
+      Packed<NP> dw[RT];
 #pragma unroll
-          for (int c = 0; c < KC; ++c) {
-            s = mfma16(kr[c], qf[0][c], s);
-            dp = mfma16(vr[c], gf[0][c], dp);
+      for (int y = 0; y < RT; ++y) {
+        f32x16 s, dp;
+        if constexpr (NP == 1) {
+          s = splat16(0.0f);
+          dp = splat16(kSub ? 0.0f : -delta[y]);
+          if constexpr (D < 128) {
+#pragma unroll
+            for (int c = 0; c < KC; ++c) {
+              s = mfma16(kr[c], qf[y][0][c], s);
+              dp = mfma16(vr[c], gf[y][0][c], dp);
+            }
+          } else {                                 // one operand's chunks at a time, for two waves a SIMD
+#pragma unroll
+            for (int c = 0; c < KC; ++c) s = mfma16(kr[c], qf[y][0][c], s);
+            read_rows<D>(at, vtile, vr);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int c = 0; c < KC; ++c) dp = mfma16(vr[c], gf[y][0][c], dp);
           }
-        } else {                                   // one operand's chunks at a time, for two waves a SIMD
-#pragma unroll
-          for (int c = 0; c < KC; ++c) s = mfma16(kr[c], qf[0][c], s);
-          read_rows<D>(at, vtile, vr);
-          __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-          for (int c = 0; c < KC; ++c) dp = mfma16(vr[c], gf[0][c], dp);
-        }
-        read_trans<D>(at, ktile, kt);
-        __builtin_amdgcn_sched_barrier(0);
-      } else {
-        s = product<NP, D>(at, ktile, STEP, qf, splat16(0.0f));
-        dp = values_product(vtile);
-      }
-      float mul = a.scale_log2, add = nl;
-      const int d0 = k0 - pos0, at_win = d0 + a.far + kWinPad - (lane & 31) + 4 * hf;
-      BiasKind kind = kBiasNear;
-      if constexpr (BIAS) {
-        kind = bias_kind(d0, a.far);
-        if (kind == kBiasNear) {
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.scale_log2, win[at_win + reg_row(r)]);
-          mul = 1.0f;
+          if (y == RT - 1) read_trans<D>(at, ktile, kt);
+          if (RT == 1) __builtin_amdgcn_sched_barrier(0);
         } else {
-          add = nl + (kind == kBiasLow ? lo : hi);
+          s = product<NP, D>(at, ktile, STEP, qf[0], splat16(0.0f));
+          dp = values_product(vtile);
         }
-      }
-      if (!PLAIN && (kb != ~0u || (a.causal && k0 + 31 > pos0)))
-        select_rows(s, a.causal ? kb & low_bits(pos0 + (lane & 31) - k0 + 1) : kb, -INFINITY);
-      float ds[16];
+        const int d0 = k0 - pos0 - 32 * y, at_win = d0 + a.far + kWinPad - (lane & 31) + 4 * hf;
+        float mul = a.scale_log2, add = nl[y];
+        BiasKind kind = kBiasNear;
+        if constexpr (BIAS) {
+          kind = bias_kind(d0, a.far);
+          if (kind == kBiasNear) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r)
-        ds[r] = __builtin_amdgcn_exp2f(fmaf(s[r], mul, add)) * (kDqTwo<NP, D> ? dp[r] - delta : dp[r]);
-      if constexpr (BIAS) {
-        if (kind == kBiasNear) {
-          // row query, column key - query + 31: the diagonals are columns, a lane each
-          float* to = skew + 63 * (lane & 31) + 31 + 4 * hf;
-#pragma unroll
-          for (int r = 0; r < 16; ++r) to[reg_row(r)] = ds[r];
-          wave_lds_sync();
-          float t[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-          for (int q = 0; q < 32; ++q) t[q & 3] += skew[64 * q + lane];
-          mine[d0 + a.far + kWinPad - 31 + lane] += (t[0] + t[1]) + (t[2] + t[3]);
-          wave_lds_sync();
-        } else {
-          float t = 0.0f;
-#pragma unroll
-          for (int r = 0; r < 16; ++r) t += ds[r];
-          if (kind == kBiasLow) sum_lo += t;
-          else sum_hi += t;
+            for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.scale_log2, win[at_win + reg_row(r)]);
+            mul = 1.0f;
+          } else {
+            add += kind == kBiasLow ? lo : hi;
+          }
         }
+        if (!PLAIN && (kb != ~0u || (a.causal && d0 + 31 > 0)))
+          select_rows(s, a.causal ? kb & low_bits((lane & 31) - d0 + 1) : kb, -INFINITY);
+        float ds[16];
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          ds[r] = __builtin_amdgcn_exp2f(fmaf(s[r], mul, add)) * (NP == 1 && kSub ? dp[r] - delta[y] : dp[r]);
+        if constexpr (BIAS) {
+          if (kind == kBiasNear) {
+            // row query, column key - query + 31: the diagonals are columns, a lane each
+            float* to = skew + 63 * (lane & 31) + 31 + 4 * hf;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) to[reg_row(r)] = ds[r];
+            wave_lds_sync();
+            float t[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int q = 0; q < 32; ++q) t[q & 3] += skew[64 * q + lane];
+            mine[d0 + a.far + kWinPad - 31 + lane] += (t[0] + t[1]) + (t[2] + t[3]);
+            wave_lds_sync();
+          } else {
+            float t = 0.0f;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) t += ds[r];
+            if (kind == kBiasLow) sum_lo += t;
+            else sum_hi += t;
+          }
+        }
+        dw[y] = pack_weights<NP>(ds);
       }
-      const Packed<NP> dw = pack_weights<NP>(ds);
-      if constexpr (NP == 1) accumulate_chunks<D>(kt, dw, dq);
-      else accumulate_t<NP, D>(at, ktile, STEP, dw, dq);
+#pragma unroll
+      for (int y = 0; y < RT; ++y) {
+        if constexpr (NP == 1) accumulate_chunks<D>(kt, dw[y], dq[y]);
+        else accumulate_t<NP, D>(at, ktile, STEP, dw[y], dq[y]);
+      }
     }
     if (more) {
       char* nxt = smem + (1 - BUF) * 2 * St::kBytes;
@@ -248,7 +262,7 @@ __global__ __launch_bounds__(kExactThreads, (kDqTwo<NP, D> ? 2 : 1)) void exact_
   // the stages whose keys all count for all of the block's queries, in pairs, then the others
   int st = begin;
   if constexpr (!BIAS && NP == 1) {
-    const int all = a.causal ? min(limit, start + qb * kDqRows + 1) : limit;
+    const int all = a.causal ? min(limit, start + qb * ROWS + 1) : limit;
     const int plain = a.key_mask != nullptr ? begin : min(max(all, 0) / KT, stages);
     for (; st + 1 < plain; st += 2) {
       stage(st, b0, std::true_type{});
@@ -259,10 +273,15 @@ __global__ __launch_bounds__(kExactThreads, (kDqTwo<NP, D> ? 2 : 1)) void exact_
     stage(st, b0, std::false_type{});
     if (st + 1 < stages) stage(st + 1, b1, std::false_type{});
   }
-  if (parts > 1)
-    store_rows<3, D>(dq, a.scale, reinterpret_cast<char*>(g.part_q + ((long long)part * a.B * a.H * a.nq + at_row) * D), i < a.nq);
-  else
-    store_rows<NP, D>(dq, a.scale, g.dq.p + b * g.dq.sb + h * g.dq.sh + ic * g.dq.sn, i < a.nq);
+#pragma unroll
+  for (int y = 0; y < RT; ++y) {
+    const int i = i0 + 32 * y, ic = min(i, a.nq - 1);
+    if (parts > 1)
+      store_rows<3, D>(dq[y], a.scale,
+                       reinterpret_cast<char*>(g.part_q + (((long long)part * a.B * a.H + bh) * a.nq + ic) * D), i < a.nq);
+    else
+      store_rows<NP, D>(dq[y], a.scale, g.dq.p + b * g.dq.sb + h * g.dq.sh + ic * g.dq.sn, i < a.nq);
+  }
   if constexpr (BIAS) {
     if (g.diag == nullptr) return;
     sum_lo = wave_sum(sum_lo);
@@ -546,24 +565,31 @@ __global__ __launch_bounds__(kBiasThreads) void exact_bias_kernel(ExactArgs a, c
 }
 
 // Several workgroups share the stages of each block where the blocks would leave half of
-// the chip idle, each with at least eight stages; their sums are float32 rows in the workspace and cost
-// a launch. 8 query heads on 2 key heads x 4 x 1503 x 128 float32: dK and dV 968 us in
-// 96 workgroups, 570 + 18 in 576. Where the blocks fill more, the sums cost what the
-// parts give (dQ of 96 heads x 333 x 64 on 1501 keys, 288 blocks: 46 us, 39 + 7 in 4 parts).
+// the chip idle; each takes at least eight stages, and more parts have to save a fifth of the
+// rounds. Their sums are float32 rows in the workspace and cost a launch. 8 query heads on 2
+// key heads x 4 x 1503 x 128 float32: dK and dV 968 us in 96 workgroups, 465 + 18 in 480. Where
+// the blocks fill more, the sums cost what the parts give (dQ there, 384 blocks: 338 us, 343 + 10
+// in two parts; dQ of 96 heads x 333 x 64 on 1501 keys, 288 blocks of 512 that fit: 46 us, 39 + 7
+// in four).
 static int parts_of(long long blocks, long long stages, int per_cu) {
   const long long room = (long long)per_cu * kCus;
-  if (2 * blocks > room || blocks == 0) return 1;
-  return (int)max(1ll, min(min(2 * room / blocks, stages / 8), 8ll));
+  if (blocks == 0 || 2 * blocks > room) return 1;
+  const int most = (int)max(1ll, min(stages / 8, 8ll));
+  auto rounds = [&](int p) { return (double)((blocks * p + room - 1) / room) / p; };
+  int best = 1;
+  for (int p = 2; p <= most; ++p)
+    if (rounds(p) <= 0.8 * rounds(best)) best = p;
+  return best;
 }
 
 BackwardPlan exact_backward_plan(const mra_exact_problem_t& p) {
   BackwardPlan b{};
-  const int per_cu = p.d == 128 || (p.dtype == MRA_F32 && p.d == 64) ? 1 : 2;
-  const int rows = p.dtype == MRA_BF16 || p.d == 32 ? 64 : 32;
+  const bool f32 = p.dtype == MRA_F32;
+  const int rows = !f32 || p.d == 32 ? 64 : 32;
   const long long kheads = (long long)p.B * p.H_kv, heads = (long long)p.B * p.H;
   const long long qstages = (p.n_q + rows - 1) / rows, kstages = (p.n_k + rows - 1) / rows;
-  b.dq_parts = parts_of(heads * exact_dq_blocks(p.n_q), kstages, per_cu);
-  b.dkv_parts = parts_of(kheads * exact_dq_blocks(p.n_k), qstages * (p.H / p.H_kv), per_cu);
+  b.dq_parts = parts_of(heads * exact_dq_blocks(p.n_q), kstages, f32 && p.d == 128 ? 1 : 2);
+  b.dkv_parts = parts_of(kheads * exact_dq_blocks(p.n_k), qstages * (p.H / p.H_kv), p.d == 128 ? 1 : 2);
   if (b.dq_parts > 1) b.q_floats = (size_t)b.dq_parts * heads * p.n_q * p.d;
   if (b.dkv_parts > 1) b.k_floats = (size_t)b.dkv_parts * kheads * p.n_k * p.d;
   return b;
@@ -579,10 +605,20 @@ static hipError_t backward_case(const ExactArgs& a, const ExactGrads& g, const B
   hipError_t e;
   if (a.nq > 0) {
     const size_t smem = dq_stage + ((1 + kExactWaves) * entries + (BIAS ? kExactWaves * kSkew : 0)) * sizeof(float);
-    auto kernel = exact_dq_kernel<NP, D, BIAS>;
-    if ((e = allow_lds(kernel, smem)) != hipSuccess) return e;
-    kernel<<<dim3((unsigned)(heads * qblocks), plan.dq_parts), kExactThreads, smem, stream>>>(a, g, qblocks);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+    auto launch = [&](auto kernel, int blocks) {
+      const hipError_t lds = allow_lds(kernel, smem);
+      if (lds != hipSuccess) return lds;
+      kernel<<<dim3((unsigned)(heads * blocks), plan.dq_parts), kExactThreads, smem, stream>>>(a, g, blocks);
+      return hipGetLastError();
+    };
+    if constexpr (NP == 1 && D <= 64 && !BIAS) {
+      // (training, 96 heads x 4096 x 64: 1.85 -> 1.82 ms)
+      e = wide_rows(heads, a.nq) ? launch(exact_dq_kernel<NP, D, 2, BIAS>, (a.nq + 2 * kDqRows - 1) / (2 * kDqRows))
+                                 : launch(exact_dq_kernel<NP, D, 1, BIAS>, qblocks);
+    } else {
+      e = launch(exact_dq_kernel<NP, D, 1, BIAS>, qblocks);
+    }
+    if (e != hipSuccess) return e;
   }
   if (a.nk > 0) {
     const size_t smem = stage + 64 * kStageRows<NP, D> + entries * sizeof(float);

@@ -536,11 +536,8 @@ static hipError_t forward_case(const ExactArgs& a, float* lse, const SplitPlan& 
     return hipGetLastError();
   }
   if constexpr (NP == 1 && D <= 64) {
-    // 64 queries per wave read K and V from LDS half as often (96 heads x 4096 x 64: 475 ->
-    // 428 us) but need the rows to fill their larger blocks, and blocks to fill the chip more than
-    // once (384 heads x 512 x 64, 768 of them: 36 -> 38 us)
-    const long long heads = (long long)a.B * a.H, wide = (a.nq + 255) / 256, narrow = (a.nq + 127) / 128;
-    if (heads * wide >= 4 * kCus && 20 * wide <= 11 * narrow) return launch_rows<NP, D, 2, BIAS>(a, lse, stream);
+    // 96 heads x 4096 x 64: 475 -> 428 us
+    if (wide_rows((long long)a.B * a.H, a.nq)) return launch_rows<NP, D, 2, BIAS>(a, lse, stream);
   }
   return launch_rows<NP, D, 1, BIAS>(a, lse, stream);
 }

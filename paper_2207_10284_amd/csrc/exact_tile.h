@@ -460,6 +460,14 @@ __device__ __forceinline__ void store_rows(const f32x16 (&o)[D / 32], float f, c
   }
 }
 
+// Whether a wave takes 64 queries: it then reads K and V from LDS half as often, but needs
+// the rows to fill the larger blocks, and blocks to fill the chip more than once
+// (forward of 384 heads x 512 x 64, 768 of them: 36 -> 38 us).
+inline bool wide_rows(long long heads, int nq) {
+  const long long wide = ((long long)nq + 255) / 256, narrow = ((long long)nq + 127) / 128;
+  return heads * wide >= 4 * kCus && 20 * wide <= 11 * narrow;
+}
+
 // More than 64 KB of dynamic LDS has to be allowed for.
 template <class Kernel>
 inline hipError_t allow_lds(Kernel kernel, size_t smem) {

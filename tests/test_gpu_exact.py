@@ -151,6 +151,7 @@ CASES = [
     ("bf16", 2, 2, 1, 1500, 1300, 64, "bhnd", dict(causal=True, mask="k")),
     ("bf16", 1, 2, 1, 1100, 1200, 128, "bhnd", dict(buckets=(32, 128, True), causal=True, start=True)),
     ("bf16", 16, 64, 64, 256, 96, 32, "bnhd", dict(causal=True, mask="l")),          # 64 rows a wave
+    ("bf16", 8, 64, 64, 512, 300, 64, "bhnd", {}),
     ("bf16", 16, 64, 32, 250, 70, 64, "bhnd", dict(buckets=(8, 20, True), mask="ke")),
     ("bf16", 2, 2, 2, 5, 0, 64, "bhnd", {}),
     ("f32", 2, 2, 1, 0, 40, 32, "bhnd", dict(buckets=(8, 20, True))),
