@@ -565,15 +565,16 @@ __global__ __launch_bounds__(kBiasThreads) void exact_bias_kernel(ExactArgs a, c
 }
 
 // Several workgroups share the stages of each block where the blocks would leave half of
-// the chip idle; each takes at least eight stages, and more parts have to save a fifth of the
-// rounds. Their sums are float32 rows in the workspace and cost a launch. 8 query heads on 2
-// key heads x 4 x 1503 x 128 float32: dK and dV 968 us in 96 workgroups, 465 + 18 in 480. Where
-// the blocks fill more, the sums cost what the parts give (dQ there, 384 blocks: 338 us, 343 + 10
-// in two parts; dQ of 96 heads x 333 x 64 on 1501 keys, 288 blocks of 512 that fit: 46 us, 39 + 7
-// in four).
+// the chip idle, or, in passes that hold one workgroup per CU, part of their last round; each takes
+// at least eight stages, and more parts have to save a fifth of the rounds. Their sums are
+// float32 rows in the workspace and cost a launch. 8 query heads on 2 key heads x 4 x 1503 x
+// 128 float32: dK and dV 968 us in 96 workgroups, 465 + 18 in 480; dQ in 768 instead of 384:
+// the training step 1047 -> 1021 us. Where two workgroups fit a CU and fill more than half, the sums
+// cost what the parts give (dQ of 96 heads x 333 x 64 on 1501 keys, 288 blocks: 46 us, 39 + 7 in
+// four parts).
 static int parts_of(long long blocks, long long stages, int per_cu) {
   const long long room = (long long)per_cu * kCus;
-  if (blocks == 0 || 2 * blocks > room) return 1;
+  if (blocks == 0 || 2 * blocks > (per_cu == 1 ? 8 : 1) * room) return 1;
   const int most = (int)max(1ll, min(stages / 8, 8ll));
   auto rounds = [&](int p) { return (double)((blocks * p + room - 1) / room) / p; };
   int best = 1;
