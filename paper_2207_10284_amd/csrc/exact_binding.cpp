@@ -12,6 +12,7 @@
 #include <torch/csrc/autograd/custom_function.h>
 
 #include <cmath>
+#include <limits>
 
 #include "binding_common.h"
 #include "mra_exact.h"
@@ -53,6 +54,15 @@ void check_rows(const at::Tensor& t, const at::Tensor& ref, at::IntArrayRef shap
   TORCH_CHECK_VALUE(dense_rows(t), name, " must have dense rows, 16-byte aligned");
 }
 
+// A result tensor of the caller's: like ref, and no two of its rows the same memory.
+void check_out(const at::Tensor& t, const at::Tensor& ref, const char* name) {
+  check_rows(t, ref, ref.sizes(), name);
+  const mra_strided_t v = view(t);
+  TORCH_CHECK_VALUE(t.numel() == 0 || ((t.size(0) == 1 || v.stride_b) && (t.size(1) == 1 || v.stride_h) &&
+                                       (t.size(2) == 1 || v.stride_n)),
+                    name, " must not be broadcast");
+}
+
 at::Tensor rows_like(const at::Tensor& t) {
   at::Tensor o = at::empty_like(t);
   return dense_rows(o) ? o : at::empty(t.sizes(), t.options());
@@ -78,6 +88,8 @@ mra_exact_problem_t problem(const at::Tensor& q, const at::Tensor& k, const at::
   const int64_t B = q.size(0), H = q.size(1), nq = q.size(2), d = q.size(3), Hkv = k.size(1), nk = k.size(2);
   TORCH_CHECK_VALUE(k.sizes() == at::IntArrayRef({B, Hkv, nk, d}) && v.sizes() == k.sizes() && (Hkv ? H % Hkv : H) == 0,
                     "k, v must share shape [B, H_kv, n_k, d] with q's B and d, H a multiple of H_kv");
+  for (const int64_t n : {B, H, nq, d, Hkv, nk})
+    TORCH_CHECK_VALUE(n <= std::numeric_limits<int>::max(), "sizes must be below 2^31");
   check_rows(q, q, q.sizes(), "q");
   check_rows(k, q, k.sizes(), "k");
   check_rows(v, q, v.sizes(), "v");
@@ -129,6 +141,8 @@ void call_forward(const mra_exact_problem_t& p, const at::Tensor& q, const at::T
   const c10::DeviceGuard guard(q.device());
   at::Tensor ws;
   if (given(workspace)) {
+    TORCH_CHECK_VALUE(workspace->device() == q.device() && workspace->is_contiguous(),
+                      "workspace must be a contiguous tensor", on(q.device()));
     ws = *workspace;
   } else if (const size_t need = api.forward_ws(&p)) {
     ws = at::empty({(int64_t)need}, q.options().dtype(at::kByte));
@@ -144,7 +158,7 @@ at::Tensor forward(const at::Tensor& q, const at::Tensor& k, const at::Tensor& v
                    const Opt& buckets, const Opt& out, const Opt& lse_out, const Opt& workspace) {
   const mra_exact_problem_t p = problem(q, k, v, scale_or(scale, q), causal,
                                         {given(lengths), given(key_mask), given(q_start), given(bias), given(buckets)});
-  if (out) check_rows(*out, q, q.sizes(), "out");
+  if (out) check_out(*out, q, "out");
   const at::Tensor z = out ? *out : rows_like(q);
   float* lse = nullptr;
   if (lse_out) {
@@ -188,7 +202,8 @@ struct Exact : torch::autograd::Function<Exact> {
     check_rows(dout, q, q.sizes(), "dout");
     const c10::DeviceGuard guard(q.device());
     const at::Tensor dq = rows_like(q), dk = rows_like(k), dv = rows_like(v);
-    const at::Tensor db = opt(5) ? at::empty_like(t[5]) : at::Tensor();
+    // q, k, v, bias are edges 0 to 3
+    const at::Tensor db = opt(5) && ctx->needs_input_grad(3) ? at::empty_like(t[5]) : at::Tensor();
     const size_t need = api.backward_ws(&p);
     at::Tensor ws;
     if (need) ws = at::empty({(int64_t)need}, q.options().dtype(at::kByte));

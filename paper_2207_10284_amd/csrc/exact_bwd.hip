@@ -221,7 +221,7 @@ __global__ __launch_bounds__(kExactThreads, (kDqTwo<NP, D> || RT == 2 ? 2 : 1)) 
 #pragma unroll
         for (int r = 0; r < 16; ++r)
           ds[r] = __builtin_amdgcn_exp2f(fmaf(s[r], mul, add)) * (NP == 1 && kSub ? dp[r] - delta[y] : dp[r]);
-        if constexpr (BIAS) {
+        if (BIAS && g.diag != nullptr) {
           if (kind == kBiasNear) {
             // row query, column key - query + 31: the diagonals are columns, a lane each
             float* to = skew + 63 * (lane & 31) + 31 + 4 * hf;

@@ -48,7 +48,7 @@ struct ExactGrads {
   Rows dout, dq, dk, dv;
   const float* lse;
   float* delta;                           // [B, H, n_q]: G . Z per query
-  float* diag;                            // [H, B, blocks, parts, window]: sums of dS over diagonals (bias gradient only)
+  float* diag;                            // [H, B, blocks, parts, window]: sums of dS over diagonals; null: not asked for
   void* dbias;
   float *part_q, *part_k, *part_v;        // [parts, B, heads, n, d]: see BackwardPlan
 };

@@ -34,20 +34,15 @@ constexpr int kTileBytes = 64 * D;                 // 32 rows of one plane
 template <int NP, int D>
 constexpr int kStageRows = NP == 1 || D == 32 ? 64 : 32;
 
-// Which of a stage's R rows count: row r is bit r % 64 of word r / 64.
+// Which of a stage's R rows count: row r is bit r.
 template <int R>
 struct RowBits {
-  static constexpr int W = (R + 63) / 64;
-  static constexpr uint64_t kAll = R >= 64 ? ~uint64_t(0) : (uint64_t(1) << (R & 63)) - 1;
-  uint64_t w[W];
-  __device__ __forceinline__ uint32_t tile(int i) const { return (uint32_t)(w[i / 2] >> (32 * (i & 1))); }
-  __device__ __forceinline__ bool all() const {
-    bool y = true;
-#pragma unroll
-    for (int i = 0; i < W; ++i) y = y && w[i] == kAll;
-    return y;
-  }
-  __device__ __forceinline__ bool row(int r) const { return ((W == 2 && r >= 64 ? w[W - 1] : w[0]) >> (r & 63)) & 1; }
+  static_assert(R == 32 || R == 64, "one ballot");
+  static constexpr uint64_t kAll = R == 64 ? ~uint64_t(0) : (uint64_t(1) << 32) - 1;
+  uint64_t w;
+  __device__ __forceinline__ uint32_t tile(int i) const { return (uint32_t)(w >> (32 * i)); }
+  __device__ __forceinline__ bool all() const { return w == kAll; }
+  __device__ __forceinline__ bool row(int r) const { return (w >> r) & 1; }
 };
 
 // R rows of D elements moved by T threads from global memory to LDS tiles: plane
@@ -237,6 +232,7 @@ template <int NP>
 struct Packed {
   u32x4 w[NP][2];
 };
+
 // All row-layout chunks of a one-plane tile.
 template <int D, class At>
 __device__ __forceinline__ void read_rows(const At& at, int tile, u32x4 (&f)[D / 16]) {
@@ -346,40 +342,26 @@ __device__ __forceinline__ int first_position(const ExactArgs& a, int b) {
   return a.q_start == nullptr ? a.nk - a.nq : min(max(a.q_start[b], -kFar), kFar);
 }
 
-// This lane's bytes of the mask of the R keys from k0 on (nonzero: counts), 64 lanes
-// a word; a lane past the keys repeats the last.
+// This lane's byte of the mask of the R keys from k0 on (nonzero: counts); a lane past
+// the keys repeats the last.
 template <int R>
 struct MaskBytes {
-  uint32_t b[RowBits<R>::W];
+  uint32_t b;
   __device__ __forceinline__ void load(const ExactArgs& a, int batch, int k0) {
-#pragma unroll
-    for (int i = 0; i < RowBits<R>::W; ++i)
-      b[i] = a.key_mask == nullptr
-                 ? 1
-                 : a.key_mask[(long long)batch * a.mask_stride + min(k0 + 64 * i + lane_id(), a.nk - 1)];
+    b = a.key_mask == nullptr ? 1 : a.key_mask[(long long)batch * a.mask_stride + min(k0 + lane_id(), a.nk - 1)];
   }
   // the keys k0 .. k0 + R - 1 that count
   __device__ __forceinline__ RowBits<R> bits(int k0, int limit) const {
-    RowBits<R> ok;
-#pragma unroll
-    for (int i = 0; i < RowBits<R>::W; ++i) {
-      const int r = 64 * i + lane_id();
-      ok.w[i] = __ballot(r < R && k0 + r < limit && b[i] != 0);
-    }
-    return ok;
+    const int r = lane_id();
+    return {__ballot(r < R && k0 + r < limit && b != 0)};
   }
 };
 
 // The rows row0 .. row0 + R - 1 below limit.
 template <int R>
 __device__ __forceinline__ RowBits<R> row_bits(int row0, int limit) {
-  RowBits<R> ok;
-#pragma unroll
-  for (int i = 0; i < RowBits<R>::W; ++i) {
-    const int r = 64 * i + lane_id();
-    ok.w[i] = __ballot(r < R && row0 + r < limit);
-  }
-  return ok;
+  const int r = lane_id();
+  return {__ballot(r < R && row0 + r < limit)};
 }
 
 __device__ __forceinline__ float bias_value(const ExactArgs& a, int h, int entry) {

@@ -632,6 +632,12 @@ def _check_rows(t, ref, shape, name):
         raise ValueError(f"{name} must have dense rows, 16-byte aligned")
 
 
+def _check_out(t, ref, name):
+    _check_rows(t, ref, ref.shape, name)
+    if t.numel() and any(n > 1 and not st for n, st in zip(t.shape, _strides(t))):
+        raise ValueError(f"{name} must not be broadcast")
+
+
 def _view(t):
     return _Strided(t.data_ptr(), *_strides(t))
 
@@ -660,6 +666,8 @@ def _exact_problem(q, k, v, scale, causal, lengths, key_mask, q_start, bias, buc
     Hkv, nk = k.shape[1], k.shape[2]
     if k.shape != (B, Hkv, nk, d) or v.shape != k.shape or (H % Hkv if Hkv else H):
         raise ValueError("k, v must share shape [B, H_kv, n_k, d] with q's B and d, H a multiple of H_kv")
+    if max(*q.shape, Hkv, nk) >= 1 << 31:
+        raise ValueError("sizes must be below 2^31")
     for t, name in ((q, "q"), (k, "k"), (v, "v")):
         _check_rows(t, q, t.shape, name)
     dev = q.device
@@ -712,8 +720,9 @@ def exact_attention_forward(q, k, v, *, scale=None, causal: bool = False, length
     given. What lies at other keys may be anything; a query for which no key
     counts gives zeros. ``bias`` ([buckets, H], float32 or q's dtype) adds
     bias[buckets[distance], h] for the distance j - position (``buckets``: see
-    ``distance_buckets``); -inf takes its distances out. ``lse_out`` (float32 [B, H, n_q]) receives the log
-    normalisers. A call whose ``workspace`` (uint8) a graph captured must not run
+    ``distance_buckets``); -inf takes its distances out. ``lse_out`` (float32
+    [B, H, n_q]) receives the log normalisers; it and ``out`` overlap no other
+    argument. A call whose ``workspace`` (uint8) a graph captured must not run
     beside another with the same one."""
     return bind_exact().forward(q, k, v, scale, causal, lengths, key_mask, q_start, bias, buckets, _result(q, out),
                                 lse_out, workspace)
@@ -737,7 +746,7 @@ def exact_attention_backward(q, k, v, out, dout, lse, *, scale=None, causal: boo
         if g is None:
             g = _rows_like(t)
         else:
-            _check_rows(g, t, t.shape, name)
+            _check_out(g, t, name)
         grads.append(g)
     if bias is None and dbias is not None:
         raise ValueError("dbias without a bias")
@@ -747,6 +756,8 @@ def exact_attention_backward(q, k, v, out, dout, lse, *, scale=None, causal: boo
         elif dbias.shape != bias.shape or dbias.dtype != bias.dtype or dbias.device != bias.device \
                 or not dbias.is_contiguous():
             raise ValueError("dbias must be like bias")
+    if workspace is not None and (workspace.device != q.device or not workspace.is_contiguous()):
+        raise ValueError(f"workspace must be a contiguous tensor on {q.device}")
     with torch.cuda.device(q.device):
         if workspace is None:
             workspace = torch.empty(max(int(load_exact().mra_exact_backward_workspace_bytes(ctypes.byref(p))), 1),
@@ -784,8 +795,10 @@ class ExactAttention(torch.autograd.Function):
 def exact_attention(q, k, v, *, scale=None, causal: bool = False, lengths=None, key_mask=None, q_start=None,
                     bias=None, buckets=None):
     """Differentiable exact softmax attention (arguments and result as
-    ``exact_attention_forward``), with gradients of q, k, v and bias; native where
-    ``mra_attention`` is."""
+    ``exact_attention_forward``), with gradients of q, k, v and bias, which are not
+    differentiable themselves; native where ``mra_attention`` is. A backward pass
+    that a graph captures needs leaves of which no eager graph is alive (torch
+    otherwise ties the capture to the eager graph's stream)."""
     tensors = (q, k, v, lengths, key_mask, q_start, bias, buckets)
     if (all(t is None or type(t) in _PLAIN for t in tensors)
             and not torch._C._are_functorch_transforms_active() and torch._C._get_tracing_state() is None

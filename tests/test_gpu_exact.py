@@ -534,3 +534,40 @@ def test_tokens_after_a_prompt(gpu, dt, d, Hkv):
         z = gpu.exact_attention_forward(token, *cache, lengths=length, q_start=length - 1, **o)
         ref, t = whole[0].transpose(1, 2)[rows, at], tol.transpose(1, 2)[rows, at]
         assert bool(((z[:, :, 0].double() - ref).abs() <= t).all())
+
+
+def test_results_and_workspaces_refused(gpu):
+    """Results whose rows share memory, workspaces elsewhere, sizes past 32 bits."""
+    q, k, v, g, o = pieces(gpu)
+    z, lse, _ = run(gpu, q, k, v, g, o)
+    flat = torch.zeros(1, 1, 1, q.shape[3], device="cuda", dtype=q.dtype)
+    with pytest.raises(ValueError, match="out must not be broadcast"):
+        gpu.exact_attention_forward(q, k, v, out=flat.expand(q.shape), **o)
+    for name, t in (("dq", q), ("dk", k), ("dv", v)):
+        with pytest.raises(ValueError, match=f"{name} must not be broadcast"):
+            gpu.exact_attention_backward(q, k, v, z, g, lse, **o, **{name: flat.expand(t.shape)})
+    size = gpu.exact_backward_workspace_bytes(q, k, v, **o)
+    for ws in (torch.empty(size, dtype=torch.uint8), torch.empty(size, 2, dtype=torch.uint8, device="cuda")[:, 0]):
+        with pytest.raises(ValueError, match="workspace"):
+            gpu.exact_attention_forward(q, k, v, workspace=ws, **o)
+        with pytest.raises(ValueError, match="workspace"):
+            gpu.exact_attention_backward(q, k, v, z, g, lse, workspace=ws, **o)
+    long = torch.zeros(q.shape[0], 1, 1, q.shape[3], device="cuda", dtype=q.dtype).expand(-1, -1, (1 << 32) + 32, -1)
+    with pytest.raises(ValueError, match="2\\^31"):
+        gpu.exact_attention_forward(q, long, long)
+    with pytest.raises(ValueError, match="2\\^31"):
+        gpu.exact_attention_backward(q, long, long, z, g, lse)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_bias_held_fixed(gpu, dt):
+    """A bias that takes no gradient: the others' gradients have the same bits, near
+    and far tiles, one part and several."""
+    print("fixed bias", dt, flush=True)
+    for nq, nk in ((100, 150), (40, 1300)):
+        q, k, v, g, o = pieces(gpu, dt, nq=nq, nk=nk, mask="lk", buckets=(8, 20, True))
+        z, lse, grads = run(gpu, q, k, v, g, o)
+        leaves = [t.clone().requires_grad_(True) for t in (q, k, v)]
+        out = gpu.exact_attention(*leaves, **o)
+        same((out, *torch.autograd.grad(out, leaves, g)), (z, *grads[:3]))
+        assert o["bias"].grad is None and not o["bias"].requires_grad
