@@ -375,3 +375,38 @@ def test_lds_fits():
         assert stage + 5 * win + 4 * 32 * 64 * 4 <= 160 * 1024      # dQ: the bias, four windows of sums and skewed tiles
         assert stage + 64 * rows + win <= 160 * 1024                # dK, dV
         assert max(4 * planes * 32 * d * 2, 3 * 32 * d * 4) + 2048 <= 160 * 1024
+
+
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("causal", [False, True])
+def test_walk_of_dk_dv(bias, causal):
+    """The walk of dK and dV from the last query down, as exact_dkv_kernel makes it: every
+    stage of every head once over the parts, none before the first query that reaches a key,
+    and the stages taken as plain have only queries that reach every key of the block."""
+    QT, rows = 64, 128
+    for group, nq, nk, start, block0, parts in ((1, 1, 1, 0, 0, 1), (3, 300, 200, -100, 128, 1), (4, 1000, 1000, 0, 384, 4),
+                                                (2, 700, 1500, 800, 1408, 3), (8, 65, 500, 900, 256, 8), (2, 0, 90, 0, 0, 2),
+                                                (4, 130, 130, -500, 0, 2), (1, 640, 640, 0, 512, 6)):
+        first = min(max(block0 - start, 0), nq) // QT * QT if causal else 0
+        stages = (nq - first + QT - 1) // QT if block0 < nk else 0
+        border = min(max(block0 + rows - 1 - start - first + QT - 1, 0) // QT, stages) if causal else 0
+        inner = 1 if bias else group
+        turn, total, seen = inner * stages, group * stages, []
+        for part in range(parts):
+            t0, t1 = total * part // parts, total * (part + 1) // parts
+            hg = group if stages == 0 else t0 // turn * inner
+            while hg < group and hg * stages < t1:
+                begin, end = max(t0 - hg * stages, 0), min(t1 - hg * stages, turn)
+                plain = begin + (max(min((stages - border) * inner, end) - begin, 0) & ~1)
+                q, hn = first + (stages - 1 - begin // inner) * QT, begin % inner
+                for st in range(begin, end):
+                    seen.append((hg + hn, q))
+                    if st < plain:
+                        assert not causal or start + q >= block0 + rows - 1
+                    if st + 1 < end:
+                        hn += 1
+                        if hn == inner:
+                            hn, q = 0, q - QT
+                hg += inner
+        want = [(h, q) for h in range(group) for q in range(first, nq, QT)] if block0 < nk else []
+        assert sorted(seen) == want
