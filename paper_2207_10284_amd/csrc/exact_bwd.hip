@@ -78,6 +78,8 @@ __global__ __launch_bounds__(kExactThreads, (kDqTwo<NP, D> || RT == 2 ? 2 : 1)) 
     const int half = hf * (D / 2) * (NP == 1 ? 2 : 4);
     const u32x4* gr = reinterpret_cast<const u32x4*>(g.dout.p + b * g.dout.sb + h * g.dout.sh + ic * g.dout.sn + half);
     const u32x4* zr = reinterpret_cast<const u32x4*>(a.out.p + b * a.out.sb + h * a.out.sh + ic * a.out.sn + half);
+    // of Z as stored: the rounding of a bfloat16 Z is one number for all keys of the query
+    // (a float32 Z kept for this pass would cost twice its bytes)
     float d = 0.0f;
 #pragma unroll
     for (int c = 0; c < LB; ++c) {
