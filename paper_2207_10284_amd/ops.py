@@ -797,8 +797,8 @@ def exact_attention(q, k, v, *, scale=None, causal: bool = False, lengths=None, 
     """Differentiable exact softmax attention (arguments and result as
     ``exact_attention_forward``), with gradients of q, k, v and bias, which are not
     differentiable themselves; native where ``mra_attention`` is. A backward pass
-    that a graph captures needs leaves of which no eager graph is alive (torch
-    otherwise ties the capture to the eager graph's stream)."""
+    that a graph captures needs leaves of which no eager graph is alive (with
+    one, torch's engine can end the process)."""
     tensors = (q, k, v, lengths, key_mask, q_start, bias, buckets)
     if (all(t is None or type(t) in _PLAIN for t in tensors)
             and not torch._C._are_functorch_transforms_active() and torch._C._get_tracing_state() is None

@@ -571,3 +571,37 @@ def test_bias_held_fixed(gpu, dt):
         out = gpu.exact_attention(*leaves, **o)
         same((out, *torch.autograd.grad(out, leaves, g)), (z, *grads[:3]))
         assert o["bias"].grad is None and not o["bias"].requires_grad
+
+
+@pytest.mark.parametrize("dt,d", [("bf16", 64), ("f32", 128)])
+def test_autograd_in_a_graph(gpu, dt, d):
+    """exact_attention and its backward captured with leaves of their own: every replay
+    has the eager bits of the values then in the leaves."""
+    print("autograd graph", dt, d, flush=True)
+    a = pieces(gpu, dt, nq=200, nk=330, d=d, mask="lk", causal=True, buckets=(8, 20, True))
+    b = pieces(gpu, dt, seed=9, nq=200, nk=330, d=d)
+    o = dict(a[4])
+    tables = o.pop("bias"), torch.flip(a[4]["bias"], (0,))
+
+    def eager(t, table):
+        leaves = [x.clone().requires_grad_(True) for x in (*t[:3], table)]
+        out = gpu.exact_attention(*leaves[:3], bias=leaves[3], **o)
+        return [x.detach().clone() for x in (out, *torch.autograd.grad(out, leaves, t[3]))]
+
+    refs = [eager(t, table) for t, table in zip((a, b), tables)]
+    leaves = [x.clone().requires_grad_(True) for x in (*a[:3], tables[0])]
+    g = a[3].clone()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = gpu.exact_attention(*leaves[:3], bias=leaves[3], **o)
+        grads = torch.autograd.grad(out, leaves, g)
+    for n in (0, 1, 0):
+        with torch.no_grad():
+            for x, y in zip((*leaves, g), (*(a, b)[n][:3], tables[n], (a, b)[n][3])):
+                x.copy_(y)
+        graph.replay()
+        torch.cuda.synchronize()
+        same((out.detach(), *grads), refs[n])
+        eager(b, tables[1])
+        torch.cuda.synchronize()
