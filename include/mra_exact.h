@@ -27,8 +27,10 @@
  *   multiple of 16 bytes. Input strides may be 0 (a broadcast axis). Outputs
  *   must not overlap themselves or another argument.
  * - d is 32, 64 or 128; 0 <= n_q, n_k <= 2^26; row strides below 2^25 bytes.
- * - A bias of -infinity (in float32, also one below -2^126) takes its distances
- *   out: such a key does not count. Other entries are finite.
+ * - A bias below -2^14 (-infinity and the usual masks of -1e9, -1e30 or a type's
+ *   lowest value among them) takes its distances out: such a key does not count.
+ *   One above 2^14 is taken as 2^14: its keys outweigh all others, and among
+ *   each other weigh as if such entries were equal. None is NaN.
  * - What lies at a key that does not count for any query of its batch
  *   (j >= lengths[b], key_mask[b][j] == 0) may be anything, also NaN. Results
  *   for other non-finite inputs are unspecified.
@@ -38,7 +40,8 @@
  * - Products accumulate in float32; bfloat16 inputs feed bfloat16 matrix
  *   products with the softmax weights (and, backward, the logit gradients)
  *   rounded to bfloat16 before their products; float32 operands enter as sums
- *   of three bfloat16 values, as in mra.h. Results are rounded once.
+ *   of three bfloat16 values, as in mra.h. Results are rounded once. L is one
+ *   float32, so the probabilities formed from it are off by about |L| 2^-23.
  * - Results of a call do not change from run to run: no sum depends on the
  *   order in which workgroups run.
  */

@@ -364,11 +364,17 @@ __device__ __forceinline__ RowBits<R> row_bits(int row0, int limit) {
   return {__ballot(r < R && row0 + r < limit)};
 }
 
+// A bias as every kernel takes it: below -kBiasRange its distances do not count, above kBiasRange it
+// is kBiasRange. A log normaliser is one float32, so a probability exp(S - L) is off by about
+// |L| 2^-23: at 2^14 by 2^-9, half a bfloat16 rounding. Beyond, the sums of a query whose keys all
+// carry such a bias leave 1 (0.93 to 1.07 at 1e6) and at -1e38 are NaN.
+constexpr float kBiasRange = 16384.0f;
 __device__ __forceinline__ float bias_value(const ExactArgs& a, int h, int entry) {
   const int e = a.map[entry];
   if ((unsigned)e >= (unsigned)a.buckets) return 0.0f;
   const long long at = (long long)e * a.H + h;
-  return a.bias_bf16 ? bf16_to_f32(static_cast<const uint16_t*>(a.bias)[at]) : static_cast<const float*>(a.bias)[at];
+  const float x = a.bias_bf16 ? bf16_to_f32(static_cast<const uint16_t*>(a.bias)[at]) : static_cast<const float*>(a.bias)[at];
+  return x < -kBiasRange ? -INFINITY : (x > kBiasRange ? kBiasRange : x);
 }
 
 // The position bias of a 32 x 32 tile depends on key - position only, 63

@@ -720,8 +720,9 @@ def exact_attention_forward(q, k, v, *, scale=None, causal: bool = False, length
     given. What lies at other keys may be anything; a query for which no key
     counts gives zeros. ``bias`` ([buckets, H], float32 or q's dtype) adds
     bias[buckets[distance], h] for the distance j - position (``buckets``: see
-    ``distance_buckets``); -inf takes its distances out. ``lse_out`` (float32
-    [B, H, n_q]) receives the log normalisers; it and ``out`` overlap no other
+    ``distance_buckets``); an entry below -2^14, -inf and the usual mask values
+    among them, takes its distances out, one above 2^14 is taken as that.
+    ``lse_out`` (float32 [B, H, n_q]) receives the log normalisers; it and ``out`` overlap no other
     argument. A call whose ``workspace`` (uint8) a graph captured must not run
     beside another with the same one."""
     return bind_exact().forward(q, k, v, scale, causal, lengths, key_mask, q_start, bias, buckets, _result(q, out),
