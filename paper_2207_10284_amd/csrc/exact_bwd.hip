@@ -23,6 +23,13 @@ namespace mra {
 constexpr int kDqRows = kExactWaves * 32;
 // floats of a wave's skewed tile (32 rows of 64: see exact_dq_kernel)
 constexpr int kSkew = 32 * 64;
+// D of the tiles beyond the bias window, per wave: a double each below and above it. A lane's float32 sums
+// go there every kFarStages stages: over a query's keys D cancels, and one float32 sum over
+// 10^5 keys would keep roundings of the sums on the way (dbias, 64 queries x 150000 keys x 64 float32: 3.3e-5 ->
+// 2.3e-5 in 2-norm; 2^20 keys whose D rise and fall: 39% -> 5e-6). Doubles in the lanes' registers
+// instead would spill (32 heads x 2048 x 128 bfloat16, training: 391 -> 425 us).
+constexpr int kFarStages = 16;
+constexpr size_t kFarBytes = kExactWaves * 2 * sizeof(double);
 
 int exact_dq_blocks(int nq) { return (nq + kDqRows - 1) / kDqRows; }
 // the window's entries, then the sums of the tiles below and above it
@@ -104,15 +111,27 @@ __global__ __launch_bounds__(kExactThreads, (kDqTwo<NP, D> || RT == 2 ? 2 : 1)) 
     nl[y] = none ? -INFINITY : -L * kLog2e;
     delta[y] = none ? 0.0f : d;
   }
-  float lo = 0.0f, hi = 0.0f, sum_lo = 0.0f, sum_hi = 0.0f;
+  float sum_lo = 0.0f, sum_hi = 0.0f;
   float* mine = acc + w * entries;
   float* skew = acc + kExactWaves * entries + w * kSkew;
+  double* far_sums = reinterpret_cast<double*>(acc + kExactWaves * (entries + kSkew));
   if constexpr (BIAS) {
     fill_window(a, h, win, tid, kExactThreads);
-    for (int x = tid; x < kExactWaves * (entries + kSkew); x += kExactThreads) acc[x] = 0.0f;
-    lo = bias_value(a, h, 0) * kLog2e;
-    hi = bias_value(a, h, 2 * a.far) * kLog2e;
+    for (int x = tid; x < kExactWaves * (entries + kSkew) + (int)(kFarBytes / 4); x += kExactThreads) acc[x] = 0.0f;
   }
+
+  // this wave's sums beyond the window, to their doubles
+  auto flush_far = [&]() {
+    float* both[2] = {&sum_lo, &sum_hi};
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      double t = (double)*both[x];
+#pragma unroll
+      for (int y = 1; y < kWave; y *= 2) t += __shfl_xor(t, y);
+      if (lane == 0) far_sums[2 * w + x] += t;
+      *both[x] = 0.0f;
+    }
+  };
 
   // G V^T - delta. The matrix cores' additions fall a little below the exact sum (5e-8 on
   // average where the sum is about 11), and an offset common to a query's keys does not
@@ -156,6 +175,8 @@ __global__ __launch_bounds__(kExactThreads, (kDqTwo<NP, D> || RT == 2 ? 2 : 1)) 
   __syncthreads();
   wait_loads<0>();                                 // the operands too: no wait for them beside the loads in flight below
   constexpr bool kSub = kDqTwo<NP, D> || RT == 2;  // delta subtracted by the vector ALU: 16 registers fewer
+  // K's columns read when D has been formed, for registers (32 heads x 2048 x 128 with a bias, training: 408 -> 391 us)
+  constexpr bool kLate = kDqTwo<NP, D> && BIAS;
   // stage st in buffer BUF (known at compile time: its part of an LDS address is an
   // offset); PLAIN: every key counts for every query, no bias
   auto stage = [&](int st, auto BUF, auto PLAIN) {
@@ -198,7 +219,7 @@ __global__ __launch_bounds__(kExactThreads, (kDqTwo<NP, D> || RT == 2 ? 2 : 1)) 
 #pragma unroll
             for (int c = 0; c < KC; ++c) dp = mfma16(vr[c], gf[y][0][c], dp);
           }
-          if (y == RT - 1) read_trans<D>(at, ktile, kt);
+          if (y == RT - 1 && !kLate) read_trans<D>(at, ktile, kt);
           if (RT == 1) __builtin_amdgcn_sched_barrier(0);
         } else {
           s = product<NP, D>(at, ktile, STEP, qf[0], splat16(0.0f));
@@ -214,7 +235,7 @@ __global__ __launch_bounds__(kExactThreads, (kDqTwo<NP, D> || RT == 2 ? 2 : 1)) 
             for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.scale_log2, win[at_win + reg_row(r)]);
             mul = 1.0f;
           } else {
-            add += kind == kBiasLow ? lo : hi;
+            add += win[kind == kBiasLow ? 0 : entries - 1];
           }
         }
         if (!PLAIN && (kb != ~0u || (a.causal && d0 + 31 > 0)))
@@ -245,6 +266,7 @@ __global__ __launch_bounds__(kExactThreads, (kDqTwo<NP, D> || RT == 2 ? 2 : 1)) 
         }
         dw[y] = pack_weights<NP>(ds);
       }
+      if constexpr (kLate) read_trans<D>(at, ktile, kt);
 #pragma unroll
       for (int y = 0; y < RT; ++y) {
         if constexpr (NP == 1) accumulate_chunks<D>(kt, dw[y], dq[y]);
@@ -274,6 +296,9 @@ __global__ __launch_bounds__(kExactThreads, (kDqTwo<NP, D> || RT == 2 ? 2 : 1)) 
   for (; st < stages; st += 2) {
     stage(st, b0, std::false_type{});
     if (st + 1 < stages) stage(st + 1, b1, std::false_type{});
+    if constexpr (BIAS) {
+      if ((st - begin) % kFarStages == kFarStages - 2) flush_far();
+    }
   }
 #pragma unroll
   for (int y = 0; y < RT; ++y) {
@@ -286,12 +311,7 @@ __global__ __launch_bounds__(kExactThreads, (kDqTwo<NP, D> || RT == 2 ? 2 : 1)) 
   }
   if constexpr (BIAS) {
     if (g.diag == nullptr) return;
-    sum_lo = wave_sum(sum_lo);
-    sum_hi = wave_sum(sum_hi);
-    if (lane == 0) {
-      win[2 * w] = sum_lo;                         // the bias window is idle
-      win[2 * w + 1] = sum_hi;
-    }
+    flush_far();
     __syncthreads();
     const long long at_part = ((long long)h * a.B + b) * qblocks * parts + (long long)qb * parts + part;
     float* out = g.diag + at_part * (entries + 2);
@@ -301,7 +321,7 @@ __global__ __launch_bounds__(kExactThreads, (kDqTwo<NP, D> || RT == 2 ? 2 : 1)) 
       for (int p = 0; p < kExactWaves; ++p) t += acc[p * entries + x];
       out[x] = t;
     }
-    if (tid < 2) out[entries + tid] = win[tid] + win[2 + tid] + win[4 + tid] + win[6 + tid];
+    if (tid < 2) out[entries + tid] = (float)((far_sums[tid] + far_sums[2 + tid]) + (far_sums[4 + tid] + far_sums[6 + tid]));
   }
 }
 
@@ -623,7 +643,7 @@ static hipError_t backward_case(const ExactArgs& a, const ExactGrads& g, const B
   const long long heads = (long long)a.B * a.H, kheads = (long long)a.B * a.Hkv;
   hipError_t e;
   if (a.nq > 0) {
-    const size_t smem = dq_stage + ((1 + kExactWaves) * entries + (BIAS ? kExactWaves * kSkew : 0)) * sizeof(float);
+    const size_t smem = dq_stage + ((1 + kExactWaves) * entries + (BIAS ? kExactWaves * kSkew : 0)) * sizeof(float) + (BIAS ? kFarBytes : 0);
     auto launch = [&](auto kernel, int blocks) {
       const hipError_t lds = allow_lds(kernel, smem);
       if (lds != hipSuccess) return lds;
