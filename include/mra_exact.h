@@ -118,7 +118,9 @@ size_t mra_exact_backward_workspace_bytes(const mra_exact_problem_t* p);
  *   out, lse : as mra_exact_forward wrote them for the same problem.
  *   dout     : [B][H][n_q][d], the gradient of out.
  *   dq, dk, dv : outputs with the shapes of q, k, v.
- *   dbias    : [buckets][H] of bias_dtype, or NULL to skip; NULL without bias.
+ *   dbias    : [buckets][H] of bias_dtype, or NULL to skip; NULL without bias. Over
+ *              many keys per distance of the map, where D's terms cancel, its D is
+ *              held to sum to 0 over a query's keys (bfloat16).
  */
 mra_status_t mra_exact_backward(const mra_exact_problem_t* p, const mra_strided_t* q,
                                 const mra_strided_t* k, const mra_strided_t* v,

@@ -100,11 +100,11 @@ mra::ExactArgs args_of(const mra_exact_problem_t& p) {
   return a;
 }
 
-// Workspace of the backward: delta per query, the diagonal sums (with a bias), the
-// partial sums of dq, dk and dv.
+// Workspace of the backward: delta per query, the diagonal sums (with a bias), the queries'
+// sums (exact_centre_kernel), the partial sums of dq, dk and dv.
 struct WsBackward {
   mra::BackwardPlan plan;
-  size_t diag, q, k, v, total;
+  size_t diag, rows, q, k, v, total;
 };
 
 WsBackward ws_backward(const mra_exact_problem_t& p) {
@@ -113,8 +113,10 @@ WsBackward ws_backward(const mra_exact_problem_t& p) {
   size_t off = align256((size_t)p.B * p.H * p.n_q * sizeof(float));
   w.diag = off;
   if (p.bias != nullptr)
-    off += align256((size_t)p.B * p.H * mra::exact_dq_blocks(p.n_q) * w.plan.dq_parts * mra::exact_window(p.far) *
+    off += align256((size_t)p.B * p.H * mra::exact_dq_blocks(p.n_q) * mra::exact_slots(w.plan) * mra::exact_window(p.far) *
                     sizeof(float));
+  w.rows = off;
+  if (w.plan.centre) off += align256((size_t)w.plan.dq_parts * p.B * p.H * p.n_q * 4 * sizeof(float));
   w.q = off; off += align256(w.plan.q_floats * sizeof(float));
   w.k = off; off += align256(w.plan.k_floats * sizeof(float));
   w.v = off; off += align256(w.plan.k_floats * sizeof(float));
@@ -196,14 +198,18 @@ mra_status_t mra_exact_backward(const mra_exact_problem_t* p, const mra_strided_
     g.dk = rows_of(dk, p->dtype);
     g.dv = rows_of(dv, p->dtype);
   }
-  mra::BackwardPlan plan{1, 1, 0, 0};
+  mra::BackwardPlan plan{1, 1, false, 0, 0};
   if (rows) {
     const WsBackward w = ws_backward(*p);
     MRA_TRY(check_workspace(workspace, workspace_bytes, w.total));
     plan = w.plan;
     auto at = [&](size_t off) { return reinterpret_cast<float*>(static_cast<char*>(workspace) + off); };
     g.delta = at(0);
-    if (dbias != nullptr) g.diag = at(w.diag);
+    if (dbias != nullptr) {
+      g.diag = at(w.diag);
+      g.slots = mra::exact_slots(plan);
+      if (plan.centre) g.row_sums = at(w.rows);
+    }
     g.part_q = at(w.q);
     g.part_k = at(w.k);
     g.part_v = at(w.v);

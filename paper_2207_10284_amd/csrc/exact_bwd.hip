@@ -14,6 +14,8 @@
 // and no partial dQ of n_k / 32 times the size. Where a pass has few blocks, several
 // workgroups share each and exact_sum_kernel adds their sums.
 //
+// exact_centre_kernel: bfloat16 over many keys, takes from dbias what roundings of Z leave in D.
+//
 // exact_bias_kernel: the diagonal sums of a head's blocks, added by bucket in a fixed
 // order.
 #include "exact_tile.h"
@@ -31,6 +33,22 @@ constexpr int kSkew = 32 * 64;
 constexpr int kFarStages = 16;
 constexpr size_t kFarBytes = kExactWaves * 2 * sizeof(double);
 
+// Adds the 16 numbers of a lane (row lane % 32 a query, 16 of its keys) of a 32 x 32 tile to a wave's
+// diagonal sums, `at` those of the tile's 63: row query, column key - query + 31 of the skewed tile,
+// so the diagonals are columns, a lane each.
+__device__ __forceinline__ void add_diagonals(float* skew, const float (&x)[16], float* at) {
+  const int lane = lane_id();
+  float* to = skew + 63 * (lane & 31) + 31 + 4 * (lane >> 5);
+#pragma unroll
+  for (int r = 0; r < 16; ++r) to[reg_row(r)] = x[r];
+  wave_lds_sync();
+  float t[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int q = 0; q < 32; ++q) t[q & 3] += skew[64 * q + lane];
+  at[lane] += (t[0] + t[1]) + (t[2] + t[3]);
+  wave_lds_sync();
+}
+
 int exact_dq_blocks(int nq) { return (nq + kDqRows - 1) / kDqRows; }
 // the window's entries, then the sums of the tiles below and above it
 int exact_window(int far) { return window_entries(far) + 2; }
@@ -42,6 +60,20 @@ template <int NP, int D>
 constexpr bool kDqTwo = NP == 1 && D == 128;
 template <int NP, int D>
 constexpr int kDqStageRows = kDqTwo<NP, D> ? 32 : kStageRows<NP, D>;
+
+// A workgroup's diagonal sums, those of its waves added in their order, to slot `slot` of its block.
+__device__ __forceinline__ void store_diagonals(const ExactGrads& g, long long block, int slot, int entries, const float* acc,
+                                                const double* far_sums) {
+  const int tid = threadIdx.x;
+  float* out = g.diag + (block * g.slots + slot) * (entries + 2);
+  for (int x = tid; x < entries; x += kExactThreads) {
+    float t = 0.0f;
+#pragma unroll
+    for (int p = 0; p < kExactWaves; ++p) t += acc[p * entries + x];
+    out[x] = t;
+  }
+  if (tid < 2) out[entries + tid] = (float)((far_sums[tid] + far_sums[2 + tid]) + (far_sums[4 + tid] + far_sums[6 + tid]));
+}
 
 // RT: 32-row tiles of queries per wave
 template <int NP, int D, int RT, bool BIAS>
@@ -85,8 +117,8 @@ __global__ __launch_bounds__(kExactThreads, (kDqTwo<NP, D> || RT == 2 ? 2 : 1)) 
     const int half = hf * (D / 2) * (NP == 1 ? 2 : 4);
     const u32x4* gr = reinterpret_cast<const u32x4*>(g.dout.p + b * g.dout.sb + h * g.dout.sh + ic * g.dout.sn + half);
     const u32x4* zr = reinterpret_cast<const u32x4*>(a.out.p + b * a.out.sb + h * a.out.sh + ic * a.out.sn + half);
-    // of Z as stored: the rounding of a bfloat16 Z is one number for all keys of the query
-    // (a float32 Z kept for this pass would cost twice its bytes)
+    // of Z as stored: the rounding of a bfloat16 Z is one number for all keys of the query (dbias: see
+    // exact_centre_kernel)
     float d = 0.0f;
 #pragma unroll
     for (int c = 0; c < LB; ++c) {
@@ -112,6 +144,8 @@ __global__ __launch_bounds__(kExactThreads, (kDqTwo<NP, D> || RT == 2 ? 2 : 1)) 
     delta[y] = none ? 0.0f : d;
   }
   float sum_lo = 0.0f, sum_hi = 0.0f;
+  double row_d = 0.0;                              // of this lane's query and keys: D, and P below and above the window
+  float row_lo = 0.0f, row_hi = 0.0f;
   float* mine = acc + w * entries;
   float* skew = acc + kExactWaves * entries + w * kSkew;
   double* far_sums = reinterpret_cast<double*>(acc + kExactWaves * (entries + kSkew));
@@ -122,6 +156,7 @@ __global__ __launch_bounds__(kExactThreads, (kDqTwo<NP, D> || RT == 2 ? 2 : 1)) 
 
   // this wave's sums beyond the window, to their doubles
   auto flush_far = [&]() {
+    if constexpr (NP == 1) row_d += (double)sum_lo + (double)sum_hi;
     float* both[2] = {&sum_lo, &sum_hi};
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
@@ -240,28 +275,30 @@ __global__ __launch_bounds__(kExactThreads, (kDqTwo<NP, D> || RT == 2 ? 2 : 1)) 
         }
         if (!PLAIN && (kb != ~0u || (a.causal && d0 + 31 > 0)))
           select_rows(s, a.causal ? kb & low_bits((lane & 31) - d0 + 1) : kb, -INFINITY);
-        float ds[16];
+        float p[16], ds[16];
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-          ds[r] = __builtin_amdgcn_exp2f(fmaf(s[r], mul, add)) * (NP == 1 && kSub ? dp[r] - delta[y] : dp[r]);
+        for (int r = 0; r < 16; ++r) {
+          p[r] = __builtin_amdgcn_exp2f(fmaf(s[r], mul, add));
+          ds[r] = p[r] * (NP == 1 && kSub ? dp[r] - delta[y] : dp[r]);
+        }
         if (BIAS && g.diag != nullptr) {
-          if (kind == kBiasNear) {
-            // row query, column key - query + 31: the diagonals are columns, a lane each
-            float* to = skew + 63 * (lane & 31) + 31 + 4 * hf;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) to[reg_row(r)] = ds[r];
-            wave_lds_sync();
-            float t[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int q = 0; q < 32; ++q) t[q & 3] += skew[64 * q + lane];
-            mine[d0 + a.far + kWinPad - 31 + lane] += (t[0] + t[1]) + (t[2] + t[3]);
-            wave_lds_sync();
-          } else {
-            float t = 0.0f;
+          if (kind == kBiasNear) add_diagonals(skew, ds, mine + (d0 + a.far + kWinPad - 31));
+          if (kind != kBiasNear || (NP == 1 && g.row_sums != nullptr)) {
+            float t = 0.0f, tp = 0.0f;
 #pragma unroll
             for (int r = 0; r < 16; ++r) t += ds[r];
             if (kind == kBiasLow) sum_lo += t;
-            else sum_hi += t;
+            if (kind == kBiasHigh) sum_hi += t;
+            if (NP == 1 && g.row_sums != nullptr) {
+              if (kind == kBiasNear) {
+                row_d += (double)t;                // of the others: flush_far
+              } else {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) tp += p[r];
+                if (kind == kBiasLow) row_lo += tp;
+                else row_hi += tp;
+              }
+            }
           }
         }
         dw[y] = pack_weights<NP>(ds);
@@ -313,16 +350,105 @@ __global__ __launch_bounds__(kExactThreads, (kDqTwo<NP, D> || RT == 2 ? 2 : 1)) 
     if (g.diag == nullptr) return;
     flush_far();
     __syncthreads();
-    const long long at_part = ((long long)h * a.B + b) * qblocks * parts + (long long)qb * parts + part;
-    float* out = g.diag + at_part * (entries + 2);
-    for (int x = tid; x < entries; x += kExactThreads) {
-      float t = 0.0f;
-#pragma unroll
-      for (int p = 0; p < kExactWaves; ++p) t += acc[p * entries + x];
-      out[x] = t;
+    store_diagonals(g, ((long long)h * a.B + b) * qblocks + qb, part, entries, acc, far_sums);
+    if (NP == 1 && g.row_sums != nullptr) {
+      const f32x4 t = {(float)(row_d + __shfl_xor(row_d, 32)), halves_sum(row_lo), halves_sum(row_hi), 0.0f};
+      if (lane < 32 && i0 < a.nq)
+        *reinterpret_cast<f32x4*>(g.row_sums + (((long long)part * a.B * a.H + bh) * a.nq + i0) * 4) = t;
     }
-    if (tid < 2) out[entries + tid] = (float)((far_sums[tid] + far_sums[2 + tid]) + (far_sums[4 + tid] + far_sums[6 + tid]));
   }
+}
+
+// dbias of bfloat16 calls over many keys. Over a query's keys D sums to 0, as P does to 1: delta
+// is the mean of G . v_j under P. As formed in the dQ pass, D sums to r = (that mean) - delta: delta is
+// G . Z of a Z whose weights and whose result were rounded. In dQ and dK r is one rounding
+// among others, but dbias sums D over many keys, which cancel, and P r stays: it grows against
+// the result like the root of the keys per distance of the window. So -P r is added to dbias (not to dQ and dK,
+// whose bits do not depend on whether dbias is asked for): beyond the window from each query's sums of P, which the
+// dQ pass leaves with r, and for the tiles of the window by forming P again, S in one product: few tiles of a long
+// row. What is left is the rounding of L, one factor a query. Error of dbias in 2-norm (float32 table): 64 queries x 20000
+// keys x 64: 9.7e-3 -> 1.9e-5; 31 x 12000 x 128: 8.8e-4 -> 4.8e-5; 2100 x 2100 x 64 causal 2.9e-3 -> 3.7e-4.
+template <int D>
+__global__ __launch_bounds__(kExactThreads) void exact_centre_kernel(ExactArgs a, ExactGrads g, int qblocks, int parts) {
+  constexpr int KT = kStageRows<1, D>, TILES = KT / 32;
+  using St = Stage<1, D, KT, kExactThreads>;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const int entries = window_entries(a.far);
+  float* win = reinterpret_cast<float*>(smem + 2 * St::kBytes);
+  float* acc = win + entries;
+  const int tid = threadIdx.x, lane = lane_id(), w = wave_uniform(tid / kWave);
+  float* mine = acc + w * entries;
+  float* skew = acc + kExactWaves * entries + w * kSkew;
+  double* far_sums = reinterpret_cast<double*>(acc + kExactWaves * (entries + kSkew));
+  const HeadBlock hb = head_block(blockIdx.x, a.B * a.H, qblocks, false);
+  const int bh = hb.head, qb = hb.block;
+  const int b = bh / a.H, h = bh - b * a.H, hk = h / a.group;
+  const int row0 = qb * kDqRows + w * 32, i = row0 + (lane & 31), ic = min(i, a.nq - 1);
+  const int limit = key_limit(a, b), start = first_position(a, b), pos0 = start + row0;
+  const int kend = a.causal ? min(limit, start + min((qb + 1) * kDqRows, a.nq)) : limit;
+  // the stages with tiles in the window of one of the block's waves, whose first queries are 32 apart
+  const int p_first = start + qb * kDqRows, p_last = p_first + kDqRows - 32;
+  const int begin = max(p_first - a.far - 30, 0) / KT;
+  const int stages = min(max(kend, 0), max(p_last + a.far + 31, 0)) > 0
+                         ? (min(kend, p_last + a.far + 31) + KT - 1) / KT : 0;
+  const char* kp = a.k.p + b * a.k.sb + hk * a.k.sh;
+
+  St ks;
+  ks.init(a.k.sn, tid);
+  MaskBytes<KT> bytes;
+  auto load = [&](int st) {
+    ks.load(kp, a.k.sn, st * KT, limit);
+    bytes.load(a, b, st * KT);
+  };
+  if (begin < stages) load(begin);
+  TileAddr<D> at;
+  at.init(smem);
+  u32x4 qf[1][D / 16];
+  load_operand<1, D>(a.q.p + b * a.q.sb + h * a.q.sh + ic * a.q.sn, i < a.nq, qf);
+  const long long at_row = (long long)bh * a.nq + ic;
+  const float L = g.lse[at_row];
+  const bool none = i >= a.nq || L == -INFINITY;
+  const float nl = none ? -INFINITY : -L * kLog2e;
+  f32x4 sums = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int p = 0; p < parts; ++p) {
+    const f32x4 t = *reinterpret_cast<const f32x4*>(g.row_sums + ((long long)p * a.B * a.H * a.nq + at_row) * 4);
+#pragma unroll
+    for (int e = 0; e < 3; ++e) sums[e] += t[e];
+  }
+  const float r = none ? 0.0f : sums[0];
+  fill_window(a, h, win, tid, kExactThreads);
+  for (int x = tid; x < kExactWaves * (entries + kSkew); x += kExactThreads) acc[x] = 0.0f;
+  for (int st = begin; st < stages; ++st) {
+    const RowBits<KT> ok = bytes.bits(st * KT, limit);
+    ks.store(smem + (st & 1) * St::kBytes, ok, tid);   // the other waves are at most a stage behind: in the other buffer
+    __syncthreads();
+    if (st + 1 < stages) load(st + 1);
+#pragma unroll
+    for (int x = 0; x < TILES; ++x) {
+      const uint32_t kb = ok.tile(x);
+      const int k0 = st * KT + 32 * x, d0 = k0 - pos0;
+      if (kb == 0 || (a.causal && d0 > 31) || bias_kind(d0, a.far) != kBiasNear) continue;
+      f32x16 s = product<1, D>(at, (st & 1) * St::kBytes + x * kTileBytes<D>, 0, qf, splat16(0.0f));
+      const float* wp = win + (d0 + a.far + kWinPad - (lane & 31) + 4 * (lane >> 5));
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] = fmaf(s[e], a.scale_log2, wp[reg_row(e)]);
+      if (kb != ~0u || (a.causal && d0 + 31 > 0))
+        select_rows(s, a.causal ? kb & low_bits((lane & 31) - d0 + 1) : kb, -INFINITY);
+      float ps[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) ps[e] = -r * __builtin_amdgcn_exp2f(s[e] + nl);
+      add_diagonals(skew, ps, mine + (d0 + a.far + kWinPad - 31));
+    }
+  }
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {                    // below and above the window
+    double t = lane < 32 && !none ? -(double)r * (double)sums[1 + x] : 0.0;
+#pragma unroll
+    for (int y = 1; y < kWave; y *= 2) t += __shfl_xor(t, y);
+    if (lane == 0) far_sums[2 * w + x] = t;
+  }
+  __syncthreads();
+  store_diagonals(g, ((long long)h * a.B + b) * qblocks + qb, parts, entries, acc, far_sums);
 }
 
 template <int NP, int D, bool BIAS>
@@ -629,6 +755,11 @@ BackwardPlan exact_backward_plan(const mra_exact_problem_t& p) {
   const long long qstages = (p.n_q + rows - 1) / rows, kstages = (p.n_k + rows - 1) / rows;
   b.dq_parts = parts_of(heads * exact_dq_blocks(p.n_q), kstages, f32 && p.d == 128 ? 1 : 2);
   b.dkv_parts = parts_of(kheads * exact_dq_blocks(p.n_k), qstages * (p.H / p.H_kv), p.d == 128 ? 1 : 2);
+  // Below eight keys per distance of the window the 2-norm of dbias's error is a bfloat16 rounding's
+  // at most (2.6e-3 at 512 keys and 183 distances, 3.2e-3 at 1503), and the window's tiles are much of a row
+  // (training, 8 x 12 heads x 1024 x 32: 133 us, 157 with exact_centre_kernel; where it runs: 32 heads x 2048 x 128
+  // causal 390 -> 423, 8 x 8192 x 128 1397 -> 1446).
+  b.centre = !f32 && p.bias != nullptr && p.n_k > 8 * (2 * (long long)p.far + 1);
   if (b.dq_parts > 1) b.q_floats = (size_t)b.dq_parts * heads * p.n_q * p.d;
   if (b.dkv_parts > 1) b.k_floats = (size_t)b.dkv_parts * kheads * p.n_k * p.d;
   return b;
@@ -658,6 +789,16 @@ static hipError_t backward_case(const ExactArgs& a, const ExactGrads& g, const B
       e = launch(exact_dq_kernel<NP, D, 1, BIAS>, qblocks);
     }
     if (e != hipSuccess) return e;
+    if constexpr (NP == 1 && BIAS) {
+      if (g.row_sums != nullptr) {
+        const size_t centre = 2 * Stage<1, D, kStageRows<1, D>, kExactThreads>::kBytes +
+                              ((1 + kExactWaves) * entries + kExactWaves * kSkew) * sizeof(float) + kFarBytes;
+        auto kernel = exact_centre_kernel<D>;
+        if ((e = allow_lds(kernel, centre)) != hipSuccess) return e;
+        kernel<<<(unsigned)(heads * qblocks), kExactThreads, centre, stream>>>(a, g, qblocks, plan.dq_parts);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+      }
+    }
   }
   if (a.nk > 0) {
     const size_t smem = stage + 64 * kStageRows<NP, D> + entries * sizeof(float);
@@ -707,7 +848,7 @@ hipError_t launch_exact_backward(const ExactArgs& a, const ExactGrads& g, const 
     if (e != hipSuccess) return e;
   }
   if (g.dbias != nullptr && a.H > 0)
-    exact_bias_kernel<<<dim3(a.H, a.buckets), kBiasThreads, 0, stream>>>(a, g.diag, a.B * exact_dq_blocks(a.nq) * plan.dq_parts, g.dbias);
+    exact_bias_kernel<<<dim3(a.H, a.buckets), kBiasThreads, 0, stream>>>(a, g.diag, a.B * exact_dq_blocks(a.nq) * g.slots, g.dbias);
   return hipGetLastError();
 }
 

@@ -48,7 +48,9 @@ struct ExactGrads {
   Rows dout, dq, dk, dv;
   const float* lse;
   float* delta;                           // [B, H, n_q]: G . Z per query
-  float* diag;                            // [H, B, blocks, parts, window]: sums of dS over diagonals; null: not asked for
+  float* diag;                            // [H, B, blocks, slots, window]: sums of dS over diagonals; null: not asked for
+  int slots;                              // parts of the dQ pass, and one of exact_centre_kernel
+  float* row_sums;                        // [parts, B, H, n_q, 4]: see exact_centre_kernel; null: it does not run
   void* dbias;
   float *part_q, *part_k, *part_v;        // [parts, B, heads, n, d]: see BackwardPlan
 };
@@ -56,9 +58,12 @@ struct ExactGrads {
 // How many workgroups share a block of the passes, and the floats of their partial sums.
 struct BackwardPlan {
   int dq_parts, dkv_parts;
+  bool centre;                            // exact_centre_kernel, where dbias is asked for
   size_t q_floats, k_floats;              // of dq; of dk, and of dv (0: one part)
 };
 BackwardPlan exact_backward_plan(const mra_exact_problem_t& p);
+// Workgroups whose diagonal sums a query block has.
+inline int exact_slots(const BackwardPlan& b) { return b.dq_parts + (b.centre ? 1 : 0); }
 // Query blocks of the dQ pass per head and floats of a block's diagonal sums.
 int exact_dq_blocks(int nq);
 int exact_window(int far);

@@ -3,6 +3,7 @@ import pytest
 import torch
 
 from oracle import exact_oracle as E
+from tests.test_gpu_exact import make, options, run
 
 
 @pytest.mark.parametrize("planes,d", [(p, d) for p in (1, 3) for d in (32, 64, 128)])
@@ -49,3 +50,52 @@ def test_terms_that_rise_and_fall(gpu, dt):
     P = 2.0 ** -n.bit_length() * 2
     assert -161 * nq * P < ref[15, 0] < -150 * nq * P
     assert abs(dbias[15, 0].double() - ref[15, 0]) <= nq * 6.5 * P + 2.0 ** -19 * ref[15, 0].abs()
+
+
+# B, H, H_kv, n_q, n_k, d, what options takes
+MANY_KEYS = [
+    (1, 1, 1, 64, 20000, 64, dict(buckets=(32, 128, True))),                         # parts of every block
+    (2, 2, 1, 256, 9000, 32, dict(buckets=(32, 128, True), mask="lk")),
+    (1, 4, 2, 2100, 2100, 128, dict(buckets=(32, 128, False), causal=True)),
+    (2, 2, 2, 150, 3000, 64, dict(buckets=(8, 20, True), start=True, mask="k")),
+    (3, 8, 8, 333, 1500, 64, dict(buckets=(16, 50, True), mask="le")),
+    (1, 2, 2, 31, 12000, 128, dict(buckets=(64, 256, True))),
+    (1, 1, 1, 700, 5000, 32, dict(buckets=(4, 8, False), causal=True, mask="l")),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("case", range(len(MANY_KEYS)))
+def test_bfloat16_over_many_keys(gpu, case):
+    """Over many keys the roundings of a bfloat16 Z stay out of dbias (a float32 table: its own
+    rounding is 2^-24). What is left in a query's D, 2-norm over the buckets:
+
+    - L is the logarithm of a sum of rounded weights: one factor for the query's D, off by the sum of
+      P_ij rho_j, roundings |rho| <= 2^-8, independent: 2^-8 |P_i| is more than twice its root mean
+      square, and it meets the query's sums of D by bucket, B_i.
+    - float32: the exponent's argument (up to 16: 2^-21), the exponential, two products of up to
+      eight matrix steps: 2^-18 of each term, independent over keys: 2^-18 |D_i|.
+
+    2-norms over queries add in quadrature, held to twice their sum. With the roundings of Z it would be about 2^-9 |P_i|
+    |G . v| |sums of P by bucket| a query, at least four times the bound except where causal rows of
+    few keys outweigh the others."""
+    B, H, Hkv, nq, nk, d, opts = MANY_KEYS[case]
+    print("many keys", MANY_KEYS[case], flush=True)
+    q, k, v, g = make(71 + case, "bf16", B, H, Hkv, nq, nk, d)
+    o = options(gpu, 72 + case, B, H, nq, nk, table="f32", **opts)
+    assert o["bias"].dtype == torch.float32 and nk > 8 * o["buckets"].numel()
+    got = run(gpu, q, k, v, g, o)[2][3]
+    ref = E.gradients(q, k, v, g, **o)[3]
+    Z, _, P = E.attention(q, k, v, **o)
+    V = E._clean(v, o.get("lengths"), o.get("key_mask")).repeat_interleave(H // Hkv, 1)
+    dP = g.double() @ V.transpose(2, 3).contiguous()
+    D = P * (dP - (g.double() * Z).sum(-1, keepdim=True))
+    far = o["buckets"].numel() // 2
+    start = torch.full((B,), nk - nq, device="cuda") if o.get("q_start") is None else o["q_start"].long()
+    rel = torch.arange(nk, device="cuda") - (start[:, None] + torch.arange(nq, device="cuda"))[:, :, None]
+    at = o["buckets"].long()[rel.clamp(-far, far) + far][:, None]
+    by_d, by_p = (sum((x * (at == c)).sum(-1).square() for c in range(o["bias"].shape[0])).sqrt() for x in (D, P))
+    size = P.norm(dim=-1)
+    bound = 2 * ((2.0 ** -8 * size * by_d).norm() + 2.0 ** -18 * D.norm())
+    assert (nq == nk and opts["causal"]) or (2.0 ** -9 * (P * dP).norm(dim=-1) * by_p).norm() > 4 * bound
+    assert (got.double() - ref).norm() <= bound
