@@ -26,7 +26,10 @@
  *   (the d elements of a row are consecutive). Every stride is >= 0 and a
  *   multiple of 16 bytes. Input strides may be 0 (a broadcast axis). Outputs
  *   must not overlap themselves or another argument.
- * - d is 32, 64 or 128; 0 <= n_q, n_k <= 2^26; row strides below 2^25 bytes.
+ * - d is 32, 64 or 128; 0 <= n_q, n_k <= 2^26; row strides below 2^25 bytes. A
+ *   pass has below 2^24 workgroups: B H ceil(n_q / 128), and in the backward
+ *   B H_kv ceil(n_k / 128); a forward with r = n_q H / H_kv <= 64 rows per key head
+ *   has B H_kv ceil(r / 32) instead.
  * - A bias below -2^14 (-infinity and the usual masks of -1e9, -1e30 or a type's
  *   lowest value among them) takes its distances out: such a key does not count.
  *   One above 2^14 is taken as 2^14: its keys outweigh all others, and among

@@ -14,7 +14,8 @@ namespace {
 thread_local int g_last_hip_error = 0;
 
 constexpr int kMaxLen = 1 << 26;
-constexpr long long kMaxGrid = 2147483647LL;
+constexpr long long kMaxIndex = 2147483647LL;     // block and row indices are 32-bit integers
+constexpr long long kMaxGroups = (1LL << 32) / 256 - 1;   // a launch has below 2^32 threads per dimension, 256 a workgroup
 constexpr int64_t kMaxRowStride = 1 << 25;        // bytes: 64 rows within 32 bits
 
 #define MRA_TRY(expr)                 \
@@ -51,17 +52,30 @@ mra_status_t check_problem(const mra_exact_problem_t* p) {
     if (p->buckets < 1 || p->far < 0 || p->bucket_map == nullptr) return MRA_ERR_INVALID_ARG;
     if (p->buckets > MRA_EXACT_MAX_BUCKETS || p->far > MRA_EXACT_MAX_FAR) return MRA_ERR_UNSUPPORTED;
   }
-  // workgroups of the largest launches: 128 rows of a head each (fewer of a key head:
-  // 32 of its heads' rows, times at most 64, and only where the former are below one per CU)
+  // blocks of 128 rows of all heads, and rows
   const long long longest = p->n_q > p->n_k ? p->n_q : p->n_k;
   const long long heads = (long long)p->B * p->H, blocks = (longest + 127) / 128;
-  if (blocks > 0 && heads > kMaxGrid / blocks) return MRA_ERR_UNSUPPORTED;
-  const long long rows = heads * p->n_q;           // one thread of the join per four columns of a row
-  if (rows > kMaxGrid) return MRA_ERR_UNSUPPORTED;
+  if (blocks > 0 && heads > kMaxIndex / blocks) return MRA_ERR_UNSUPPORTED;
+  const long long rows = heads * p->n_q;
+  if (rows > kMaxIndex) return MRA_ERR_UNSUPPORTED;
   return MRA_OK;
 }
 
 bool empty(const mra_exact_problem_t& p) { return p.B == 0 || p.H == 0 || p.n_q == 0; }
+
+// Whether every launch of a call fits; those not named have fewer workgroups (the join: splits are
+// several only below two workgroups a CU; the parts' sums: only where a pass has at most eight).
+mra_status_t check_forward_grid(const mra_exact_problem_t& p, const mra::SplitPlan& plan) {
+  const long long groups = plan.use ? (long long)p.B * p.H_kv * plan.mtiles * plan.splits
+                                    : (long long)p.B * p.H * ((p.n_q + 127) / 128);
+  return groups <= kMaxGroups ? MRA_OK : MRA_ERR_UNSUPPORTED;
+}
+
+mra_status_t check_backward_grid(const mra_exact_problem_t& p) {
+  const long long dq = (long long)p.B * p.H * mra::exact_dq_blocks(p.n_q), dkv = (long long)p.B * p.H_kv * mra::exact_dq_blocks(p.n_k);
+  const long long bias = p.bias != nullptr ? p.H : 0;
+  return dq <= kMaxGroups && dkv <= kMaxGroups && bias <= kMaxGroups ? MRA_OK : MRA_ERR_UNSUPPORTED;
+}
 
 mra_status_t check_tensor(const mra_strided_t* t, mra_dtype_t dt) {
   if (t == nullptr || t->data == nullptr) return MRA_ERR_INVALID_ARG;
@@ -137,7 +151,8 @@ extern "C" {
 
 size_t mra_exact_forward_workspace_bytes(const mra_exact_problem_t* p) {
   if (check_problem(p) != MRA_OK || empty(*p)) return 0;
-  return mra::exact_split_plan(*p).bytes;
+  const mra::SplitPlan plan = mra::exact_split_plan(*p);
+  return check_forward_grid(*p, plan) == MRA_OK ? plan.bytes : 0;
 }
 
 mra_status_t mra_exact_forward(const mra_exact_problem_t* p, const mra_strided_t* q, const mra_strided_t* k,
@@ -145,6 +160,8 @@ mra_status_t mra_exact_forward(const mra_exact_problem_t* p, const mra_strided_t
                                size_t workspace_bytes, void* stream) {
   MRA_TRY(check_problem(p));
   if (empty(*p)) return MRA_OK;
+  const mra::SplitPlan plan = mra::exact_split_plan(*p);
+  MRA_TRY(check_forward_grid(*p, plan));
   MRA_TRY(check_tensor(q, p->dtype));
   MRA_TRY(check_tensor(out, p->dtype));
   if (p->n_k > 0) {
@@ -152,7 +169,6 @@ mra_status_t mra_exact_forward(const mra_exact_problem_t* p, const mra_strided_t
     MRA_TRY(check_tensor(v, p->dtype));
   }
   if (lse_out != nullptr && !aligned16(lse_out)) return MRA_ERR_MISALIGNED;
-  const mra::SplitPlan plan = mra::exact_split_plan(*p);
   MRA_TRY(check_workspace(workspace, workspace_bytes, plan.bytes));
   mra::ExactArgs a = args_of(*p);
   a.q = rows_of(q, p->dtype);
@@ -166,7 +182,7 @@ mra_status_t mra_exact_forward(const mra_exact_problem_t* p, const mra_strided_t
 }
 
 size_t mra_exact_backward_workspace_bytes(const mra_exact_problem_t* p) {
-  if (check_problem(p) != MRA_OK || empty(*p)) return 0;
+  if (check_problem(p) != MRA_OK || check_backward_grid(*p) != MRA_OK || empty(*p)) return 0;
   return ws_backward(*p).total;
 }
 
@@ -176,6 +192,7 @@ mra_status_t mra_exact_backward(const mra_exact_problem_t* p, const mra_strided_
                                 const mra_strided_t* dv, void* dbias, void* workspace, size_t workspace_bytes,
                                 void* stream) {
   MRA_TRY(check_problem(p));
+  MRA_TRY(check_backward_grid(*p));
   if (dbias != nullptr && p->bias == nullptr) return MRA_ERR_INVALID_ARG;
   if (dbias != nullptr && !aligned16(dbias)) return MRA_ERR_MISALIGNED;
   const bool rows = !empty(*p), keys = p->B > 0 && p->H > 0 && p->n_k > 0;
