@@ -10,6 +10,8 @@
 #include <ATen/ops/empty_like.h>
 #include <c10/core/DeviceGuard.h>
 #include <torch/csrc/autograd/custom_function.h>
+#include <torch/csrc/autograd/functions/basic_ops.h>
+#include <torch/csrc/autograd/functions/utils.h>
 
 #include <cmath>
 #include <limits>
@@ -213,7 +215,24 @@ struct Exact : torch::autograd::Function<Exact> {
        api.backward(&p, &vq, &vk, &vv, &vo, &vg, static_cast<const float*>(lse.data_ptr()), &vdq, &vdk, &vdv,
                     db.defined() ? db.data_ptr() : nullptr, need ? ws.data_ptr() : nullptr, need, stream_of(q)));
     const at::Tensor none;
-    return {dq, dk, dv, db, none, none, none, none, none, none};
+    torch::autograd::variable_list result{dq, dk, dv, db, none, none, none, none, none, none};
+    if (at::GradMode::is_enabled()) differentiated_once(result, {q, k, v, t[5], dout});
+    return result;
+  }
+
+  // Gradients taken with a graph of their own, which does not reach through them: where the output's
+  // gradient (the last of `of`) has one, a node whose backward raises stands between them and
+  // what they depend on; where it is a constant they are constants too, and a warning says so.
+  static void differentiated_once(torch::autograd::variable_list& grads, const torch::autograd::variable_list& of) {
+    if (!of.back().requires_grad()) {
+      TORCH_WARN("the gradients of exact_attention are not differentiable: these are constants of the graph");
+      return;
+    }
+    const auto error = std::make_shared<torch::autograd::Error>(
+        "the gradients of exact_attention are not differentiable: trying to differentiate twice",
+        torch::autograd::collect_next_edges(of));
+    for (at::Tensor& t : grads)
+      if (t.defined()) torch::autograd::set_history(t, error);
   }
 };
 

@@ -20,6 +20,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
+import warnings
 
 import torch
 
@@ -769,6 +770,21 @@ def exact_attention_backward(q, k, v, out, dout, lse, *, scale=None, causal: boo
     return (*grads, dbias)
 
 
+_ONCE = "the gradients of exact_attention are not differentiable"
+
+
+class _DifferentiatedOnce(torch.autograd.Function):
+    """Gradients (the first four) as functions of what follows, whose derivatives raise."""
+
+    @staticmethod
+    def forward(ctx, *tensors):
+        return tuple(None if t is None else t.detach() for t in tensors[:4])
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError(f"{_ONCE}: trying to differentiate twice")
+
+
 class ExactAttention(torch.autograd.Function):
     """``exact_attention_forward`` as a differentiable op of q, k, v and bias."""
 
@@ -782,22 +798,26 @@ class ExactAttention(torch.autograd.Function):
         return out
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
     def backward(ctx, dout):
         q, k, v, out, lse, bias, buckets, lengths, key_mask, q_start = ctx.saved_tensors
-        if not _dense_rows(dout):
-            dout = dout.contiguous()
-        dq, dk, dv, dbias = exact_attention_backward(q, k, v, out, dout, lse, scale=ctx.scale, causal=ctx.causal,
-                                                     lengths=lengths, key_mask=key_mask, q_start=q_start, bias=bias,
-                                                     buckets=buckets)
-        return dq, dk, dv, dbias, None, None, None, None, None, None
+        with torch.no_grad():
+            g = dout if _dense_rows(dout) else dout.contiguous()
+            grads = exact_attention_backward(q, k, v, out, g, lse, scale=ctx.scale, causal=ctx.causal, lengths=lengths,
+                                             key_mask=key_mask, q_start=q_start, bias=bias, buckets=buckets)
+        if torch.is_grad_enabled():
+            if dout.requires_grad:
+                grads = _DifferentiatedOnce.apply(*grads, q, k, v, bias, dout)
+            else:
+                warnings.warn(f"{_ONCE}: these are constants of the graph")
+        return (*grads, None, None, None, None, None, None)
 
 
 def exact_attention(q, k, v, *, scale=None, causal: bool = False, lengths=None, key_mask=None, q_start=None,
                     bias=None, buckets=None):
     """Differentiable exact softmax attention (arguments and result as
     ``exact_attention_forward``), with gradients of q, k, v and bias, which are not
-    differentiable themselves; native where ``mra_attention`` is. A backward pass
+    differentiable themselves: taken with create_graph, they raise where they are
+    differentiated, or warn if the output's gradient is a constant; native where ``mra_attention`` is. A backward pass
     that a graph captures needs leaves of which no eager graph is alive (with
     one, torch's engine can end the process)."""
     tensors = (q, k, v, lengths, key_mask, q_start, bias, buckets)
