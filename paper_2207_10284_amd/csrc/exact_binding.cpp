@@ -9,7 +9,9 @@
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_like.h>
 #include <c10/core/DeviceGuard.h>
+#include <c10/hip/HIPGraphsC10Utils.h>
 #include <torch/csrc/autograd/custom_function.h>
+#include <torch/csrc/autograd/functions/accumulate_grad.h>
 #include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/csrc/autograd/functions/utils.h>
 
@@ -173,6 +175,23 @@ at::Tensor forward(const at::Tensor& q, const at::Tensor& k, const at::Tensor& v
   return z;
 }
 
+// A leaf's accumulator belongs to the stream on which the leaf entered the oldest graph that is
+// alive: of eager work, the default stream. The engine would have it wait for the stream of a backward that a HIP
+// graph captures, which the default stream cannot: the capture fails in the engine, where that can end
+// the process. So such a backward is refused before it enqueues anything. (Leaves further up are not in sight.)
+void check_capture(const torch::autograd::Node& node) {
+  for (size_t i = 0; i < node.num_outputs(); ++i) {
+    const torch::autograd::Edge& e = node.next_edge(i);
+    if (!node.task_should_compute_output(i)) continue;   // of a backward for other inputs
+    if (dynamic_cast<torch::autograd::AccumulateGrad*>(e.function.get()) == nullptr) continue;
+    const auto stream = e.function->stream();
+    if (!stream || stream->id() != 0) continue;    // 0: the default stream
+    TORCH_CHECK(c10::hip::currentStreamCaptureStatusMayInitCtx() == c10::hip::CaptureStatus::None,
+                "a graph captures the backward of exact_attention while an eager graph of one of its inputs is alive, "
+                "whose gradient belongs to the default stream; drop the outputs of that graph first");
+  }
+}
+
 // ops.exact_attention
 struct Exact : torch::autograd::Function<Exact> {
   static at::Tensor forward(torch::autograd::AutogradContext* ctx, const at::Tensor& q, const at::Tensor& k,
@@ -194,6 +213,7 @@ struct Exact : torch::autograd::Function<Exact> {
   // the gradients, with everything allocated here (ops.exact_attention_backward)
   static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx,
                                                  torch::autograd::variable_list grads) {
+    check_capture(*torch::autograd::get_current_node());
     const auto t = ctx->get_saved_variables();
     const at::Tensor &q = t[0], &k = t[1], &v = t[2], &out = t[3], &lse = t[4];
     auto opt = [&](int i) { return t[i].defined() ? &t[i] : nullptr; };
@@ -252,6 +272,10 @@ PYBIND11_MODULE(_binding_exact, m) {
     bind_one(a, "mra_exact_backward", api.backward);
     status_error = std::move(raiser);
   });
+  // of the backward that runs, or of the one that made z
+  m.def("check_capture", [](const std::optional<at::Tensor>& z) {
+    check_capture(z ? *z->grad_fn() : *torch::autograd::get_current_node());
+  }, py::arg("z") = py::none());
   m.def("forward", torch::wrap_pybind_function_no_gil(forward));
   m.def("exact_attention", torch::wrap_pybind_function_no_gil(exact_attention));
 }

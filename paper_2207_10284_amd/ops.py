@@ -799,6 +799,8 @@ class ExactAttention(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, dout):
+        if not torch.compiler.is_compiling() and torch.cuda.is_current_stream_capturing():
+            bind_exact().check_capture()
         q, k, v, out, lse, bias, buckets, lengths, key_mask, q_start = ctx.saved_tensors
         with torch.no_grad():
             g = dout if _dense_rows(dout) else dout.contiguous()
@@ -818,8 +820,9 @@ def exact_attention(q, k, v, *, scale=None, causal: bool = False, lengths=None, 
     ``exact_attention_forward``), with gradients of q, k, v and bias, which are not
     differentiable themselves: taken with create_graph, they raise where they are
     differentiated, or warn if the output's gradient is a constant; native where ``mra_attention`` is. A backward pass
-    that a graph captures needs leaves of which no eager graph is alive (with
-    one, torch's engine can end the process)."""
+    that a graph captures needs leaves of which no eager graph is alive (with one
+    on the default stream, torch's engine can end the process): a RuntimeError where
+    such a leaf is an input, unseen where the inputs were computed from it."""
     tensors = (q, k, v, lengths, key_mask, q_start, bias, buckets)
     if (all(t is None or type(t) in _PLAIN for t in tensors)
             and not torch._C._are_functorch_transforms_active() and torch._C._get_tracing_state() is None
