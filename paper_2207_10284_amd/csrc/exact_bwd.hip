@@ -492,7 +492,7 @@ __global__ __launch_bounds__(kExactThreads, NP == 3 && D == 64 ? 2 : 1) void exa
   // The stages go from the last query down, and with one bias through all heads at each: workgroups
   // that start together then read the same rows, which the XCD's L2 holds, wherever their keys'
   // first query lies (16 heads on 4 x 16384 x 128 causal: 0.9 GB from beyond L2, 5.3 head after
-  // head from each block's first query on; training 5.13 -> 5.05 ms).
+  // head from each block's first query on; training 5.13 -> 5.05 ms in turn on one card, less than cards differ by).
   const int inner = BIAS ? 1 : a.group;
   // this workgroup's part of the stages of all heads
   const long long all = (long long)a.group * stages;

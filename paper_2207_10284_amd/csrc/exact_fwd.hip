@@ -133,7 +133,7 @@ template <int NP, int D, int R>
 __device__ __forceinline__ void products(const TileAddr<D>& at, int tile, int step, const FwdRow<NP, D> (&row)[R],
                                          f32x16 (&s)[R]) {
   static_assert(NP == 1 || R == 1, "float32: 32 queries per wave");
-  if constexpr (NP == 3 && D == 128) {             // fewer chunks at a time, for registers: 342 -> 325 us, 32 heads x 1503
+  if constexpr (NP == 3 && D == 128) {             // fewer chunks at a time, for registers: 314 -> 296 us, 32 heads x 1503
     s[0] = product<NP, D>(at, tile, step, row[0].qf, splat16(0.0f));
     return;
   }
@@ -476,10 +476,10 @@ __global__ __launch_bounds__(256) void exact_join_kernel(ExactArgs a, float* __r
     lse[((long long)b * a.H + h) * a.nq + i] = sum > 0.0f ? (log2f(sum) + top) * kLn2 : -INFINITY;
 }
 
-// The split kernel serves calls whose 128-row workgroups would leave most of the
-// chip idle, and those whose rows would leave most of each workgroup idle; its
-// workgroups are at least two per CU where the keys allow, each with at least two
-// tiles per wave.
+// The split kernel serves calls of fewer 128-row workgroups than CUs, and those whose
+// rows would leave at least half of each workgroup idle (up to 64 rows a key head); its
+// workgroups are at least two per CU where the keys allow, at most one per 256 keys begun.
+// Measured well inside either side (4 and 48 blocks, single tokens; 288 blocks and more), not at the border.
 SplitPlan exact_split_plan(const mra_exact_problem_t& p) {
   SplitPlan s{};
   const long long heads = (long long)p.B * p.H, kheads = (long long)p.B * p.H_kv;
