@@ -185,7 +185,8 @@ void check_capture(const torch::autograd::Node& node) {
     if (!node.task_should_compute_output(i)) continue;   // of a backward for other inputs
     if (dynamic_cast<torch::autograd::AccumulateGrad*>(e.function.get()) == nullptr) continue;
     const auto stream = e.function->stream();
-    if (!stream || stream->id() != 0) continue;    // 0: the default stream
+    // 0: the default stream, which does not capture itself
+    if (!stream || stream->id() != 0 || c10::hip::getCurrentHIPStream(stream->device_index()).id() == 0) continue;
     TORCH_CHECK(c10::hip::currentStreamCaptureStatusMayInitCtx() == c10::hip::CaptureStatus::None,
                 "a graph captures the backward of exact_attention while an eager graph of one of its inputs is alive, "
                 "whose gradient belongs to the default stream; drop the outputs of that graph first");
