@@ -1,6 +1,6 @@
-"""Build libmra.so and libmra_exact.so (the HIP kernels and their C ABIs, gfx950)
-and _binding.so and _binding_exact.so (the torch bindings of ops.py's calls, host
-code) in-tree.
+"""Build libmra.so, libmra_exact.so and libmra_layer.so (the HIP kernels and their C
+ABIs, gfx950) and _binding.so, _binding_exact.so and _binding_layer.so (the torch
+bindings of ops.py's calls, host code) in-tree.
 
     python -m paper_2207_10284_amd.build
 
@@ -23,11 +23,14 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libmra.so")
 LIB_EXACT = os.path.join(PKG, "libmra_exact.so")
+LIB_LAYER = os.path.join(PKG, "libmra_layer.so")
 BINDING = os.path.join(PKG, "_binding.so")
 BINDING_EXACT = os.path.join(PKG, "_binding_exact.so")
+BINDING_LAYER = os.path.join(PKG, "_binding_layer.so")
 SOURCES = ["api.cpp", "pool.hip", "coarse.hip", "select.hip", "select_global.hip", "tile.hip",
            "bwd.hip", "multilevel.hip", "noalloc.hip"]
 EXACT_SOURCES = ["exact_api.cpp", "exact_fwd.hip", "exact_bwd.hip"]
+LAYER_SOURCES = ["layer_api.cpp", "rotary.hip", "fp4_cache.hip", "fp4_attention.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
@@ -83,16 +86,20 @@ def build(verbose: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
     with cf.ThreadPoolExecutor(max_workers=8) as ex:
         bindings = [ex.submit(_build_binding, "binding.cpp", BINDING),
-                    ex.submit(_build_binding, "exact_binding.cpp", BINDING_EXACT)]
+                    ex.submit(_build_binding, "exact_binding.cpp", BINDING_EXACT),
+                    ex.submit(_build_binding, "layer_binding.cpp", BINDING_LAYER)]
         exact = [ex.submit(_compile, s) for s in EXACT_SOURCES]
+        layer = [ex.submit(_compile, s) for s in LAYER_SOURCES]
         objs = list(ex.map(_compile, SOURCES))
         exact = [f.result() for f in exact]
+        layer = [f.result() for f in layer]
         for b in bindings:
             b.result()
     _link(objs, LIB)
     _link(exact, LIB_EXACT)
+    _link(layer, LIB_LAYER)
     if verbose:
-        print(f"built {LIB}, {LIB_EXACT}, {BINDING} and {BINDING_EXACT}")
+        print(f"built {LIB}, {LIB_EXACT}, {LIB_LAYER}, {BINDING}, {BINDING_EXACT} and {BINDING_LAYER}")
     return LIB
 
 

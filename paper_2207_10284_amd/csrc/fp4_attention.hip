@@ -1,0 +1,276 @@
+// Attention over the 4-bit cache (mra_layer.h).
+//
+// As in exact_fwd.hip S is formed transposed, S^T = K Q^T, so that a lane's scores of one
+// query are the B operand of O^T += V^T P^T as they are, and the softmax runs against a reference
+// that moves only when a tile outgrows it. The rows of a key head, all queries of all its heads,
+// are one list: row m is query m / group of head hk group + m % group.
+//
+// fp4_rows_kernel: a workgroup's four waves take 32 rows each and walk the keys
+// together, 64 at a time. Codes come through registers and are converted once per workgroup: keys to
+// bfloat16 rows in LDS, values to rows of a channel's 64 tokens, which is the A operand that the second
+// product wants, so nothing is transposed.
+#include "exact_rows.h"
+#include "fp4_tile.h"
+
+namespace mra {
+
+namespace {
+
+__device__ __forceinline__ int cached_keys(const CacheAttentionArgs& a, int b) {
+  return min(max(a.lengths[b], 0), a.c.cap);
+}
+
+// Position of query 0 of sequence b.
+__device__ __forceinline__ int first_query(const CacheAttentionArgs& a, int b, int keys) {
+  constexpr int kFar = 1 << 29;
+  return a.q_start == nullptr ? keys - a.nq : min(max(a.q_start[b], -kFar), kFar);
+}
+
+// Bits of a step dword's byte i as a float32 step.
+__device__ __forceinline__ float step_of(uint32_t w, int i) { return fp4_step(w >> 8 * i & 255u); }
+
+// A stage's 64 keys of one head on their way from the cache to LDS.
+template <int D>
+struct CacheStage {
+  using Pg = Fp4Page<D>;
+  static constexpr int kKeys = 128 * D;            // bytes of the keys in LDS; the values take as many
+  // 16 bytes of codes a lane: all lanes have keys and values at D = 128, half of them either
+  // at 64; at 32 keys are 64 lanes' and values 8 bytes of 128 lanes
+  static constexpr int KU = 2 * D, VU = D == 32 ? 128 : 2 * D, V0 = kExactThreads - VU;
+  static constexpr int kSteps = Pg::NB * 8 / 4;    // dwords of eight tokens' steps
+  u32x4 k, v;
+  uint32_t ke, ve[kSteps];
+
+  // pg: the pages of the two halves of the stage, null where no key counts
+  __device__ __forceinline__ void load(const char* (&pg)[2], int k0, int size, int tid) {
+    const int slot0 = k0 & (size - 1), slot1 = (k0 + 32) & (size - 1);
+    if (tid < KU) {
+      const int r = tid / Pg::NB, blk = tid % Pg::NB;
+      const char* p = r < 32 ? pg[0] : pg[1];
+      const int slot = (r < 32 ? slot0 : slot1) + r % 32;
+      k = u32x4{0, 0, 0, 0};
+      ke = 127;
+      if (p != nullptr) {
+        k = *reinterpret_cast<const u32x4*>(p + slot * (D / 2) + blk * 16);
+        ke = (uint8_t)p[Pg::key_steps(size) + slot * Pg::NB + blk];
+      }
+    }
+    if (tid >= V0) {
+      const int u = tid - V0, t8 = u / (VU / 8);   // a tile of eight tokens
+      const char* p = t8 < 4 ? pg[0] : pg[1];
+      const int slot = (t8 < 4 ? slot0 : slot1) + t8 % 4 * 8;
+      v = u32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i) ve[i] = 0x7f7f7f7fu;
+      if (p != nullptr) {
+        const char* from = p + Pg::values(size) + slot * (D / 2) + u % (VU / 8) * (D == 32 ? 8 : 16);
+        if constexpr (D == 32) {
+          const u32x2 x = *reinterpret_cast<const u32x2*>(from);
+          v[0] = x[0];
+          v[1] = x[1];
+        } else {
+          v = *reinterpret_cast<const u32x4*>(from);
+        }
+        const uint32_t* s = reinterpret_cast<const uint32_t*>(p + Pg::value_steps(size) + slot * Pg::NB);
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) ve[i] = s[i];
+      }
+    }
+  }
+
+  // ok: the keys that count; the steps of others may be anything
+  __device__ __forceinline__ void store(char* lds, const RowBits<64>& ok, int tid) const {
+    if (tid < KU) {
+      const int r = tid / Pg::NB, blk = tid % Pg::NB;
+      // key 16 u + 8 h + 4 a + c of a tile lies at row 16 u + 8 a + 4 h + c: a lane's scores are then of
+      // eight neighbouring keys twice
+      const int row = (r & 19) | (r & 4) << 1 | (r & 8) >> 1;
+      const float step = fp4_step(ke);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<u32x4*>(lds + (r >> 5) * kTileBytes<D> + raw_offset<D, exact_swz<D>>(row, 32 * blk + 8 * j)) =
+            fp4_decode(k[j], step);
+    }
+    if (tid >= V0) {
+      constexpr int P = Pg::P;
+      const int u = tid - V0, t8 = u / (VU / 8), x = u % (VU / 8);
+      const int i = D == 128 ? x / 2 : x, c = D == 128 ? x % 2 : 0;
+      uint32_t se[kSteps];
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) se[s] = ve[s];
+      if (!ok.all()) {                             // wave-uniform
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (!ok.row(8 * t8 + (4 * s + e) / Pg::NB)) se[s] = (se[s] & ~(255u << 8 * e)) | 127u << 8 * e;
+      }
+#pragma unroll
+      for (int b = 0; b < P; ++b) {
+        uint32_t pr[8];                            // token r: channels + i (low half) and + 16 + i
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+          // byte r P + b of the codes; the steps of token r are NB bytes, of which c P + b is the block's
+          const uint32_t w = v[(r * P + b) / 4];
+          const int at = r * Pg::NB + b;
+          const float step = D == 128 ? fp4_step(se[r] >> (16 * c + 8 * b) & 255u) : step_of(se[at / 4], at % 4);
+          switch ((r * P + b) % 4) {
+            case 0: pr[r] = fp4_pair<0>(w, step); break;
+            case 1: pr[r] = fp4_pair<1>(w, step); break;
+            case 2: pr[r] = fp4_pair<2>(w, step); break;
+            default: pr[r] = fp4_pair<3>(w, step); break;
+          }
+        }
+        u32x4 lo, hi;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          lo[j] = __builtin_amdgcn_perm(pr[2 * j + 1], pr[2 * j], 0x05040100u);
+          hi[j] = __builtin_amdgcn_perm(pr[2 * j + 1], pr[2 * j], 0x07060302u);
+        }
+        const int ch = 32 * (c * P + b) + i;
+        char* to = lds + kKeys + ch * 128 + ((t8 ^ (ch & 7)) << 4);
+        *reinterpret_cast<u32x4*>(to) = lo;
+        *reinterpret_cast<u32x4*>(to + 16 * 128) = hi;       // 16 channels on: the same place in the swizzle
+      }
+    }
+  }
+};
+
+// Scores of keys that do not count become -inf; register r holds key 16 (r / 8) + 8 (lane / 32) + r % 8.
+__device__ __forceinline__ void mask_keys(f32x16& s, uint32_t bits) {
+  const uint32_t m = bits >> (8 * (lane_id() >> 5));
+#pragma unroll
+  for (int r = 0; r < 16; ++r) s[r] = (m >> (16 * (r >> 3) + (r & 7))) & 1 ? s[r] : -INFINITY;
+}
+
+}  // namespace
+
+template <int NP, int D>
+__global__ __launch_bounds__(kExactThreads) void fp4_rows_kernel(CacheAttentionArgs a, int mtiles) {
+  using St = CacheStage<D>;
+  constexpr int KC = D / 16, NT = D / 32, BUF = 2 * St::kKeys;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const int tid = threadIdx.x, lane = lane_id(), w = wave_uniform(tid / kWave);
+  const HeadBlock hb = head_block(blockIdx.x, a.B * a.c.Hkv, mtiles, a.causal);
+  const int bk = hb.head, mt = mtiles - 1 - hb.block;         // causal: the longest first
+  const int b = bk / a.c.Hkv, hk = bk - b * a.c.Hkv, size = 1 << a.c.page_log2;
+  const int rows = a.nq * a.group, row0 = (mt * kExactWaves + w) * 32;
+  const int m = row0 + (lane & 31), mc = min(m, rows - 1), i = mc / a.group, h = hk * a.group + (mc - i * a.group);
+  const int limit = cached_keys(a, b), start = first_query(a, b, limit);
+  const int pos = start + i;                                  // of this lane's row
+  const int pos_first = start + min(row0, rows - 1) / a.group, pos_last = start + min(row0 + 31, rows - 1) / a.group;
+  const int kend = a.causal ? min(limit, start + min((mt + 1) * kExactWaves * 32 - 1, rows - 1) / a.group + 1) : limit;
+  const int stages = kend > 0 ? (kend + 63) / 64 : 0;
+
+  TileAddr<D> at;
+  at.init(smem);
+  uint32_t va[2][2];                               // this lane's part of the values: 32 keys i, half u
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+      va[t][u] = lds_addr(smem) + St::kKeys + (lane & 31) * 128 + (((4 * t + 2 * u + (lane >> 5)) ^ (lane & 7)) << 4);
+  FwdRow<NP, D> row[1];
+  load_operand<NP, D>(a.q.p + b * a.q.sb + h * a.q.sh + i * a.q.sn, m < rows, row[0].qf);
+  row[0].init();
+
+  auto pages = [&](int k0, const char* (&pg)[2]) {
+#pragma unroll
+    for (int x = 0; x < 2; ++x) pg[x] = k0 + 32 * x < kend ? fp4_page(a.c, b, hk, k0 + 32 * x) : nullptr;
+  };
+  // the keys of a stage that count for some row
+  auto counted = [&](int k0, const char* const (&pg)[2]) {
+    return RowBits<64>{__ballot(k0 + lane < kend && (lane < 32 ? pg[0] : pg[1]) != nullptr)};
+  };
+  St st;
+  RowBits<64> ok{};
+  const char* pg[2] = {nullptr, nullptr};
+  if (stages > 0) {
+    pages(0, pg);
+    st.load(pg, 0, size, tid);
+    ok = counted(0, pg);
+    st.store(smem, ok, tid);
+    pages(64, pg);
+  }
+  __syncthreads();
+  auto stage = [&](int n, auto B) {
+    constexpr int kbuf = B * BUF;
+    const bool more = n + 1 < stages;
+    RowBits<64> next{};
+    if (more) {
+      st.load(pg, 64 * (n + 1), size, tid);
+      next = counted(64 * (n + 1), pg);
+      pages(64 * (n + 2), pg);                     // a stage ahead: the loads do not wait for the table
+    }
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const uint32_t kb = ok.tile(x);
+      const int k0 = 64 * n + 32 * x;
+      if (kb == 0 || (a.causal && k0 > pos_last)) continue;   // no key counts for the wave
+      f32x16 s[1] = {splat16(0.0f)};
+#pragma unroll
+      for (int c = 0; c < KC; ++c) {
+        const u32x4 k = at.row(kbuf + x * kTileBytes<D>, c);
+#pragma unroll
+        for (int q = NP - 1; q >= 0; --q) s[0] = mfma16(k, row[0].qf[q][c], s[0]);
+      }
+      const uint32_t bits = a.causal ? kb & low_bits(pos - k0 + 1) : kb;
+      if (kb != ~0u || (a.causal && k0 + 31 > pos_first)) mask_keys(s[0], bits);
+      const float mul[1] = {a.scale_log2}, add[1] = {0.0f};
+      Packed<NP> pw[1];
+      tile_weights<NP, D, 1>(row, s, mul, add, pw);
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const u32x4 v = *(const __attribute__((address_space(3))) u32x4*)(lds_ptr)(va[x][u] + kbuf + t * 32 * 128);
+#pragma unroll
+          for (int q = NP - 1; q >= 0; --q) row[0].o[t] = mfma16(v, pw[0].w[q][u], row[0].o[t]);
+        }
+    }
+    if (more) {
+      ok = next;
+      st.store(smem + (1 - B) * BUF, ok, tid);
+    }
+    __syncthreads();
+  };
+  for (int n = 0; n < stages; n += 2) {
+    stage(n, std::integral_constant<int, 0>{});
+    if (n + 1 < stages) stage(n + 1, std::integral_constant<int, 1>{});
+  }
+  const float den = halves_sum(row[0].sum);
+  store_rows<NP, D>(row[0].o, den > 0.0f ? 1.0f / den : 0.0f, a.out.p + b * a.out.sb + h * a.out.sh + i * a.out.sn,
+                    m < rows);
+  if (a.lse != nullptr && lane < 32 && m < rows)
+    a.lse[((long long)b * a.H + h) * a.nq + i] = den > 0.0f ? (log2f(den) + row[0].ref) * kLn2 : -INFINITY;
+}
+
+CachePlan cache_plan(int B, int Hkv, long long rows, int cap, int d) {
+  CachePlan p{};
+  p.splits = 1;
+  p.mtiles = (int)((rows + 127) / 128);
+  return p;
+}
+
+template <int NP, int D>
+static hipError_t attention_case(const CacheAttentionArgs& a, const CachePlan& plan, void* ws, hipStream_t stream) {
+  constexpr size_t smem = 4 * CacheStage<D>::kKeys;
+  auto kernel = fp4_rows_kernel<NP, D>;
+  const hipError_t e = allow_lds(kernel, smem);
+  if (e != hipSuccess) return e;
+  kernel<<<(unsigned)((long long)a.B * a.c.Hkv * plan.mtiles), kExactThreads, smem, stream>>>(a, plan.mtiles);
+  return hipGetLastError();
+}
+
+hipError_t launch_cache_attention(const CacheAttentionArgs& a, int d, int dtype, const CachePlan& plan, void* ws,
+                                  hipStream_t stream) {
+  auto width = [&](auto np) {
+    constexpr int NP = decltype(np)::value;
+    if (d == 32) return attention_case<NP, 32>(a, plan, ws, stream);
+    if (d == 64) return attention_case<NP, 64>(a, plan, ws, stream);
+    return attention_case<NP, 128>(a, plan, ws, stream);
+  };
+  return dtype == BF16 ? width(std::integral_constant<int, 1>{}) : width(std::integral_constant<int, 3>{});
+}
+
+}  // namespace mra

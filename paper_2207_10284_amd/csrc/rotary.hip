@@ -1,0 +1,405 @@
+// Rotary positions and head norms, forward and gradients (mra_layer.h).
+//
+// Bound by memory: an element is read and written once (backward with a norm: two read, one
+// written) for some ten operations. What is left to do is to keep the angles
+// cheap, a float64 product and a sine and cosine each: a workgroup takes a tile of
+// tokens with all their heads, makes the tile's sines and cosines once in LDS, and
+// its rows read them there.
+//
+// A row is shared by D / 16 lanes. A lane holds two chunks of eight elements such that
+// the eight pairs within them are its own: chunks i and rot/2 + i (half), or
+// two neighbours (interleaved); norms are sums over the row's lanes, and nothing else moves between
+// lanes. Where a row's lanes are fewer than a cache line's, rows that lie next to each other
+// are taken next to each other (head_fast).
+#include "common.h"
+#include "layer_kernels.h"
+#include "tile_ops.h"
+
+namespace mra {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kMaxTile = 16;                       // tokens of a tile
+
+// Eight consecutive elements.
+template <int DT>
+struct Chunk {
+  static constexpr int kBytes = DT == BF16 ? 16 : 32;
+  u32x4 raw[DT == BF16 ? 1 : 2];
+
+  __device__ __forceinline__ void load(const char* p) {
+#pragma unroll
+    for (int i = 0; i < (DT == BF16 ? 1 : 2); ++i) raw[i] = reinterpret_cast<const u32x4*>(p)[i];
+  }
+  __device__ __forceinline__ void get(float* f) const {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if constexpr (DT == BF16)
+        f[e] = e % 2 ? __uint_as_float(raw[0][e / 2] & 0xffff0000u) : __uint_as_float(raw[0][e / 2] << 16);
+      else
+        f[e] = __uint_as_float(raw[e / 4][e % 4]);
+    }
+  }
+};
+
+template <int DT>
+__device__ __forceinline__ void store_chunk(char* p, const float* f) {
+  if constexpr (DT == BF16) {
+    u32x4 r;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      bf16x2 b;
+      b[0] = (__bf16)f[2 * e];
+      b[1] = (__bf16)f[2 * e + 1];
+      r[e] = __builtin_bit_cast(uint32_t, b);
+    }
+    *reinterpret_cast<u32x4*>(p) = r;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      reinterpret_cast<f32x4*>(p)[i] = f32x4{f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]};
+  }
+}
+
+// Sum over the L lanes of a row.
+template <int L>
+__device__ __forceinline__ float row_sum(float v) {
+#pragma unroll
+  for (int s = 1; s < L; s *= 2) v += __shfl_xor(v, s);
+  return v;
+}
+
+// The pair elements of v (16 elements of a lane) turned by (cos, sin), sin's sign times `sign`.
+template <bool INTER>
+__device__ __forceinline__ void turn(float (&v)[16], const float2 (&cs)[8], float sign) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    float &a = INTER ? v[2 * j] : v[j], &b = INTER ? v[2 * j + 1] : v[8 + j];
+    const float c = cs[j].x, s = sign * cs[j].y, x = a, y = b;
+    a = x * c - y * s;
+    b = y * c + x * s;
+  }
+}
+
+// What the rows of a workgroup's tile share.
+template <int D>
+struct Tile {
+  static constexpr int L = D / 16, ROWS = kThreads / L;
+  int c, row;                             // this lane's part of a row, and its row among ROWS
+  int pairs;                              // lanes of a row that hold pairs
+  int e0, e1;                             // the elements of the lane's two chunks
+
+  __device__ __forceinline__ void init(int rot, bool inter) {
+    c = threadIdx.x % L;
+    row = threadIdx.x / L;
+    pairs = rot / 16;
+    e0 = inter || c >= pairs ? 16 * c : 8 * c;
+    e1 = inter || c >= pairs ? 16 * c + 8 : rot / 2 + 8 * c;
+  }
+};
+
+// cos and sin (times the magnitude) of the tile's tokens and frequencies, and each token's
+// batch and place.
+__device__ __forceinline__ void fill_angles(const RotaryArgs& a, long long first, int tokens, float2* cs, int2* at) {
+  const int half = a.rot / 2;
+  if ((int)threadIdx.x < tokens) {
+    const long long t = first + threadIdx.x;
+    const long long b = t / a.n;
+    at[threadIdx.x] = int2{(int)b, (int)(t - b * a.n)};
+  }
+  if (half == 0) return;
+  // half is a multiple of eight, at most 64, not always a power of two
+  for (int i = threadIdx.x; i < tokens * half; i += kThreads) {
+    const int t = i / half, f = i - t * half;
+    const long long g = first + t, b = g / a.n;
+    const int n = (int)(g - b * a.n);
+    const int pos = a.positions == nullptr ? n : a.positions[b * a.positions_stride + n];
+    double turns = (double)pos * (a.freqs[f] * 0.15915494309189535);
+    turns -= rint(turns);
+    float s, c;
+    sincospif(2.0f * (float)turns, &s, &c);
+    cs[i] = float2{c * a.magnitude, s * a.magnitude};
+  }
+}
+
+template <int D>
+__device__ __forceinline__ void read_angles(const float2* cs, int token, int half, int c, float2 (&out)[8]) {
+  const f32x4* p = reinterpret_cast<const f32x4*>(cs + token * half + 8 * c);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const f32x4 v = p[j];
+    out[2 * j] = float2{v[0], v[1]};
+    out[2 * j + 1] = float2{v[2], v[3]};
+  }
+}
+
+// Row r of a side's tile: its token and head.
+__device__ __forceinline__ int2 row_of(const RotarySide& s, int r, int tokens) {
+  if (s.head_fast) {
+    const int t = r / s.heads;
+    return int2{t, r - t * s.heads};
+  }
+  const int h = r / tokens;
+  return int2{r - h * tokens, h};
+}
+
+__device__ __forceinline__ long long row_offset(const Rows& r, const int2& at, int h) {
+  return at.x * r.sb + h * r.sh + at.y * r.sn;
+}
+
+template <int DT, int D>
+__device__ __forceinline__ void load_weight(const RotaryArgs& a, const void* w, int e0, int e1, float (&f)[16]) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int e = i < 8 ? e0 + i : e1 + i - 8;
+    f[i] = a.weight_bf16 ? bf16_to_f32(static_cast<const uint16_t*>(w)[e]) : static_cast<const float*>(w)[e];
+  }
+}
+
+}  // namespace
+
+template <int DT, int D, bool INTER>
+__global__ __launch_bounds__(kThreads) void rotary_forward_kernel(RotaryArgs a, int tile) {
+  using T = Tile<D>;
+  constexpr int E = DT == BF16 ? 2 : 4;
+  constexpr int U = 2;                             // rows of a lane in flight
+  __shared__ __attribute__((aligned(16))) float2 cs[kMaxTile * (D / 2)];
+  __shared__ int2 at[kMaxTile];
+  T t;
+  t.init(a.rot, INTER);
+  const long long first = (long long)blockIdx.x * tile;
+  const int tokens = (int)min((long long)tile, a.tokens - first), half = a.rot / 2;
+  fill_angles(a, first, tokens, cs, at);
+  __syncthreads();
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    const RotarySide& s = a.side[x];
+    const int rows = tokens * s.heads;
+    if (rows == 0) continue;
+    float w[16];
+    if (s.w != nullptr) load_weight<DT, D>(a, s.w, t.e0, t.e1, w);
+    for (int r0 = t.row; r0 < rows; r0 += U * T::ROWS) {
+      Chunk<DT> in[U][2];
+      long long to[U];
+      int token[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int2 rh = row_of(s, min(r0 + u * T::ROWS, rows - 1), tokens);
+        const int2 bi = at[rh.x];
+        const char* p = s.x.p + row_offset(s.x, bi, rh.y);
+        in[u][0].load(p + t.e0 * E);
+        in[u][1].load(p + t.e1 * E);
+        to[u] = row_offset(s.y, bi, rh.y);
+        token[u] = rh.x;
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        float v[16];
+        in[u][0].get(v);
+        in[u][1].get(v + 8);
+        if (s.w != nullptr) {
+          float sum = 0.0f;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) sum = fmaf(v[i], v[i], sum);
+          const float inv = 1.0f / sqrtf(row_sum<T::L>(sum) * (1.0f / D) + a.eps);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) v[i] = v[i] * inv * w[i];
+        }
+        if (t.c < t.pairs) {
+          float2 c[8];
+          read_angles<D>(cs, token[u], half, t.c, c);
+          turn<INTER>(v, c, 1.0f);
+        }
+        if (u == 0 || r0 + u * T::ROWS < rows) {
+          char* p = s.y.p + to[u];
+          store_chunk<DT>(p + t.e0 * E, v);
+          store_chunk<DT>(p + t.e1 * E, v + 8);
+        }
+      }
+    }
+  }
+}
+
+// Each workgroup takes every gridDim.x-th tile and leaves one row of sums of g y per side.
+template <int DT, int D, bool INTER>
+__global__ __launch_bounds__(kThreads) void rotary_backward_kernel(RotaryArgs a, int tile) {
+  using T = Tile<D>;
+  constexpr int E = DT == BF16 ? 2 : 4;
+  constexpr int U = DT == BF16 ? 2 : 1;
+  __shared__ __attribute__((aligned(16))) float2 cs[kMaxTile * (D / 2)];
+  __shared__ int2 at[kMaxTile];
+  __shared__ __attribute__((aligned(16))) float sums[kThreads * 16];
+  T t;
+  t.init(a.rot, INTER);
+  const int half = a.rot / 2;
+  float dw[2][16];
+#pragma unroll
+  for (int x = 0; x < 2; ++x)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) dw[x][i] = 0.0f;
+  for (long long first = (long long)blockIdx.x * tile; first < a.tokens; first += (long long)gridDim.x * tile) {
+    const int tokens = (int)min((long long)tile, a.tokens - first);
+    __syncthreads();                               // the last tile's angles have been read
+    fill_angles(a, first, tokens, cs, at);
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const RotarySide& s = a.side[x];
+      const int rows = tokens * s.heads;
+      if (rows == 0) continue;
+      const bool norm = s.w != nullptr;
+      float w[16];
+      if (norm) load_weight<DT, D>(a, s.w, t.e0, t.e1, w);
+      for (int r0 = t.row; r0 < rows; r0 += U * T::ROWS) {
+        Chunk<DT> gr[U][2], in[U][2];
+        long long to[U];
+        int token[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int2 rh = row_of(s, min(r0 + u * T::ROWS, rows - 1), tokens);
+          const int2 bi = at[rh.x];
+          const char* p = s.g.p + row_offset(s.g, bi, rh.y);
+          gr[u][0].load(p + t.e0 * E);
+          gr[u][1].load(p + t.e1 * E);
+          if (norm) {
+            p = s.x.p + row_offset(s.x, bi, rh.y);
+            in[u][0].load(p + t.e0 * E);
+            in[u][1].load(p + t.e1 * E);
+          }
+          to[u] = row_offset(s.y, bi, rh.y);
+          token[u] = rh.x;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const bool on = u == 0 || r0 + u * T::ROWS < rows;
+          float g[16];
+          gr[u][0].get(g);
+          gr[u][1].get(g + 8);
+          if (t.c < t.pairs) {
+            float2 c[8];
+            read_angles<D>(cs, token[u], half, t.c, c);
+            turn<INTER>(g, c, -1.0f);
+          }
+          if (norm) {
+            float v[16], sum = 0.0f, dot = 0.0f;
+            in[u][0].get(v);
+            in[u][1].get(v + 8);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sum = fmaf(v[i], v[i], sum);
+            const float inv = 1.0f / sqrtf(row_sum<T::L>(sum) * (1.0f / D) + a.eps);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              v[i] *= inv;
+              const float gy = g[i] * v[i];
+              dw[x][i] += on ? gy : 0.0f;
+              dot = fmaf(gy, w[i], dot);
+            }
+            dot = row_sum<T::L>(dot) * (1.0f / D);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) g[i] = inv * (g[i] * w[i] - v[i] * dot);
+          }
+          if (on) {
+            char* p = s.y.p + to[u];
+            store_chunk<DT>(p + t.e0 * E, g);
+            store_chunk<DT>(p + t.e1 * E, g + 8);
+          }
+        }
+      }
+    }
+  }
+  if (a.part == nullptr) return;
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    if (a.side[x].w == nullptr) continue;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sums[t.row * D + (i < 8 ? t.e0 + i : t.e1 + i - 8)] = dw[x][i];
+    __syncthreads();
+    if ((int)threadIdx.x < D) {
+      float v = 0.0f;
+      for (int r = 0; r < T::ROWS; ++r) v += sums[r * D + threadIdx.x];
+      a.part[((long long)blockIdx.x * 2 + x) * D + threadIdx.x] = v;
+    }
+  }
+}
+
+// The workgroups' sums in double, 32 threads across columns and 32 across the sums.
+constexpr int kSumThreads = 1024;
+__global__ __launch_bounds__(kSumThreads) void rotary_weight_kernel(const float* __restrict__ part, int groups, int D,
+                                                                    void* dq_weight, void* dk_weight, int bf16) {
+  __shared__ double sums[32][33];
+  const int x = blockIdx.y, i = threadIdx.x % 32, g = threadIdx.x / 32, e = blockIdx.x * 32 + i;
+  void* to = x == 0 ? dq_weight : dk_weight;
+  if (to == nullptr) return;
+  double v = 0.0;
+  for (int r = g; r < groups; r += 32) v += part[((long long)r * 2 + x) * D + e];
+  sums[g][i] = v;
+  __syncthreads();
+  if (g != 0) return;
+  for (int r = 1; r < 32; ++r) v += sums[r][i];
+  if (bf16) {
+    const float f = (float)v;
+    // a float32 on the way is at most 2^-24 of the value off, which moves only values that near a tie
+    static_cast<__bf16*>(to)[e] = (__bf16)f;
+  } else {
+    static_cast<float*>(to)[e] = (float)v;
+  }
+}
+
+// Tokens of a tile: 16, fewer while that leaves CUs without a workgroup.
+static int rotary_tile(long long tokens) {
+  int tile = kMaxTile;
+  while (tile > 1 && tokens < (long long)tile * 2 * kCus) tile /= 2;
+  return tile;
+}
+
+int rotary_backward_groups(long long tokens) {
+  const long long tiles = (tokens + rotary_tile(tokens) - 1) / rotary_tile(tokens);
+  return (int)(tiles < 4 * kCus ? tiles : 4 * kCus);
+}
+
+template <class F>
+static hipError_t rotary_variant(int d, int dtype, int interleaved, F run) {
+  auto inter = [&](auto dt, auto dd) {
+    return interleaved ? run(dt, dd, std::true_type{}) : run(dt, dd, std::false_type{});
+  };
+  auto width = [&](auto dt) {
+    if (d == 32) return inter(dt, std::integral_constant<int, 32>{});
+    if (d == 64) return inter(dt, std::integral_constant<int, 64>{});
+    return inter(dt, std::integral_constant<int, 128>{});
+  };
+  return dtype == BF16 ? width(std::integral_constant<int, BF16>{}) : width(std::integral_constant<int, F32>{});
+}
+
+hipError_t launch_rotary_forward(const RotaryArgs& a, int d, int dtype, int interleaved, hipStream_t stream) {
+  const int tile = rotary_tile(a.tokens);
+  return rotary_variant(d, dtype, interleaved, [&](auto dt, auto dd, auto inter) {
+    rotary_forward_kernel<dt.value, dd.value, inter.value>
+        <<<(unsigned)((a.tokens + tile - 1) / tile), kThreads, 0, stream>>>(a, tile);
+    return hipGetLastError();
+  });
+}
+
+hipError_t launch_rotary_backward(const RotaryArgs& a, int d, int dtype, int interleaved, void* dq_weight,
+                                  void* dk_weight, hipStream_t stream) {
+  const int tile = rotary_tile(a.tokens);
+  const bool weights = dq_weight != nullptr || dk_weight != nullptr;
+  // without sums to leave, a workgroup per tile
+  const unsigned groups = weights ? (unsigned)rotary_backward_groups(a.tokens) : (unsigned)((a.tokens + tile - 1) / tile);
+  if (a.tokens > 0) {
+    const hipError_t e = rotary_variant(d, dtype, interleaved, [&](auto dt, auto dd, auto inter) {
+      rotary_backward_kernel<dt.value, dd.value, inter.value><<<groups, kThreads, 0, stream>>>(a, tile);
+      return hipGetLastError();
+    });
+    if (e != hipSuccess) return e;
+  }
+  if (weights) {
+    rotary_weight_kernel<<<dim3(d / 32, 2), kSumThreads, 0, stream>>>(a.part, a.tokens > 0 ? (int)groups : 0, d, dq_weight,
+                                                                   dk_weight, a.weight_bf16);
+    return hipGetLastError();
+  }
+  return hipSuccess;
+}
+
+}  // namespace mra

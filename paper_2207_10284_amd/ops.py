@@ -19,6 +19,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import math
 import os
 import warnings
 
@@ -829,3 +830,255 @@ def exact_attention(q, k, v, *, scale=None, causal: bool = False, lengths=None, 
             and not torch.compiler.is_compiling()):
         return bind_exact().exact_attention(q, k, v, scale, causal, lengths, key_mask, q_start, bias, buckets)
     return ExactAttention.apply(q, k, v, bias, buckets, lengths, key_mask, q_start, scale, causal)
+
+
+# ---------------------------------------------------------------------------
+# Rotary positions, head norms and the 4-bit cache (include/mra_layer.h)
+LAYER_LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libmra_layer.so")
+
+# name -> (restype, argtypes); mirrors include/mra_layer.h
+LAYER_SIGNATURES = {
+    "mra_rotary_forward": (_I, [_P] * 6),
+    "mra_rotary_backward_workspace_bytes": (_Z, [_P]),
+    "mra_rotary_backward": (_I, [_P] * 10 + [_Z, _P]),
+    "mra_fp4_page_bytes": (_Z, [_I, _I]),
+    "mra_fp4_cache_write": (_I, [_P, _P, _P, _I, _I, _P, _P, _P]),
+    "mra_fp4_cache_read": (_I, [_P, _P, _P, _I, _I, _P, _P, _P]),
+    "mra_fp4_attention_workspace_bytes": (_Z, [_P, _P]),
+    "mra_fp4_attention": (_I, [_P] * 6 + [_Z, _P]),
+    "mra_layer_last_hip_error": (_I, []),
+}
+
+_layer_lib = None
+_layer_native = None    # csrc/layer_binding.cpp, bound to _layer_lib by the first call that needs it
+
+
+class _LayerStatus:
+    """What MraError asks of a library: the shared status texts, this library's HIP error."""
+
+    def mra_status_str(self, status):
+        return load().mra_status_str(status)
+
+    def mra_last_hip_error(self):
+        return load_layer().mra_layer_last_hip_error()
+
+
+def load_layer(path: str = LAYER_LIB_PATH):
+    """Open libmra_layer.so once and declare its signatures. Raises if it is missing."""
+    global _layer_lib
+    if _layer_lib is None:
+        if not os.path.exists(path):
+            raise RuntimeError(f"{path} is not built; run `python -m paper_2207_10284_amd.build` "
+                               "(hipcc, gfx950) first")
+        lib = ctypes.CDLL(path)
+        for name, (res, args) in LAYER_SIGNATURES.items():
+            fn = getattr(lib, name)
+            fn.restype, fn.argtypes = res, args
+        _layer_lib = lib
+    return _layer_lib
+
+
+def bind_layer():
+    """The native binding of these calls (as ``bind``)."""
+    global _layer_native
+    if _layer_native is None:
+        lib = load_layer()
+        try:
+            from paper_2207_10284_amd import _binding_layer
+        except ImportError as e:
+            raise RuntimeError(f"the torch binding is not built ({e}); run `python -m paper_2207_10284_amd.build` "
+                               "first") from e
+        _binding_layer.bind({name: ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in LAYER_SIGNATURES},
+                            lambda fn, status: MraError(fn, status, _LayerStatus()))
+        _layer_native = _binding_layer
+    return _layer_native
+
+
+def rotary_frequencies(rotary_dim: int, base: float = 10000.0, *, scaling: str | None = None, factor: float = 1.0,
+                       original: int | None = None, device="cuda"):
+    """The frequencies of rotary positions, radians a position: float64
+    [rotary_dim / 2], base^(-2i / rotary_dim). ``scaling`` stretches them to contexts
+    ``factor`` times as long (arXiv 2306.15595, 2309.00071): "linear" divides all by the factor; "ntk" raises
+    the base so that the first stays and the last is divided; "by_parts" divides those that
+    turn at most once within the ``original`` context, keeps those that turn 32 times or more, and mixes
+    the two in between, linearly in the turns (with it belongs ``rotary_magnitude``). Any other
+    float64 tensor serves as well."""
+    rotary_dim, base, factor = int(rotary_dim), float(base), float(factor)
+    if rotary_dim < 0 or rotary_dim % 16:
+        raise ValueError("rotary_dim must be a multiple of 16")
+    if not (1.0 < base < math.inf and 0.0 < factor < math.inf):
+        raise ValueError("base must be above 1 and factor above 0")
+    if scaling not in (None, "linear", "ntk", "by_parts"):
+        raise ValueError(f"unknown scaling {scaling!r}")
+    if scaling == "by_parts" and (original is None or original <= 0):
+        raise ValueError("by_parts needs the original context")
+    if scaling == "ntk":
+        base *= factor ** (rotary_dim / (rotary_dim - 2))
+    f = base ** (-torch.arange(0, rotary_dim, 2, dtype=torch.float64) / max(rotary_dim, 1))
+    if scaling == "linear":
+        f = f / factor
+    elif scaling == "by_parts":
+        keep = ((original / (2 * math.pi) * f - 1) / 31).clamp(0, 1)
+        f = keep * f + (1 - keep) * f / factor
+    return f.to(device)
+
+
+def rotary_magnitude(factor: float) -> float:
+    """The magnitude that belongs to "by_parts" frequencies: 0.1 ln(factor) + 1 (1 up to factor 1)."""
+    return 0.1 * math.log(factor) + 1.0 if factor > 1 else 1.0
+
+
+def rotary_forward(q, k=None, freqs=None, *, positions=None, interleaved: bool = False, magnitude: float = 1.0,
+                   q_weight=None, k_weight=None, eps: float = 1e-6, q_out=None, k_out=None):
+    """Rotary positions of queries and keys, and before them their norms: (q', k'),
+    k' None without k.
+
+    q: [B, H, n, d], k: [B, H_kv, n, d] as in ``exact_attention``. ``freqs`` (float64
+    [r / 2], r at most d: ``rotary_frequencies``) turns the first r elements of a row, in pairs i and i + r/2
+    (``interleaved``: 2i and 2i + 1), by position times frequency and times ``magnitude``;
+    none: no rotation. ``positions``: int32 [n] or [B, n], 0 to n - 1 if not given. With
+    ``q_weight`` or ``k_weight`` ([d], float32 or q's dtype) a row x is x / sqrt(mean(x^2) + eps) times the weight
+    before it is turned. ``q_out`` may be q and ``k_out`` k: changed in place; they
+    overlap no other argument."""
+    return bind_layer().rotary_forward(q, k, freqs, positions, interleaved, magnitude, q_weight, k_weight, eps,
+                                       _result(q, q_out), k_out if k is None else _result(k, k_out))
+
+
+def rotary_backward(dq_out, dk_out, q=None, k=None, freqs=None, *, positions=None, interleaved: bool = False,
+                    magnitude: float = 1.0, q_weight=None, k_weight=None, eps: float = 1e-6, dq=None, dk=None):
+    """Gradients (dq, dk, dq_weight, dk_weight) of one ``rotary_forward`` with the
+    same arguments, for those of its results; one of ``dq_out`` and ``dk_out`` may be None, and so are
+    then its gradients. q and k are needed with their weights only. ``dq`` may be ``dq_out`` and
+    ``dk`` ``dk_out``. The same bits every time."""
+    return bind_layer().rotary_backward(dq_out, dk_out, q, k, freqs, positions, interleaved, magnitude, q_weight,
+                                        k_weight, eps, dq, dk)
+
+
+_TURNED_ONCE = "the gradients of rotary are not differentiable"
+
+
+class _TurnedOnce(torch.autograd.Function):
+    """Gradients (the first four) as functions of what follows, whose derivatives raise."""
+
+    @staticmethod
+    def forward(ctx, *tensors):
+        return tuple(None if t is None else t.detach() for t in tensors[:4])
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError(f"{_TURNED_ONCE}: trying to differentiate twice")
+
+
+class Rotary(torch.autograd.Function):
+    """``rotary_forward`` as a differentiable op of q, k and the weights."""
+
+    @staticmethod
+    def forward(ctx, q, k, q_weight, k_weight, freqs, positions, interleaved, magnitude, eps):
+        yq, yk = rotary_forward(q, k, freqs, positions=positions, interleaved=interleaved, magnitude=magnitude,
+                                q_weight=q_weight, k_weight=k_weight, eps=eps)
+        ctx.set_materialize_grads(False)
+        ctx.save_for_backward(q if q_weight is not None else None, k if k_weight is not None else None, q_weight,
+                              k_weight, freqs, positions)
+        ctx.args = dict(interleaved=interleaved, magnitude=magnitude, eps=eps)
+        return yq, yk
+
+    @staticmethod
+    def backward(ctx, gq, gk):
+        if not torch.compiler.is_compiling() and torch.cuda.is_current_stream_capturing():
+            bind_layer().check_capture()
+        if gq is None and gk is None:
+            return (None,) * 9
+        q, k, q_weight, k_weight, freqs, positions = ctx.saved_tensors
+        with torch.no_grad():
+            rows = [None if g is None else g if _dense_rows(g) else g.contiguous() for g in (gq, gk)]
+            grads = rotary_backward(*rows, q, k, freqs, positions=positions, q_weight=q_weight, k_weight=k_weight,
+                                    **ctx.args)
+        if torch.is_grad_enabled():
+            if any(g is not None and g.requires_grad for g in (gq, gk)):
+                grads = _TurnedOnce.apply(*grads, q, k, q_weight, k_weight, gq, gk)
+            else:
+                warnings.warn(f"{_TURNED_ONCE}: these are constants of the graph")
+        return (*grads, None, None, None, None, None)
+
+
+def rotary(q, k=None, freqs=None, *, positions=None, interleaved: bool = False, magnitude: float = 1.0, q_weight=None,
+           k_weight=None, eps: float = 1e-6):
+    """Differentiable rotary positions and head norms (arguments and result as
+    ``rotary_forward``), with gradients of q, k and the weights, which are not differentiable
+    themselves, and captured into graphs, as those of ``exact_attention``. Without a weight nothing of
+    q and k is kept for the backward."""
+    tensors = (q, k, freqs, positions, q_weight, k_weight)
+    if (all(t is None or type(t) in _PLAIN for t in tensors)
+            and not torch._C._are_functorch_transforms_active() and torch._C._get_tracing_state() is None
+            and not torch.compiler.is_compiling()):
+        return bind_layer().rotary(q, k, freqs, positions, interleaved, magnitude, q_weight, k_weight, eps)
+    return Rotary.apply(q, k, q_weight, k_weight, freqs, positions, interleaved, magnitude, eps)
+
+
+class Fp4Cache:
+    """A paged cache of keys and values in 4 bits: ``data`` (uint8 [pages, H_kv,
+    page bytes] on the device, include/mra_layer.h has its layout), ``page_size`` tokens a page, head width ``d``.
+    Pages may be copied, moved and shared whole."""
+    __slots__ = ("data", "page_size", "d")
+
+    def __init__(self, data, page_size: int, d: int):
+        page_size, d = int(page_size), int(d)
+        if page_size < 0 or d < 0 or max(page_size, d) >= 1 << 31 or not (need := fp4_page_bytes(page_size, d)):
+            raise ValueError("page_size must be 32, 64, .. 1024 and d 32, 64 or 128")
+        if data.dtype != torch.uint8 or data.dim() != 3 or data.shape[2] != need or not data.is_contiguous():
+            raise ValueError(f"data must be a contiguous uint8 tensor [pages, H_kv, {need}]")
+        self.data, self.page_size, self.d = data, page_size, d
+
+    def _args(self):
+        return self.data, self.page_size, self.d
+
+
+def fp4_page_bytes(page_size: int, d: int) -> int:
+    """Bytes of one page of one head: 17/32 byte a value (0: sizes that are not supported)."""
+    return int(load_layer().mra_fp4_page_bytes(page_size, d))
+
+
+def fp4_cache(pages: int, kv_heads: int, page_size: int, d: int, device="cuda") -> Fp4Cache:
+    """An empty cache of ``pages`` pages (all values 0). page_size: a power of two from 32 to 1024."""
+    if page_size < 0 or d < 0 or max(page_size, d) >= 1 << 31 or not (need := fp4_page_bytes(page_size, d)):
+        raise ValueError("page_size must be 32, 64, .. 1024 and d 32, 64 or 128")
+    return Fp4Cache(torch.zeros(pages, kv_heads, need, dtype=torch.uint8, device=device), page_size, d)
+
+
+def fp4_cache_write(cache: Fp4Cache, k, v, table, *, starts=None, counts=None) -> None:
+    """Writes the first ``counts[b]`` (all if not given) tokens of sequence b to its
+    places from ``starts[b]`` (0) on.
+
+    k, v: [B, H_kv, n, d], float32 or bfloat16, any strides with dense 16-byte aligned
+    rows. ``table`` (int32 [B, m]): the pages of each sequence; place t is in its page
+    t // page_size. ``starts``, ``counts``: int32 [B]. Places beyond the table or in an entry that is no page (-1) are not
+    written. 32 consecutive channels share a power-of-two step, the smallest with
+    their largest magnitude at most 7 steps; a value is held as the nearest of 0, 1/2, 1, 3/2, 2, 3, 4
+    and 6 steps, ties to the even one in this order. Only the written tokens' bytes change. Two sequences that write to one place leave
+    either's values, or a mix."""
+    bind_layer().cache_write(*cache._args(), k, v, table, starts, counts)
+
+
+def fp4_cache_read(cache: Fp4Cache, table, n: int, *, starts=None, counts=None, dtype=torch.bfloat16, k_out=None,
+                   v_out=None):
+    """The values held for the first ``counts[b]`` (n) tokens from place ``starts[b]``
+    (0) on: (k, v), [B, H_kv, n, d] of ``dtype`` (float32 or bfloat16: exact in either); 0
+    behind them and where there is no page. Arguments as in ``fp4_cache_write``."""
+    return bind_layer().cache_read(*cache._args(), table, n, starts, counts, dtype, k_out, v_out)
+
+
+def fp4_attention_workspace_bytes(q, cache: Fp4Cache, table, lengths) -> int:
+    """Workspace of ``fp4_cache_attention`` for these arguments (0: none)."""
+    return int(bind_layer().attention_workspace(*cache._args(), q, table, lengths))
+
+
+def fp4_cache_attention(q, cache: Fp4Cache, table, lengths, *, scale=None, causal: bool = False, q_start=None,
+                        out=None, lse_out=None, workspace=None):
+    """Softmax attention softmax(scale q k^T) v of q [B, H, n_q, d] over the first
+    ``lengths[b]`` (int32 [B]) tokens that the cache holds for each sequence; query
+    head h reads key head h // (H / H_kv). Query i stands at ``q_start[b] + i`` (int32 [B];
+    lengths[b] - n_q + i if not given) and with ``causal`` sees the tokens up to there. Tokens in an
+    entry of the table that is no page do not count; a query for which none counts gives zeros. ``scale``, ``out``, ``lse_out`` and
+    ``workspace`` as in ``exact_attention_forward``. Not differentiable."""
+    return bind_layer().attention(*cache._args(), q, table, lengths, scale, causal, q_start, _result(q, out), lse_out,
+                                  workspace)
