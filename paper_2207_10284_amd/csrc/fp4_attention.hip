@@ -245,15 +245,324 @@ __global__ __launch_bounds__(kExactThreads) void fp4_rows_kernel(CacheAttentionA
     a.lse[((long long)b * a.H + h) * a.nq + i] = den > 0.0f ? (log2f(den) + row[0].ref) * kLn2 : -INFINITY;
 }
 
+// ---- few rows
+
+constexpr int kTokenWaves = 4;
+constexpr int kTokenRows = 16;
+
+__device__ __forceinline__ f32x4 mfma4(const u32x4& a, const u32x4& b, const f32x4& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// op over the four lanes of a column (lane, lane ^ 16, lane ^ 32, lane ^ 48).
+__device__ __forceinline__ float column_max(float v) {
+  v = fmaxf(v, __shfl_xor(v, 16));
+  return fmaxf(v, __shfl_xor(v, 32));
+}
+__device__ __forceinline__ float column_sum(float v) {
+  v += __shfl_xor(v, 16);
+  return v + __shfl_xor(v, 32);
+}
+
+// 32 keys of one head as the wave's lanes hold them: lane (g, i) = (lane / 16, lane % 16) has channels
+// g D/4 .. of keys 8 (i / 4) + 4 x + i % 4 (x = 0, 1), so that register r of the scores of x is key
+// 8 g + 4 x + r of column i, and of the values entry i of keys 8 g .. 8 g + 7.
+template <int D>
+struct CacheTile {
+  using Pg = Fp4Page<D>;
+  uint32_t k[2][D / 32], ke[2], v[D / 16], ve[D / 16];
+
+  template <int N>
+  static __device__ __forceinline__ void words(const char* p, uint32_t (&w)[N]) {
+    if constexpr (N % 4 == 0) {
+#pragma unroll
+      for (int i = 0; i < N / 4; ++i) {
+        const u32x4 x = reinterpret_cast<const u32x4*>(p)[i];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[4 * i + e] = x[e];
+      }
+    } else if constexpr (N == 2) {
+      const u32x2 x = *reinterpret_cast<const u32x2*>(p);
+      w[0] = x[0];
+      w[1] = x[1];
+    } else {
+      w[0] = *reinterpret_cast<const uint32_t*>(p);
+    }
+  }
+
+  __device__ __forceinline__ void load(const char* page, int slot, int size) {
+    const int lane = lane_id(), g = lane >> 4, i = lane & 15;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const int row = slot + 8 * (i >> 2) + 4 * x + (i & 3);
+      words(page + row * (D / 2) + g * (D / 8), k[x]);
+      ke[x] = (uint8_t)page[Pg::key_steps(size) + row * Pg::NB + g * Pg::NB / 4];
+    }
+    words(page + Pg::values(size) + slot * (D / 2) + g * Pg::kTile + i * (D / 4), v);
+    words(page + Pg::value_steps(size) + (slot + 8 * g) * Pg::NB, ve);
+  }
+
+  // Steps of keys that do not count may be anything; `bits`: those of this lane's eight that do.
+  __device__ __forceinline__ void clean(uint32_t bits) {
+#pragma unroll
+    for (int w = 0; w < D / 16; ++w)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (!(bits >> (4 * w + e) / Pg::NB & 1)) ve[w] = (ve[w] & ~(255u << 8 * e)) | 127u << 8 * e;
+  }
+
+  // The A operands of the channels 32 b + 0 .. 15 and 32 b + 16 .. 31.
+  __device__ __forceinline__ void values(int b, u32x4& lo, u32x4& hi) const {
+    constexpr int P = Pg::P, NB = Pg::NB;
+    uint32_t pr[8];
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      const int at = (b / P * 8 + r) * P + b % P, es = r * NB + b;
+      const float step = fp4_step(ve[es / 4] >> 8 * (es % 4) & 255u);
+      switch (at % 4) {
+        case 0: pr[r] = fp4_pair<0>(v[at / 4], step); break;
+        case 1: pr[r] = fp4_pair<1>(v[at / 4], step); break;
+        case 2: pr[r] = fp4_pair<2>(v[at / 4], step); break;
+        default: pr[r] = fp4_pair<3>(v[at / 4], step); break;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      lo[j] = __builtin_amdgcn_perm(pr[2 * j + 1], pr[2 * j], 0x05040100u);
+      hi[j] = __builtin_amdgcn_perm(pr[2 * j + 1], pr[2 * j], 0x07060302u);
+    }
+  }
+};
+
+// The running softmax of 16 rows, a column each (as FwdRow).
+template <int NP, int D>
+struct TokenRows {
+  u32x4 qf[NP][D / 32];
+  f32x4 o[D / 16];
+  float ref, sum;
+
+  __device__ __forceinline__ void init() {
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t) o[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    ref = -INFINITY;
+    sum = 0.0f;
+  }
+
+  __device__ __forceinline__ void load_queries(const char* row, bool on) {
+    const char* p = row + (lane_id() >> 4) * (D / 4) * (NP == 1 ? 2 : 4);
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) {
+      if constexpr (NP == 1) {
+        qf[0][c] = on ? reinterpret_cast<const u32x4*>(p)[c] : u32x4{0, 0, 0, 0};
+      } else {
+        float f[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = on ? reinterpret_cast<const float*>(p)[8 * c + e] : 0.0f;
+        u32x4 pl[3];
+        split8(f, pl);
+#pragma unroll
+        for (int q = 0; q < 3; ++q) qf[q][c] = pl[q];
+      }
+    }
+  }
+
+  // weights exp2(s mul - at) of a lane's eight keys as the next operand's planes, and their sum
+  __device__ __forceinline__ float weights(const float (&s)[8], float mul, float at, u32x4 (&w)[NP]) const {
+    float p[8], t = 0.0f;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) p[r] = __builtin_amdgcn_exp2f(fmaf(s[r], mul, -at));
+    if constexpr (NP == 1) {
+      const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        bf16x2 b;
+        b[0] = (__bf16)p[2 * e];
+        b[1] = (__bf16)p[2 * e + 1];
+        w[0][e] = __builtin_bit_cast(uint32_t, b);
+        t = __builtin_amdgcn_fdot2_f32_bf16(b, ones, t, false);
+      }
+    } else {
+      split8(p, w);
+#pragma unroll
+      for (int r = 0; r < 8; ++r) t += p[r];
+    }
+    return t;
+  }
+
+  // Weights of a tile's scores; a reference that it outgrows is moved first, in all lanes of its column.
+  __device__ __forceinline__ void tile(const float (&s)[8], float mul, u32x4 (&w)[NP]) {
+    float t = weights(s, mul, ref, w);
+    if (__ballot(!(t <= kCap)) != 0) {             // also where ref is -inf
+      float mx = s[0];
+#pragma unroll
+      for (int r = 1; r < 8; ++r) mx = fmaxf(mx, s[r]);
+      mx = column_max(mx) * mul;
+      const float next = mx > ref ? mx + kMargin : ref;
+      const float f = next == ref ? 1.0f : __builtin_amdgcn_exp2f(ref - next);
+#pragma unroll
+      for (int x = 0; x < D / 16; ++x) o[x] *= f;
+      sum *= f;
+      ref = next;
+      t = weights(s, mul, ref == -INFINITY ? 0.0f : ref, w);    // no key yet: every s is -inf
+    }
+    sum += t;
+  }
+};
+
+template <int NP, int D>
+__global__ __launch_bounds__(kTokenWaves * kWave) void fp4_token_kernel(CacheAttentionArgs a, int mtiles, int splits,
+                                                                        float* __restrict__ part_o,
+                                                                        float* __restrict__ part_l) {
+  constexpr int KC = D / 32, NT = D / 16;
+  __shared__ __attribute__((aligned(16))) f32x4 merged[kTokenWaves - 1][NT][kWave];
+  __shared__ float refs[kTokenWaves][kWave], sums[kTokenWaves][kWave];
+  const int lane = lane_id(), w = wave_uniform(threadIdx.x / kWave), g4 = lane >> 4;
+  const int g = xcd_remap(blockIdx.x, gridDim.x);
+  const int sp = g % splits, mt = g / splits % mtiles, bk = g / splits / mtiles;
+  const int b = bk / a.c.Hkv, hk = bk - b * a.c.Hkv, size = 1 << a.c.page_log2;
+  const int rows = a.nq * a.group, row0 = mt * kTokenRows;
+  const int m = row0 + (lane & 15), mc = min(m, rows - 1), i = mc / a.group, h = hk * a.group + (mc - i * a.group);
+  const int limit = cached_keys(a, b), start = first_query(a, b, limit);
+  const int pos = start + i, pos_first = start + row0 / a.group;
+  const int pos_last = start + min(row0 + kTokenRows - 1, rows - 1) / a.group;
+  const int kend = a.causal ? min(limit, pos_last + 1) : limit;
+  const int tiles = kend > 0 ? (kend + 31) / 32 : 0;
+  const int t0 = (int)((long long)tiles * sp / splits), t1 = (int)((long long)tiles * (sp + 1) / splits);
+
+  TokenRows<NP, D> row;
+  row.load_queries(a.q.p + b * a.q.sb + h * a.q.sh + i * a.q.sn, m < rows);
+  row.init();
+  auto page_of = [&](int t) { return t < t1 ? fp4_page(a.c, b, hk, 32 * t) : nullptr; };
+  CacheTile<D> next;
+  int t = t0 + w;
+  const char* page = page_of(t);
+  if (page != nullptr) next.load(page, 32 * t & (size - 1), size);
+  const char* ahead = page_of(t + kTokenWaves);
+  for (; t < t1; t += kTokenWaves) {
+    CacheTile<D> tile = next;
+    const bool some = page != nullptr;
+    page = ahead;
+    if (page != nullptr) next.load(page, 32 * (t + kTokenWaves) & (size - 1), size);
+    ahead = page_of(t + 2 * kTokenWaves);
+    if (!some) continue;                           // no page: no key
+    const int k0 = 32 * t;
+    float s[8];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      f32x4 c = {0.0f, 0.0f, 0.0f, 0.0f};
+      const float step = fp4_step(tile.ke[x]);
+#pragma unroll
+      for (int n = 0; n < KC; ++n) {
+        const u32x4 k = fp4_decode(tile.k[x][n], step);
+#pragma unroll
+        for (int q = NP - 1; q >= 0; --q) c = mfma4(k, row.qf[q][n], c);
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) s[4 * x + r] = c[r];
+    }
+    if (k0 + 32 > kend || (a.causal && k0 + 31 > pos_first)) {
+      const uint32_t bits = low_bits((a.causal ? min(kend, pos + 1) : kend) - k0 - 8 * g4);
+#pragma unroll
+      for (int r = 0; r < 8; ++r) s[r] = bits >> r & 1 ? s[r] : -INFINITY;
+      if (k0 + 32 > kend) tile.clean(low_bits(kend - k0 - 8 * g4));
+    }
+    u32x4 pw[NP];
+    row.tile(s, a.scale_log2, pw);
+#pragma unroll
+    for (int n = 0; n < D / 32; ++n) {
+      u32x4 lo, hi;
+      tile.values(n, lo, hi);
+#pragma unroll
+      for (int q = NP - 1; q >= 0; --q) {
+        row.o[2 * n] = mfma4(lo, pw[q], row.o[2 * n]);
+        row.o[2 * n + 1] = mfma4(hi, pw[q], row.o[2 * n + 1]);
+      }
+    }
+  }
+  // the waves' sums relative to the largest reference, added in wave order
+  float sum = column_sum(row.sum);
+  refs[w][lane] = row.ref;
+  sums[w][lane] = sum;
+  __syncthreads();
+  float top = refs[0][lane];
+#pragma unroll
+  for (int x = 1; x < kTokenWaves; ++x) top = fmaxf(top, refs[x][lane]);
+  auto factor = [&](float ref) { return ref == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ref - top); };
+  const float f = factor(row.ref);
+#pragma unroll
+  for (int x = 0; x < NT; ++x) row.o[x] *= f;
+  if (w != 0)
+#pragma unroll
+    for (int x = 0; x < NT; ++x) merged[w - 1][x][lane] = row.o[x];
+  __syncthreads();
+  if (w != 0) return;
+  sum *= f;
+#pragma unroll
+  for (int p = 1; p < kTokenWaves; ++p) {
+    sum += sums[p][lane] * factor(refs[p][lane]);
+#pragma unroll
+    for (int x = 0; x < NT; ++x) row.o[x] += merged[p - 1][x][lane];
+  }
+  if (m >= rows) return;
+  const float inv = splits > 1 ? 1.0f : sum > 0.0f ? 1.0f / sum : 0.0f;
+  const long long pr = ((long long)sp * a.B * a.c.Hkv + bk) * rows + m;   // the partial row
+  char* to = splits > 1 ? reinterpret_cast<char*>(part_o + pr * D) : a.out.p + b * a.out.sb + h * a.out.sh + i * a.out.sn;
+#pragma unroll
+  for (int x = 0; x < NT; ++x) {
+    const float z[4] = {row.o[x][0] * inv, row.o[x][1] * inv, row.o[x][2] * inv, row.o[x][3] * inv};
+    const int c = 16 * x + 4 * g4;
+    if (NP == 1 && splits == 1) store4<1>(to + 2 * c, z);
+    else store4<3>(to + 4 * c, z);
+  }
+  if (g4 != 0) return;
+  if (splits > 1) {
+    part_l[2 * pr] = top;
+    part_l[2 * pr + 1] = sum;
+  } else if (a.lse != nullptr) {
+    a.lse[((long long)b * a.H + h) * a.nq + i] = sum > 0.0f ? (log2f(sum) + top) * kLn2 : -INFINITY;
+  }
+}
+
+// The token kernel serves up to 64 rows a key head. Its workgroups are at least two per CU where
+// the keys allow, at most one per 256 keys begun.
 CachePlan cache_plan(int B, int Hkv, long long rows, int cap, int d) {
   CachePlan p{};
   p.splits = 1;
-  p.mtiles = (int)((rows + 127) / 128);
+  p.few = rows <= 64;
+  p.mtiles = (int)(p.few ? (rows + kTokenRows - 1) / kTokenRows : (rows + 127) / 128);
+  if (p.few) {
+    const long long wgs = (long long)B * Hkv * p.mtiles, most = (cap + 255) / 256;
+    long long want = (2 * kCus + wgs - 1) / wgs;
+    if (want > most) want = most;
+    if (want > 64) want = 64;
+    if (want > 1) p.splits = (int)want;
+    if (p.splits > 1) p.bytes = (size_t)p.splits * B * Hkv * rows * (d + 2) * sizeof(float);
+  }
   return p;
 }
 
 template <int NP, int D>
 static hipError_t attention_case(const CacheAttentionArgs& a, const CachePlan& plan, void* ws, hipStream_t stream) {
+  if (plan.few) {
+    const long long heads = (long long)a.B * a.c.Hkv, rows = (long long)a.nq * a.group;
+    float* part_o = static_cast<float*>(ws);
+    float* part_l = part_o + (plan.splits > 1 ? plan.splits * heads * rows * D : 0);
+    fp4_token_kernel<NP, D><<<(unsigned)(heads * plan.mtiles * plan.splits), kTokenWaves * kWave, 0, stream>>>(
+        a, plan.mtiles, plan.splits, part_o, part_l);
+    if (plan.splits > 1) {
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+      ExactArgs x{};
+      x.out = a.out;
+      x.B = a.B;
+      x.H = a.H;
+      x.Hkv = a.c.Hkv;
+      x.group = a.group;
+      x.nq = a.nq;
+      launch_join<NP, D>(x, a.lse, plan.splits, part_o, part_l, stream);
+    }
+    return hipGetLastError();
+  }
   constexpr size_t smem = 4 * CacheStage<D>::kKeys;
   auto kernel = fp4_rows_kernel<NP, D>;
   const hipError_t e = allow_lds(kernel, smem);
