@@ -146,13 +146,14 @@ __device__ __forceinline__ void mask_keys(f32x16& s, uint32_t bits) {
 }  // namespace
 
 template <int NP, int D>
-__global__ __launch_bounds__(kExactThreads) void fp4_rows_kernel(CacheAttentionArgs a, int mtiles) {
+__global__ __launch_bounds__(kExactThreads) void fp4_rows_kernel(CacheAttentionArgs a, int mtiles, int splits,
+                                                                 float* __restrict__ part_o, float* __restrict__ part_l) {
   using St = CacheStage<D>;
   constexpr int KC = D / 16, NT = D / 32, BUF = 2 * St::kKeys;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const int tid = threadIdx.x, lane = lane_id(), w = wave_uniform(tid / kWave);
-  const HeadBlock hb = head_block(blockIdx.x, a.B * a.c.Hkv, mtiles, a.causal);
-  const int bk = hb.head, mt = mtiles - 1 - hb.block;         // causal: the longest first
+  const HeadBlock hb = head_block(blockIdx.x, a.B * a.c.Hkv, mtiles * splits, a.causal);
+  const int bk = hb.head, sp = hb.block % splits, mt = mtiles - 1 - hb.block / splits;   // causal: the longest first
   const int b = bk / a.c.Hkv, hk = bk - b * a.c.Hkv, size = 1 << a.c.page_log2;
   const int rows = a.nq * a.group, row0 = (mt * kExactWaves + w) * 32;
   const int m = row0 + (lane & 31), mc = min(m, rows - 1), i = mc / a.group, h = hk * a.group + (mc - i * a.group);
@@ -161,6 +162,7 @@ __global__ __launch_bounds__(kExactThreads) void fp4_rows_kernel(CacheAttentionA
   const int pos_first = start + min(row0, rows - 1) / a.group, pos_last = start + min(row0 + 31, rows - 1) / a.group;
   const int kend = a.causal ? min(limit, start + min((mt + 1) * kExactWaves * 32 - 1, rows - 1) / a.group + 1) : limit;
   const int stages = kend > 0 ? (kend + 63) / 64 : 0;
+  const int n0 = (int)((long long)stages * sp / splits), n1 = (int)((long long)stages * (sp + 1) / splits);
 
   TileAddr<D> at;
   at.init(smem);
@@ -185,17 +187,17 @@ __global__ __launch_bounds__(kExactThreads) void fp4_rows_kernel(CacheAttentionA
   St st;
   RowBits<64> ok{};
   const char* pg[2] = {nullptr, nullptr};
-  if (stages > 0) {
-    pages(0, pg);
-    st.load(pg, 0, size, tid);
-    ok = counted(0, pg);
+  if (n0 < n1) {
+    pages(64 * n0, pg);
+    st.load(pg, 64 * n0, size, tid);
+    ok = counted(64 * n0, pg);
     st.store(smem, ok, tid);
-    pages(64, pg);
+    pages(64 * (n0 + 1), pg);
   }
   __syncthreads();
   auto stage = [&](int n, auto B) {
     constexpr int kbuf = B * BUF;
-    const bool more = n + 1 < stages;
+    const bool more = n + 1 < n1;
     RowBits<64> next{};
     if (more) {
       st.load(pg, 64 * (n + 1), size, tid);
@@ -234,11 +236,20 @@ __global__ __launch_bounds__(kExactThreads) void fp4_rows_kernel(CacheAttentionA
     }
     __syncthreads();
   };
-  for (int n = 0; n < stages; n += 2) {
+  for (int n = n0; n < n1; n += 2) {
     stage(n, std::integral_constant<int, 0>{});
-    if (n + 1 < stages) stage(n + 1, std::integral_constant<int, 1>{});
+    if (n + 1 < n1) stage(n + 1, std::integral_constant<int, 1>{});
   }
   const float den = halves_sum(row[0].sum);
+  if (splits > 1) {
+    const long long pr = ((long long)sp * a.B * a.c.Hkv + bk) * rows + mc;   // the partial row
+    store_rows<3, D>(row[0].o, 1.0f, reinterpret_cast<char*>(part_o + pr * D), m < rows);
+    if (lane < 32 && m < rows) {
+      part_l[2 * pr] = row[0].ref;
+      part_l[2 * pr + 1] = den;
+    }
+    return;
+  }
   store_rows<NP, D>(row[0].o, den > 0.0f ? 1.0f / den : 0.0f, a.out.p + b * a.out.sb + h * a.out.sh + i * a.out.sn,
                     m < rows);
   if (a.lse != nullptr && lane < 32 && m < rows)
@@ -523,51 +534,48 @@ __global__ __launch_bounds__(kTokenWaves * kWave) void fp4_token_kernel(CacheAtt
   }
 }
 
-// The token kernel serves up to 64 rows a key head. Its workgroups are at least two per CU where
-// the keys allow, at most one per 256 keys begun.
+// The token kernel serves up to 64 rows a key head. Where the rows' workgroups are fewer than two
+// per CU several share the keys of the same rows, each at least 256 (512 of the shared-tile kernel).
 CachePlan cache_plan(int B, int Hkv, long long rows, int cap, int d) {
   CachePlan p{};
-  p.splits = 1;
   p.few = rows <= 64;
   p.mtiles = (int)(p.few ? (rows + kTokenRows - 1) / kTokenRows : (rows + 127) / 128);
-  if (p.few) {
-    const long long wgs = (long long)B * Hkv * p.mtiles, most = (cap + 255) / 256;
-    long long want = (2 * kCus + wgs - 1) / wgs;
-    if (want > most) want = most;
-    if (want > 64) want = 64;
-    if (want > 1) p.splits = (int)want;
-    if (p.splits > 1) p.bytes = (size_t)p.splits * B * Hkv * rows * (d + 2) * sizeof(float);
-  }
+  const long long wgs = (long long)B * Hkv * p.mtiles, most = p.few ? (cap + 255) / 256 : (cap + 511) / 512;
+  long long want = (2 * kCus + wgs - 1) / wgs;
+  if (want > most) want = most;
+  if (want > 64) want = 64;
+  p.splits = want > 1 ? (int)want : 1;
+  if (p.splits > 1) p.bytes = (size_t)p.splits * B * Hkv * rows * (d + 2) * sizeof(float);
   return p;
 }
 
 template <int NP, int D>
 static hipError_t attention_case(const CacheAttentionArgs& a, const CachePlan& plan, void* ws, hipStream_t stream) {
+  const long long heads = (long long)a.B * a.c.Hkv, rows = (long long)a.nq * a.group;
+  const unsigned wgs = (unsigned)(heads * plan.mtiles * plan.splits);
+  float* part_o = static_cast<float*>(ws);
+  float* part_l = part_o + (plan.splits > 1 ? plan.splits * heads * rows * D : 0);
   if (plan.few) {
-    const long long heads = (long long)a.B * a.c.Hkv, rows = (long long)a.nq * a.group;
-    float* part_o = static_cast<float*>(ws);
-    float* part_l = part_o + (plan.splits > 1 ? plan.splits * heads * rows * D : 0);
-    fp4_token_kernel<NP, D><<<(unsigned)(heads * plan.mtiles * plan.splits), kTokenWaves * kWave, 0, stream>>>(
-        a, plan.mtiles, plan.splits, part_o, part_l);
-    if (plan.splits > 1) {
-      const hipError_t e = hipGetLastError();
-      if (e != hipSuccess) return e;
-      ExactArgs x{};
-      x.out = a.out;
-      x.B = a.B;
-      x.H = a.H;
-      x.Hkv = a.c.Hkv;
-      x.group = a.group;
-      x.nq = a.nq;
-      launch_join<NP, D>(x, a.lse, plan.splits, part_o, part_l, stream);
-    }
-    return hipGetLastError();
+    fp4_token_kernel<NP, D><<<wgs, kTokenWaves * kWave, 0, stream>>>(a, plan.mtiles, plan.splits, part_o, part_l);
+  } else {
+    constexpr size_t smem = 4 * CacheStage<D>::kKeys;
+    auto kernel = fp4_rows_kernel<NP, D>;
+    const hipError_t e = allow_lds(kernel, smem);
+    if (e != hipSuccess) return e;
+    kernel<<<wgs, kExactThreads, smem, stream>>>(a, plan.mtiles, plan.splits, part_o, part_l);
   }
-  constexpr size_t smem = 4 * CacheStage<D>::kKeys;
-  auto kernel = fp4_rows_kernel<NP, D>;
-  const hipError_t e = allow_lds(kernel, smem);
-  if (e != hipSuccess) return e;
-  kernel<<<(unsigned)((long long)a.B * a.c.Hkv * plan.mtiles), kExactThreads, smem, stream>>>(a, plan.mtiles);
+  if (plan.splits > 1) {
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    ExactArgs x{};
+    x.out = a.out;
+    x.B = a.B;
+    x.H = a.H;
+    x.Hkv = a.c.Hkv;
+    x.group = a.group;
+    x.nq = a.nq;
+    launch_join<NP, D>(x, a.lse, plan.splits, part_o, part_l, stream);
+  }
   return hipGetLastError();
 }
 
