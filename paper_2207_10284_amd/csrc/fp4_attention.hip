@@ -30,22 +30,32 @@ __device__ __forceinline__ int first_query(const CacheAttentionArgs& a, int b, i
 __device__ __forceinline__ float step_of(uint32_t w, int i) { return fp4_step(w >> 8 * i & 255u); }
 
 // A stage's 64 keys of one head on their way from the cache to LDS.
-template <int D>
+template <int D, int T>
 struct CacheStage {
   using Pg = Fp4Page<D>;
   static constexpr int kKeys = 128 * D;            // bytes of the keys in LDS; the values take as many
   // 16 bytes of codes a lane: all lanes have keys and values at D = 128, half of them either
   // at 64; at 32 keys are 64 lanes' and values 8 bytes of 128 lanes
-  static constexpr int KU = 2 * D, VU = D == 32 ? 128 : 2 * D, V0 = kExactThreads - VU;
+  static constexpr int KU = 2 * D, VU = D == 32 ? 128 : 2 * D, V0 = T - VU;
   static constexpr int kSteps = Pg::NB * 8 / 4;    // dwords of eight tokens' steps
   u32x4 k, v;
   uint32_t ke, ve[kSteps];
+
+  // The token of a lane's key unit: 16 lanes' stores of a chunk reach every bank once (neighbouring
+  // tokens four lanes apart; in their order 4-way conflicts)
+  static __device__ __forceinline__ int key_token(int tid) {
+    const int t = tid / Pg::NB;
+    return (t & 48) | (t & 3) << 2 | (t >> 2 & 3);
+  }
+  // Entry i and block pair c of a lane's value unit x of a tile of eight tokens.
+  static __device__ __forceinline__ int value_entry(int x) { return x % 16; }
+  static __device__ __forceinline__ int value_pair(int x) { return x / 16; }
 
   // pg: the pages of the two halves of the stage, null where no key counts
   __device__ __forceinline__ void load(const char* (&pg)[2], int k0, int size, int tid) {
     const int slot0 = k0 & (size - 1), slot1 = (k0 + 32) & (size - 1);
     if (tid < KU) {
-      const int r = tid / Pg::NB, blk = tid % Pg::NB;
+      const int r = key_token(tid), blk = tid % Pg::NB;
       const char* p = r < 32 ? pg[0] : pg[1];
       const int slot = (r < 32 ? slot0 : slot1) + r % 32;
       k = u32x4{0, 0, 0, 0};
@@ -63,7 +73,8 @@ struct CacheStage {
 #pragma unroll
       for (int i = 0; i < kSteps; ++i) ve[i] = 0x7f7f7f7fu;
       if (p != nullptr) {
-        const char* from = p + Pg::values(size) + slot * (D / 2) + u % (VU / 8) * (D == 32 ? 8 : 16);
+        const int x = u % (VU / 8);
+        const char* from = p + Pg::values(size) + slot * (D / 2) + (value_entry(x) * (VU / 128) + value_pair(x)) * (D == 32 ? 8 : 16);
         if constexpr (D == 32) {
           const u32x2 x = *reinterpret_cast<const u32x2*>(from);
           v[0] = x[0];
@@ -81,7 +92,7 @@ struct CacheStage {
   // ok: the keys that count; the steps of others may be anything
   __device__ __forceinline__ void store(char* lds, const RowBits<64>& ok, int tid) const {
     if (tid < KU) {
-      const int r = tid / Pg::NB, blk = tid % Pg::NB;
+      const int r = key_token(tid), blk = tid % Pg::NB;
       // key 16 u + 8 h + 4 a + c of a tile lies at row 16 u + 8 a + 4 h + c: a lane's scores are then of
       // eight neighbouring keys twice
       const int row = (r & 19) | (r & 4) << 1 | (r & 8) >> 1;
@@ -94,7 +105,7 @@ struct CacheStage {
     if (tid >= V0) {
       constexpr int P = Pg::P;
       const int u = tid - V0, t8 = u / (VU / 8), x = u % (VU / 8);
-      const int i = D == 128 ? x / 2 : x, c = D == 128 ? x % 2 : 0;
+      const int i = value_entry(x), c = value_pair(x);
       uint32_t se[kSteps];
 #pragma unroll
       for (int s = 0; s < kSteps; ++s) se[s] = ve[s];
@@ -128,7 +139,7 @@ struct CacheStage {
           hi[j] = __builtin_amdgcn_perm(pr[2 * j + 1], pr[2 * j], 0x07060302u);
         }
         const int ch = 32 * (c * P + b) + i;
-        char* to = lds + kKeys + ch * 128 + ((t8 ^ (ch & 7)) << 4);
+        char* to = lds + kKeys + ch * 128 + ((t8 ^ (ch >> 1 & 7)) << 4);
         *reinterpret_cast<u32x4*>(to) = lo;
         *reinterpret_cast<u32x4*>(to + 16 * 128) = hi;       // 16 channels on: the same place in the swizzle
       }
@@ -145,33 +156,33 @@ __device__ __forceinline__ void mask_keys(f32x16& s, uint32_t bits) {
 
 }  // namespace
 
-template <int NP, int D>
-__global__ __launch_bounds__(kExactThreads) void fp4_rows_kernel(CacheAttentionArgs a, int mtiles, int splits,
+template <int NP, int D, int W>
+__global__ __launch_bounds__(W * kWave) void fp4_rows_kernel(CacheAttentionArgs a, int mtiles, int splits,
                                                                  float* __restrict__ part_o, float* __restrict__ part_l) {
-  using St = CacheStage<D>;
+  using St = CacheStage<D, W * kWave>;
   constexpr int KC = D / 16, NT = D / 32, BUF = 2 * St::kKeys;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const int tid = threadIdx.x, lane = lane_id(), w = wave_uniform(tid / kWave);
   const HeadBlock hb = head_block(blockIdx.x, a.B * a.c.Hkv, mtiles * splits, a.causal);
   const int bk = hb.head, sp = hb.block % splits, mt = mtiles - 1 - hb.block / splits;   // causal: the longest first
   const int b = bk / a.c.Hkv, hk = bk - b * a.c.Hkv, size = 1 << a.c.page_log2;
-  const int rows = a.nq * a.group, row0 = (mt * kExactWaves + w) * 32;
+  const int rows = a.nq * a.group, row0 = (mt * W + w) * 32;
   const int m = row0 + (lane & 31), mc = min(m, rows - 1), i = mc / a.group, h = hk * a.group + (mc - i * a.group);
   const int limit = cached_keys(a, b), start = first_query(a, b, limit);
   const int pos = start + i;                                  // of this lane's row
   const int pos_first = start + min(row0, rows - 1) / a.group, pos_last = start + min(row0 + 31, rows - 1) / a.group;
-  const int kend = a.causal ? min(limit, start + min((mt + 1) * kExactWaves * 32 - 1, rows - 1) / a.group + 1) : limit;
+  const int kend = a.causal ? min(limit, start + min((mt + 1) * W * 32 - 1, rows - 1) / a.group + 1) : limit;
   const int stages = kend > 0 ? (kend + 63) / 64 : 0;
   const int n0 = (int)((long long)stages * sp / splits), n1 = (int)((long long)stages * (sp + 1) / splits);
 
   TileAddr<D> at;
   at.init(smem);
-  uint32_t va[2][2];                               // this lane's part of the values: 32 keys i, half u
+  uint32_t va[2][2];                               // this lane's part of the values: 32 keys t, half u
 #pragma unroll
   for (int t = 0; t < 2; ++t)
 #pragma unroll
     for (int u = 0; u < 2; ++u)
-      va[t][u] = lds_addr(smem) + St::kKeys + (lane & 31) * 128 + (((4 * t + 2 * u + (lane >> 5)) ^ (lane & 7)) << 4);
+      va[t][u] = lds_addr(smem) + St::kKeys + (lane & 31) * 128 + (((4 * t + 2 * u + (lane >> 5)) ^ (lane >> 1 & 7)) << 4);
   FwdRow<NP, D> row[1];
   load_operand<NP, D>(a.q.p + b * a.q.sb + h * a.q.sh + i * a.q.sn, m < rows, row[0].qf);
   row[0].init();
@@ -534,14 +545,17 @@ __global__ __launch_bounds__(kTokenWaves * kWave) void fp4_token_kernel(CacheAtt
   }
 }
 
+template <int D>
+constexpr int kRowWaves = D == 128 ? 8 : 4;
+
 // The token kernel serves up to 64 rows a key head. Where the rows' workgroups are fewer than two
 // per CU several share the keys of the same rows, each at least 256 (512 of the shared-tile kernel).
 CachePlan cache_plan(int B, int Hkv, long long rows, int cap, int d) {
   CachePlan p{};
   p.few = rows <= 64;
-  p.mtiles = (int)(p.few ? (rows + kTokenRows - 1) / kTokenRows : (rows + 127) / 128);
+  p.mtiles = (int)(p.few ? (rows + kTokenRows - 1) / kTokenRows : (rows + (d == 128 ? 255 : 127)) / (d == 128 ? 256 : 128));
   const long long wgs = (long long)B * Hkv * p.mtiles, most = p.few ? (cap + 255) / 256 : (cap + 511) / 512;
-  long long want = (2 * kCus + wgs - 1) / wgs;
+  long long want = ((d == 128 && !p.few ? 1 : 2) * kCus + wgs - 1) / wgs;
   if (want > most) want = most;
   if (want > 64) want = 64;
   p.splits = want > 1 ? (int)want : 1;
@@ -558,11 +572,12 @@ static hipError_t attention_case(const CacheAttentionArgs& a, const CachePlan& p
   if (plan.few) {
     fp4_token_kernel<NP, D><<<wgs, kTokenWaves * kWave, 0, stream>>>(a, plan.mtiles, plan.splits, part_o, part_l);
   } else {
-    constexpr size_t smem = 4 * CacheStage<D>::kKeys;
-    auto kernel = fp4_rows_kernel<NP, D>;
+    constexpr int W = kRowWaves<D>;
+    constexpr size_t smem = 4 * CacheStage<D, W * kWave>::kKeys;
+    auto kernel = fp4_rows_kernel<NP, D, W>;
     const hipError_t e = allow_lds(kernel, smem);
     if (e != hipSuccess) return e;
-    kernel<<<wgs, kExactThreads, smem, stream>>>(a, plan.mtiles, plan.splits, part_o, part_l);
+    kernel<<<wgs, W * kWave, smem, stream>>>(a, plan.mtiles, plan.splits, part_o, part_l);
   }
   if (plan.splits > 1) {
     const hipError_t e = hipGetLastError();
