@@ -154,6 +154,24 @@ __device__ __forceinline__ void mask_keys(f32x16& s, uint32_t bits) {
   for (int r = 0; r < 16; ++r) s[r] = (m >> (16 * (r >> 3) + (r & 7))) & 1 ? s[r] : -INFINITY;
 }
 
+// Weights of the scores s of a stage's two tiles (log2 logits s mul; -inf: does not count) and their sum; a
+// reference that they outgrow is moved first (see tile_weights).
+template <int D>
+__device__ __forceinline__ void stage_weights(FwdRow<1, D>& row, const f32x16 (&s)[2], float mul, Packed<1> (&w)[2]) {
+  float t[2];
+  bool again = false;
+  while (true) {
+    const float c = again && row.ref == -INFINITY ? 0.0f : -row.ref;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) t[x] = row.weights(s[x], mul, c, w[x]);
+    if (again || __ballot(!(t[0] <= kCap && t[1] <= kCap)) == 0) break;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) row.move(s[x], mul, 0.0f);
+    again = true;
+  }
+  row.sum += t[0] + t[1];
+}
+
 }  // namespace
 
 template <int NP, int D, int W>
@@ -163,8 +181,8 @@ __global__ __launch_bounds__(W * kWave) void fp4_rows_kernel(CacheAttentionArgs 
   constexpr int KC = D / 16, NT = D / 32, BUF = 2 * St::kKeys;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const int tid = threadIdx.x, lane = lane_id(), w = wave_uniform(tid / kWave);
-  const HeadBlock hb = head_block(blockIdx.x, a.B * a.c.Hkv, mtiles * splits, a.causal);
-  const int bk = hb.head, sp = hb.block % splits, mt = mtiles - 1 - hb.block / splits;   // causal: the longest first
+  const int sp = blockIdx.x % splits, g = blockIdx.x / splits, bk = g / mtiles;
+  const int mt = mtiles - 1 - (g - bk * mtiles);   // causal: the longest first
   const int b = bk / a.c.Hkv, hk = bk - b * a.c.Hkv, size = 1 << a.c.page_log2;
   const int rows = a.nq * a.group, row0 = (mt * W + w) * 32;
   const int m = row0 + (lane & 31), mc = min(m, rows - 1), i = mc / a.group, h = hk * a.group + (mc - i * a.group);
@@ -183,6 +201,9 @@ __global__ __launch_bounds__(W * kWave) void fp4_rows_kernel(CacheAttentionArgs 
 #pragma unroll
     for (int u = 0; u < 2; ++u)
       va[t][u] = lds_addr(smem) + St::kKeys + (lane & 31) * 128 + (((4 * t + 2 * u + (lane >> 5)) ^ (lane >> 1 & 7)) << 4);
+  auto value = [&](int x, int u, int t, int off) {
+    return *(const __attribute__((address_space(3))) u32x4*)(lds_ptr)(va[x][u] + off + t * 32 * 128);
+  };
   FwdRow<NP, D> row[1];
   load_operand<NP, D>(a.q.p + b * a.q.sb + h * a.q.sh + i * a.q.sn, m < rows, row[0].qf);
   row[0].init();
@@ -196,25 +217,57 @@ __global__ __launch_bounds__(W * kWave) void fp4_rows_kernel(CacheAttentionArgs 
     return RowBits<64>{__ballot(k0 + lane < kend && (lane < 32 ? pg[0] : pg[1]) != nullptr)};
   };
   St st;
-  RowBits<64> ok{};
-  const char* pg[2] = {nullptr, nullptr};
+  RowBits<64> ok{}, ok1{};                         // of this stage and the next
+  const char* pg[2] = {nullptr, nullptr};          // of the next stage to load: its loads do not wait for the table
+  auto load = [&](int n) {
+    st.load(pg, 64 * n, size, tid);
+    ok1 = counted(64 * n, pg);
+    pages(64 * (n + 1), pg);
+  };
   if (n0 < n1) {
     pages(64 * n0, pg);
-    st.load(pg, 64 * n0, size, tid);
-    ok = counted(64 * n0, pg);
+    load(n0);
+    ok = ok1;
     st.store(smem, ok, tid);
-    pages(64 * (n0 + 1), pg);
+    if (n0 + 1 < n1) load(n0 + 1);
   }
   __syncthreads();
+  // Of a SIMD's two waves one converts the next stage before its products and the other after them, so that
+  // one's vector work runs beside the other's matrix work.
+  const bool early = W == 8 && w >= W / 2;
   auto stage = [&](int n, auto B) {
     constexpr int kbuf = B * BUF;
     const bool more = n + 1 < n1;
-    RowBits<64> next{};
-    if (more) {
-      st.load(pg, 64 * (n + 1), size, tid);
-      next = counted(64 * (n + 1), pg);
-      pages(64 * (n + 2), pg);                     // a stage ahead: the loads do not wait for the table
-    }
+    const RowBits<64> next = ok1;
+    auto refill = [&] {
+      st.store(smem + (1 - B) * BUF, next, tid);
+      if (n + 2 < n1) load(n + 2);
+    };
+    if (more && early) refill();
+    if constexpr (NP == 1) {
+      // both tiles at once: one's products beside the other's exponentials
+      const int k0 = 64 * n;
+      if (ok.w != 0 && !(a.causal && k0 > pos_last)) {        // some key counts for the wave
+        f32x16 s[2] = {splat16(0.0f), splat16(0.0f)};
+#pragma unroll
+        for (int c = 0; c < KC; ++c)
+#pragma unroll
+          for (int x = 0; x < 2; ++x) s[x] = mfma16(at.row(kbuf + x * kTileBytes<D>, c), row[0].qf[0][c], s[x]);
+        if (!ok.all() || (a.causal && k0 + 63 > pos_first)) {
+#pragma unroll
+          for (int x = 0; x < 2; ++x)
+            mask_keys(s[x], a.causal ? ok.tile(x) & low_bits(pos - k0 - 32 * x + 1) : ok.tile(x));
+        }
+        Packed<1> pw[2];
+        stage_weights(row[0], s, a.scale_log2, pw);
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) row[0].o[t] = mfma16(value(x, u, t, kbuf), pw[x].w[0][u], row[0].o[t]);
+      }
+    } else {
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
       const uint32_t kb = ok.tile(x);
@@ -236,15 +289,14 @@ __global__ __launch_bounds__(W * kWave) void fp4_rows_kernel(CacheAttentionArgs 
       for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-          const u32x4 v = *(const __attribute__((address_space(3))) u32x4*)(lds_ptr)(va[x][u] + kbuf + t * 32 * 128);
+          const u32x4 v = value(x, u, t, kbuf);
 #pragma unroll
           for (int q = NP - 1; q >= 0; --q) row[0].o[t] = mfma16(v, pw[0].w[q][u], row[0].o[t]);
         }
     }
-    if (more) {
-      ok = next;
-      st.store(smem + (1 - B) * BUF, ok, tid);
     }
+    if (more && !early) refill();
+    ok = next;
     __syncthreads();
   };
   for (int n = n0; n < n1; n += 2) {
@@ -545,17 +597,18 @@ __global__ __launch_bounds__(kTokenWaves * kWave) void fp4_token_kernel(CacheAtt
   }
 }
 
-template <int D>
-constexpr int kRowWaves = D == 128 ? 8 : 4;
+// Waves of fp4_rows_kernel: eight where a stage's conversion costs most and registers allow it.
+constexpr int row_waves(int np, int d) { return np == 1 && d == 128 ? 8 : 4; }
 
 // The token kernel serves up to 64 rows a key head. Where the rows' workgroups are fewer than two
 // per CU several share the keys of the same rows, each at least 256 (512 of the shared-tile kernel).
-CachePlan cache_plan(int B, int Hkv, long long rows, int cap, int d) {
+CachePlan cache_plan(int B, int Hkv, long long rows, int cap, int d, int dtype) {
   CachePlan p{};
   p.few = rows <= 64;
-  p.mtiles = (int)(p.few ? (rows + kTokenRows - 1) / kTokenRows : (rows + (d == 128 ? 255 : 127)) / (d == 128 ? 256 : 128));
+  const int waves = p.few ? kTokenWaves : row_waves(dtype == BF16 ? 1 : 3, d);
+  p.mtiles = (int)(p.few ? (rows + kTokenRows - 1) / kTokenRows : (rows + 32 * waves - 1) / (32 * waves));
   const long long wgs = (long long)B * Hkv * p.mtiles, most = p.few ? (cap + 255) / 256 : (cap + 511) / 512;
-  long long want = ((d == 128 && !p.few ? 1 : 2) * kCus + wgs - 1) / wgs;
+  long long want = ((waves == 8 ? 1 : 2) * kCus + wgs - 1) / wgs;
   if (want > most) want = most;
   if (want > 64) want = 64;
   p.splits = want > 1 ? (int)want : 1;
@@ -572,7 +625,7 @@ static hipError_t attention_case(const CacheAttentionArgs& a, const CachePlan& p
   if (plan.few) {
     fp4_token_kernel<NP, D><<<wgs, kTokenWaves * kWave, 0, stream>>>(a, plan.mtiles, plan.splits, part_o, part_l);
   } else {
-    constexpr int W = kRowWaves<D>;
+    constexpr int W = row_waves(NP, D);
     constexpr size_t smem = 4 * CacheStage<D, W * kWave>::kKeys;
     auto kernel = fp4_rows_kernel<NP, D, W>;
     const hipError_t e = allow_lds(kernel, smem);

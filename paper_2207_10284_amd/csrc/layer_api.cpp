@@ -179,7 +179,8 @@ mra_status_t check_attention(const mra_fp4_cache_t* c, const mra_fp4_attention_t
 bool no_rows(const mra_fp4_cache_t& c, const mra_fp4_attention_t& p) { return c.B == 0 || p.H == 0 || p.n_q == 0; }
 
 mra::CachePlan attention_plan(const mra_fp4_cache_t& c, const mra_fp4_attention_t& p) {
-  return mra::cache_plan(c.B, c.H_kv, (long long)p.n_q * (p.H / c.H_kv), c.max_pages * c.page_size, c.d);
+  return mra::cache_plan(c.B, c.H_kv, (long long)p.n_q * (p.H / c.H_kv), c.max_pages * c.page_size, c.d,
+                         (int)p.dtype);
 }
 
 mra_status_t check_attention_grid(const mra_fp4_cache_t& c, const mra::CachePlan& plan) {

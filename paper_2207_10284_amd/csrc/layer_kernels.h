@@ -62,13 +62,13 @@ struct CacheAttentionArgs {
   float* lse;
 };
 
-// Few rows per key head: `splits` workgroups share the keys of a row tile.
+// Row tiles per key head, and the workgroups that share the keys of one.
 struct CachePlan {
   bool few;                               // fp4_token_kernel
   int splits, mtiles;
   size_t bytes;                           // workspace (0 for one split)
 };
-CachePlan cache_plan(int B, int Hkv, long long rows, int cap, int d);
+CachePlan cache_plan(int B, int Hkv, long long rows, int cap, int d, int dtype);
 hipError_t launch_cache_attention(const CacheAttentionArgs& a, int d, int dtype, const CachePlan& plan, void* ws,
                                   hipStream_t stream);
 
