@@ -93,11 +93,8 @@ mra_status_t mra_rotary_backward(const mra_rotary_problem_t* p, const mra_stride
  *
  * The bytes of one page of one head, page_size tokens of d channels (4 bits: codes
  * 0 to 7 in the order above, 8 more for negative ones; e is held as e + 127):
- *   keys         [page_size][d/2]       channel 2j low, 2j + 1 high
- *   values       [page_size/8][16][d/32/P][8][P]  P = min(2, d/32); entry [t][i][c][r][x] is
- *                 of token 8t + r, channels 32 (cP + x) + i low, + 16 high
- *   key steps    [page_size][d/32]
- *   value steps  [page_size][d/32]
+ *   keys, values           [page_size][d/2] each; channel 2j low, 2j + 1 high
+ *   key and value steps    [page_size][d/32] each
  *
  * A sequence's tokens lie in the pages of its row of `table`: token t in page
  * table[b][t / page_size], place t % page_size. Sequences may share pages. An entry

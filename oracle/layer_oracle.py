@@ -80,25 +80,13 @@ def held(x):
     return (v * torch.exp2(e)).flatten(-2), e.squeeze(-1).long()
 
 
-def page_bytes(k, v, page_size):
+def page_bytes(k, v):
     """The bytes of one page of one head, of its tokens' k and v [page_size, d] (host tensors)."""
-    d = k.shape[-1]
-    P = min(2, d // 32)
-    codes = []
+    codes, steps = [], []
     for x in (k, v):
         h, e = held(x)
         y = (h.unflatten(-1, (-1, 32)) / torch.exp2(e.double())[..., None]).flatten(-2)
-        c = (y.abs().unsqueeze(-1) == torch.tensor(GRID, dtype=torch.float64)).int().argmax(-1)
-        codes.append((c + 8 * (y < 0).int(), e))
-    (kc, ke), (vc, ve) = codes
-    keys = kc[:, 0::2] | kc[:, 1::2] << 4
-    values = torch.zeros(page_size // 8, 16, d // 32 // P, 8, P, dtype=torch.int32)
-    for t in range(page_size // 8):
-        for i in range(16):
-            for c in range(d // 32 // P):
-                for r in range(8):
-                    for x in range(P):
-                        row = vc[8 * t + r]
-                        values[t, i, c, r, x] = row[32 * (c * P + x) + i] | row[32 * (c * P + x) + 16 + i] << 4
-    parts = (keys.flatten(), values.flatten(), (ke + 127).flatten(), (ve + 127).flatten())
-    return torch.cat([p.to(torch.uint8) for p in parts])
+        c = (y.abs().unsqueeze(-1) == torch.tensor(GRID, dtype=torch.float64)).int().argmax(-1) + 8 * (y < 0).int()
+        codes.append(c[:, 0::2] | c[:, 1::2] << 4)
+        steps.append(e + 127)
+    return torch.cat([p.flatten().to(torch.uint8) for p in codes + steps])

@@ -26,133 +26,59 @@ __device__ __forceinline__ int first_query(const CacheAttentionArgs& a, int b, i
   return a.q_start == nullptr ? keys - a.nq : min(max(a.q_start[b], -kFar), kFar);
 }
 
-// Bits of a step dword's byte i as a float32 step.
-__device__ __forceinline__ float step_of(uint32_t w, int i) { return fp4_step(w >> 8 * i & 255u); }
-
-// A stage's 64 keys of one head on their way from the cache to LDS.
+// A stage's 64 keys of one head on their way from the cache to LDS, by T threads.
 template <int D, int T>
 struct CacheStage {
   using Pg = Fp4Page<D>;
   static constexpr int kKeys = 128 * D;            // bytes of the keys in LDS; the values take as many
-  // 16 bytes of codes a lane: all lanes have keys and values at D = 128, half of them either
-  // at 64; at 32 keys are 64 lanes' and values 8 bytes of 128 lanes
-  static constexpr int KU = 2 * D, VU = D == 32 ? 128 : 2 * D, V0 = T - VU;
-  static constexpr int kSteps = Pg::NB * 8 / 4;    // dwords of eight tokens' steps
-  u32x4 k, v;
-  uint32_t ke, ve[kSteps];
+  // 16 bytes of codes, a block, per lane: with fewer lanes than blocks a lane has keys and values
+  static constexpr int U = 2 * D, N = 2 * U > T ? 2 : 1;
+  static_assert(N == 1 || U == T, "a lane has one unit of either, or of one of them");
+  u32x4 w[N];
+  uint32_t e[N];
 
-  // The token of a lane's key unit: 16 lanes' stores of a chunk reach every bank once (neighbouring
-  // tokens four lanes apart; in their order 4-way conflicts)
-  static __device__ __forceinline__ int key_token(int tid) {
-    const int t = tid / Pg::NB;
-    return (t & 48) | (t & 3) << 2 | (t >> 2 & 3);
+  // Unit n of a lane: keys or values (x), token and block; false: none. 16 lanes' stores of a chunk reach every bank once:
+  // neighbouring tokens are four units apart (in their order: 4-way conflicts).
+  static __device__ __forceinline__ bool unit(int n, int tid, int& x, int& r, int& blk) {
+    const int u = tid % U, t = u / Pg::NB;
+    x = N == 2 ? n : tid / U;
+    r = (t & 48) | (t & 3) << 2 | (t >> 2 & 3);
+    blk = u % Pg::NB;
+    return x < 2;
   }
-  // Entry i and block pair c of a lane's value unit x of a tile of eight tokens.
-  static __device__ __forceinline__ int value_entry(int x) { return x % 16; }
-  static __device__ __forceinline__ int value_pair(int x) { return x / 16; }
 
   // pg: the pages of the two halves of the stage, null where no key counts
   __device__ __forceinline__ void load(const char* (&pg)[2], int k0, int size, int tid) {
     const int slot0 = k0 & (size - 1), slot1 = (k0 + 32) & (size - 1);
-    if (tid < KU) {
-      const int r = key_token(tid), blk = tid % Pg::NB;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      int x, r, blk;
+      if (!unit(n, tid, x, r, blk)) continue;
       const char* p = r < 32 ? pg[0] : pg[1];
       const int slot = (r < 32 ? slot0 : slot1) + r % 32;
-      k = u32x4{0, 0, 0, 0};
-      ke = 127;
+      w[n] = u32x4{0, 0, 0, 0};
+      e[n] = 127;
       if (p != nullptr) {
-        k = *reinterpret_cast<const u32x4*>(p + slot * (D / 2) + blk * 16);
-        ke = (uint8_t)p[Pg::key_steps(size) + slot * Pg::NB + blk];
-      }
-    }
-    if (tid >= V0) {
-      const int u = tid - V0, t8 = u / (VU / 8);   // a tile of eight tokens
-      const char* p = t8 < 4 ? pg[0] : pg[1];
-      const int slot = (t8 < 4 ? slot0 : slot1) + t8 % 4 * 8;
-      v = u32x4{0, 0, 0, 0};
-#pragma unroll
-      for (int i = 0; i < kSteps; ++i) ve[i] = 0x7f7f7f7fu;
-      if (p != nullptr) {
-        const int x = u % (VU / 8);
-        const char* from = p + Pg::values(size) + slot * (D / 2) + (value_entry(x) * (VU / 128) + value_pair(x)) * (D == 32 ? 8 : 16);
-        if constexpr (D == 32) {
-          const u32x2 x = *reinterpret_cast<const u32x2*>(from);
-          v[0] = x[0];
-          v[1] = x[1];
-        } else {
-          v = *reinterpret_cast<const u32x4*>(from);
-        }
-        const uint32_t* s = reinterpret_cast<const uint32_t*>(p + Pg::value_steps(size) + slot * Pg::NB);
-#pragma unroll
-        for (int i = 0; i < kSteps; ++i) ve[i] = s[i];
+        w[n] = *reinterpret_cast<const u32x4*>(p + Pg::codes(x, size) + slot * (D / 2) + blk * 16);
+        e[n] = (uint8_t)p[Pg::steps(x, size) + slot * Pg::NB + blk];
       }
     }
   }
 
   // ok: the keys that count; the steps of others may be anything
   __device__ __forceinline__ void store(char* lds, const RowBits<64>& ok, int tid) const {
-    if (tid < KU) {
-      const int r = key_token(tid), blk = tid % Pg::NB;
-      // key 16 u + 8 h + 4 a + c of a tile lies at row 16 u + 8 a + 4 h + c: a lane's scores are then of
-      // eight neighbouring keys twice
-      const int row = (r & 19) | (r & 4) << 1 | (r & 8) >> 1;
-      const float step = fp4_step(ke);
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      int x, r, blk;
+      if (!unit(n, tid, x, r, blk)) continue;
+      const float step = fp4_step(ok.all() || ok.row(r) ? e[n] : 127);
+      char* to = lds + x * kKeys + (r >> 5) * kTileBytes<D>;
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        *reinterpret_cast<u32x4*>(lds + (r >> 5) * kTileBytes<D> + raw_offset<D, exact_swz<D>>(row, 32 * blk + 8 * j)) =
-            fp4_decode(k[j], step);
-    }
-    if (tid >= V0) {
-      constexpr int P = Pg::P;
-      const int u = tid - V0, t8 = u / (VU / 8), x = u % (VU / 8);
-      const int i = value_entry(x), c = value_pair(x);
-      uint32_t se[kSteps];
-#pragma unroll
-      for (int s = 0; s < kSteps; ++s) se[s] = ve[s];
-      if (!ok.all()) {                             // wave-uniform
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (!ok.row(8 * t8 + (4 * s + e) / Pg::NB)) se[s] = (se[s] & ~(255u << 8 * e)) | 127u << 8 * e;
-      }
-#pragma unroll
-      for (int b = 0; b < P; ++b) {
-        uint32_t pr[8];                            // token r: channels + i (low half) and + 16 + i
-#pragma unroll
-        for (int r = 0; r < 8; ++r) {
-          // byte r P + b of the codes; the steps of token r are NB bytes, of which c P + b is the block's
-          const uint32_t w = v[(r * P + b) / 4];
-          const int at = r * Pg::NB + b;
-          const float step = D == 128 ? fp4_step(se[r] >> (16 * c + 8 * b) & 255u) : step_of(se[at / 4], at % 4);
-          switch ((r * P + b) % 4) {
-            case 0: pr[r] = fp4_pair<0>(w, step); break;
-            case 1: pr[r] = fp4_pair<1>(w, step); break;
-            case 2: pr[r] = fp4_pair<2>(w, step); break;
-            default: pr[r] = fp4_pair<3>(w, step); break;
-          }
-        }
-        u32x4 lo, hi;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          lo[j] = __builtin_amdgcn_perm(pr[2 * j + 1], pr[2 * j], 0x05040100u);
-          hi[j] = __builtin_amdgcn_perm(pr[2 * j + 1], pr[2 * j], 0x07060302u);
-        }
-        const int ch = 32 * (c * P + b) + i;
-        char* to = lds + kKeys + ch * 128 + ((t8 ^ (ch >> 1 & 7)) << 4);
-        *reinterpret_cast<u32x4*>(to) = lo;
-        *reinterpret_cast<u32x4*>(to + 16 * 128) = hi;       // 16 channels on: the same place in the swizzle
-      }
+        *reinterpret_cast<u32x4*>(to + raw_offset<D, exact_swz<D>>(r & 31, 32 * blk + 8 * j)) = fp4_decode(w[n][j], step);
     }
   }
 };
-
-// Scores of keys that do not count become -inf; register r holds key 16 (r / 8) + 8 (lane / 32) + r % 8.
-__device__ __forceinline__ void mask_keys(f32x16& s, uint32_t bits) {
-  const uint32_t m = bits >> (8 * (lane_id() >> 5));
-#pragma unroll
-  for (int r = 0; r < 16; ++r) s[r] = (m >> (16 * (r >> 3) + (r & 7))) & 1 ? s[r] : -INFINITY;
-}
 
 // Weights of the scores s of a stage's two tiles (log2 logits s mul; -inf: does not count) and their sum; a
 // reference that they outgrow is moved first (see tile_weights).
@@ -195,15 +121,6 @@ __global__ __launch_bounds__(W * kWave) void fp4_rows_kernel(CacheAttentionArgs 
 
   TileAddr<D> at;
   at.init(smem);
-  uint32_t va[2][2];                               // this lane's part of the values: 32 keys t, half u
-#pragma unroll
-  for (int t = 0; t < 2; ++t)
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-      va[t][u] = lds_addr(smem) + St::kKeys + (lane & 31) * 128 + (((4 * t + 2 * u + (lane >> 5)) ^ (lane >> 1 & 7)) << 4);
-  auto value = [&](int x, int u, int t, int off) {
-    return *(const __attribute__((address_space(3))) u32x4*)(lds_ptr)(va[x][u] + off + t * 32 * 128);
-  };
   FwdRow<NP, D> row[1];
   load_operand<NP, D>(a.q.p + b * a.q.sb + h * a.q.sh + i * a.q.sn, m < rows, row[0].qf);
   row[0].init();
@@ -256,7 +173,7 @@ __global__ __launch_bounds__(W * kWave) void fp4_rows_kernel(CacheAttentionArgs 
         if (!ok.all() || (a.causal && k0 + 63 > pos_first)) {
 #pragma unroll
           for (int x = 0; x < 2; ++x)
-            mask_keys(s[x], a.causal ? ok.tile(x) & low_bits(pos - k0 - 32 * x + 1) : ok.tile(x));
+            select_rows(s[x], a.causal ? ok.tile(x) & low_bits(pos - k0 - 32 * x + 1) : ok.tile(x), -INFINITY);
         }
         Packed<1> pw[2];
         stage_weights(row[0], s, a.scale_log2, pw);
@@ -265,7 +182,7 @@ __global__ __launch_bounds__(W * kWave) void fp4_rows_kernel(CacheAttentionArgs 
 #pragma unroll
           for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int t = 0; t < NT; ++t) row[0].o[t] = mfma16(value(x, u, t, kbuf), pw[x].w[0][u], row[0].o[t]);
+            for (int t = 0; t < NT; ++t) row[0].o[t] = mfma16(at.trans(kbuf + St::kKeys + x * kTileBytes<D>, u, t), pw[x].w[0][u], row[0].o[t]);
       }
     } else {
 #pragma unroll
@@ -281,7 +198,7 @@ __global__ __launch_bounds__(W * kWave) void fp4_rows_kernel(CacheAttentionArgs 
         for (int q = NP - 1; q >= 0; --q) s[0] = mfma16(k, row[0].qf[q][c], s[0]);
       }
       const uint32_t bits = a.causal ? kb & low_bits(pos - k0 + 1) : kb;
-      if (kb != ~0u || (a.causal && k0 + 31 > pos_first)) mask_keys(s[0], bits);
+      if (kb != ~0u || (a.causal && k0 + 31 > pos_first)) select_rows(s[0], bits, -INFINITY);
       const float mul[1] = {a.scale_log2}, add[1] = {0.0f};
       Packed<NP> pw[1];
       tile_weights<NP, D, 1>(row, s, mul, add, pw);
@@ -289,7 +206,7 @@ __global__ __launch_bounds__(W * kWave) void fp4_rows_kernel(CacheAttentionArgs 
       for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-          const u32x4 v = value(x, u, t, kbuf);
+          const u32x4 v = at.trans(kbuf + St::kKeys + x * kTileBytes<D>, u, t);
 #pragma unroll
           for (int q = NP - 1; q >= 0; --q) row[0].o[t] = mfma16(v, pw[0].w[q][u], row[0].o[t]);
         }
@@ -340,71 +257,69 @@ __device__ __forceinline__ float column_sum(float v) {
 
 // 32 keys of one head as the wave's lanes hold them: lane (g, i) = (lane / 16, lane % 16) has channels
 // g D/4 .. of keys 8 (i / 4) + 4 x + i % 4 (x = 0, 1), so that register r of the scores of x is key
-// 8 g + 4 x + r of column i, and of the values entry i of keys 8 g .. 8 g + 7.
+// 8 g + 4 x + r of column i; and of the values of keys 16 x + i.
 template <int D>
 struct CacheTile {
   using Pg = Fp4Page<D>;
-  uint32_t k[2][D / 32], ke[2], v[D / 16], ve[D / 16];
+  uint32_t w[2][2][D / 32], e[2][2];               // keys and values, x
 
-  template <int N>
-  static __device__ __forceinline__ void words(const char* p, uint32_t (&w)[N]) {
-    if constexpr (N % 4 == 0) {
-#pragma unroll
-      for (int i = 0; i < N / 4; ++i) {
-        const u32x4 x = reinterpret_cast<const u32x4*>(p)[i];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) w[4 * i + e] = x[e];
-      }
-    } else if constexpr (N == 2) {
-      const u32x2 x = *reinterpret_cast<const u32x2*>(p);
-      w[0] = x[0];
-      w[1] = x[1];
-    } else {
-      w[0] = *reinterpret_cast<const uint32_t*>(p);
-    }
+  static __device__ __forceinline__ int row(int value, int x) {
+    const int i = lane_id() & 15;
+    return value ? 16 * x + i : 8 * (i >> 2) + 4 * x + (i & 3);
   }
 
   __device__ __forceinline__ void load(const char* page, int slot, int size) {
-    const int lane = lane_id(), g = lane >> 4, i = lane & 15;
+    const int g = lane_id() >> 4;
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const int row = slot + 8 * (i >> 2) + 4 * x + (i & 3);
-      words(page + row * (D / 2) + g * (D / 8), k[x]);
-      ke[x] = (uint8_t)page[Pg::key_steps(size) + row * Pg::NB + g * Pg::NB / 4];
-    }
-    words(page + Pg::values(size) + slot * (D / 2) + g * Pg::kTile + i * (D / 4), v);
-    words(page + Pg::value_steps(size) + (slot + 8 * g) * Pg::NB, ve);
-  }
-
-  // Steps of keys that do not count may be anything; `bits`: those of this lane's eight that do.
-  __device__ __forceinline__ void clean(uint32_t bits) {
+    for (int v = 0; v < 2; ++v)
 #pragma unroll
-    for (int w = 0; w < D / 16; ++w)
+      for (int x = 0; x < 2; ++x) {
+        const int r = slot + row(v, x);
+        const char* p = page + Pg::codes(v, size) + r * (D / 2) + g * (D / 8);
+        if constexpr (D == 128) {
+          const u32x4 q = *reinterpret_cast<const u32x4*>(p);
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (!(bits >> (4 * w + e) / Pg::NB & 1)) ve[w] = (ve[w] & ~(255u << 8 * e)) | 127u << 8 * e;
-  }
-
-  // The A operands of the channels 32 b + 0 .. 15 and 32 b + 16 .. 31.
-  __device__ __forceinline__ void values(int b, u32x4& lo, u32x4& hi) const {
-    constexpr int P = Pg::P, NB = Pg::NB;
-    uint32_t pr[8];
-#pragma unroll
-    for (int r = 0; r < 8; ++r) {
-      const int at = (b / P * 8 + r) * P + b % P, es = r * NB + b;
-      const float step = fp4_step(ve[es / 4] >> 8 * (es % 4) & 255u);
-      switch (at % 4) {
-        case 0: pr[r] = fp4_pair<0>(v[at / 4], step); break;
-        case 1: pr[r] = fp4_pair<1>(v[at / 4], step); break;
-        case 2: pr[r] = fp4_pair<2>(v[at / 4], step); break;
-        default: pr[r] = fp4_pair<3>(v[at / 4], step); break;
+          for (int n = 0; n < 4; ++n) w[v][x][n] = q[n];
+        } else if constexpr (D == 64) {
+          const u32x2 q = *reinterpret_cast<const u32x2*>(p);
+          w[v][x][0] = q[0];
+          w[v][x][1] = q[1];
+        } else {
+          w[v][x][0] = *reinterpret_cast<const uint32_t*>(p);
+        }
+        e[v][x] = (uint8_t)page[Pg::steps(v, size) + r * Pg::NB + g * Pg::NB / 4];
       }
-    }
+  }
+};
+
+// A wave's 32 values of D channels in LDS (256-byte aligned), rows of bfloat16. A row's blocks of 16 channels, and the halves of a block,
+// are exchanged by row so that neither the stores of 8 rows at a time nor the transposing reads of 4 or 8 meet in a bank.
+template <int D>
+struct ValueTile {
+  uint32_t to, from[2];                            // this lane's first chunk of a row; transposed rows + 0 and + 4
+
+  static __device__ __forceinline__ int place(int r, int c) {    // of channel c, a multiple of 4
+    const int f = D == 128 ? (r & 3) | (r >> 3 & 1) << 2 : D == 64 ? (r >> 1 & 1) | (r >> 3 & 1) << 1 : r >> 3 & 1;
+    return r * 2 * D + (((c >> 4) ^ f) << 5) + (((c >> 3 & 1) ^ (r >> 2 & 1)) << 4) + (c & 4) * 2;
+  }
+  __device__ __forceinline__ void init(const char* lds) {
+    const int lane = lane_id(), g = lane >> 4, i = lane & 15;
+    to = lds_addr(lds) + place(i, g * (D / 4));
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      lo[j] = __builtin_amdgcn_perm(pr[2 * j + 1], pr[2 * j], 0x05040100u);
-      hi[j] = __builtin_amdgcn_perm(pr[2 * j + 1], pr[2 * j], 0x07060302u);
-    }
+    for (int e = 0; e < 2; ++e) from[e] = lds_addr(lds) + place(8 * g + 4 * e + (i >> 2), 4 * (i & 3));
+  }
+  // chunk n (8 channels) of this lane's row 16 x + lane % 16
+  __device__ __forceinline__ void put(int x, int n, const u32x4& v) const {
+    *(__attribute__((address_space(3))) u32x4*)(lds_ptr)((to ^ 16u * n) + x * 16 * 2 * D) = v;
+  }
+  // the A operand of channels 16 t ..: of channel 16 t + lane % 16, rows 8 (lane / 16) + 0 .. 7
+  __device__ __forceinline__ u32x4 get(int t) const {
+    u32x2 x[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+      x[e] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                           (__attribute__((address_space(3))) s16x4*)(lds_ptr)(from[e] ^ 32u * t)));
+    return u32x4{x[0][0], x[0][1], x[1][0], x[1][1]};
   }
 };
 
@@ -463,13 +378,22 @@ struct TokenRows {
     return t;
   }
 
-  // Weights of a tile's scores; a reference that it outgrows is moved first, in all lanes of its column.
-  __device__ __forceinline__ void tile(const float (&s)[8], float mul, u32x4 (&w)[NP]) {
-    float t = weights(s, mul, ref, w);
-    if (__ballot(!(t <= kCap)) != 0) {             // also where ref is -inf
-      float mx = s[0];
+  // Weights of U tiles' scores; a reference that they outgrow is moved first, in all lanes of its column.
+  template <int U>
+  __device__ __forceinline__ void tiles(const float (&s)[U][8], float mul, u32x4 (&w)[U][NP]) {
+    float t[U];
+    bool fits = true;
 #pragma unroll
-      for (int r = 1; r < 8; ++r) mx = fmaxf(mx, s[r]);
+    for (int u = 0; u < U; ++u) {
+      t[u] = weights(s[u], mul, ref, w[u]);
+      fits = fits && t[u] <= kCap;                 // not so where ref is -inf
+    }
+    if (__ballot(!fits) != 0) {
+      float mx = s[0][0];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int r = 0; r < 8; ++r) mx = fmaxf(mx, s[u][r]);
       mx = column_max(mx) * mul;
       const float next = mx > ref ? mx + kMargin : ref;
       const float f = next == ref ? 1.0f : __builtin_amdgcn_exp2f(ref - next);
@@ -477,21 +401,26 @@ struct TokenRows {
       for (int x = 0; x < D / 16; ++x) o[x] *= f;
       sum *= f;
       ref = next;
-      t = weights(s, mul, ref == -INFINITY ? 0.0f : ref, w);    // no key yet: every s is -inf
+#pragma unroll
+      for (int u = 0; u < U; ++u) t[u] = weights(s[u], mul, ref == -INFINITY ? 0.0f : ref, w[u]);   // no key yet: every s is -inf
     }
-    sum += t;
+#pragma unroll
+    for (int u = 0; u < U; ++u) sum += t[u];
   }
 };
 
-template <int NP, int D>
-__global__ __launch_bounds__(kTokenWaves * kWave) void fp4_token_kernel(CacheAttentionArgs a, int mtiles, int splits,
+template <int NP, int D, int W, int U>
+__global__ __launch_bounds__(W * kWave) void fp4_token_kernel(CacheAttentionArgs a, int mtiles, int splits,
                                                                         float* __restrict__ part_o,
                                                                         float* __restrict__ part_l) {
   constexpr int KC = D / 32, NT = D / 16;
-  __shared__ __attribute__((aligned(16))) f32x4 merged[kTokenWaves - 1][NT][kWave];
-  __shared__ float refs[kTokenWaves][kWave], sums[kTokenWaves][kWave];
+  // the waves' values, at the end the sums of all but the first
+  constexpr int kValues = W * U * 64 * D, kMerge = (W - 1) * NT * kWave * 16;
+  __shared__ __attribute__((aligned(256))) char lds[kValues > kMerge ? kValues : kMerge];
+  f32x4(*merged)[NT][kWave] = reinterpret_cast<f32x4(*)[NT][kWave]>(lds);
+  __shared__ float refs[W][kWave], sums[W][kWave];
   const int lane = lane_id(), w = wave_uniform(threadIdx.x / kWave), g4 = lane >> 4;
-  const int g = xcd_remap(blockIdx.x, gridDim.x);
+  const int g = blockIdx.x;
   const int sp = g % splits, mt = g / splits % mtiles, bk = g / splits / mtiles;
   const int b = bk / a.c.Hkv, hk = bk - b * a.c.Hkv, size = 1 << a.c.page_log2;
   const int rows = a.nq * a.group, row0 = mt * kTokenRows;
@@ -507,51 +436,72 @@ __global__ __launch_bounds__(kTokenWaves * kWave) void fp4_token_kernel(CacheAtt
   row.load_queries(a.q.p + b * a.q.sb + h * a.q.sh + i * a.q.sn, m < rows);
   row.init();
   auto page_of = [&](int t) { return t < t1 ? fp4_page(a.c, b, hk, 32 * t) : nullptr; };
-  CacheTile<D> next;
+  ValueTile<D> values[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) values[u].init(lds + (w * U + u) * 64 * D);
+  CacheTile<D> next[U];
+  const char *page[U], *ahead[U];                  // of the tiles in next, and of those behind them
   int t = t0 + w;
-  const char* page = page_of(t);
-  if (page != nullptr) next.load(page, 32 * t & (size - 1), size);
-  const char* ahead = page_of(t + kTokenWaves);
-  for (; t < t1; t += kTokenWaves) {
-    CacheTile<D> tile = next;
-    const bool some = page != nullptr;
-    page = ahead;
-    if (page != nullptr) next.load(page, 32 * (t + kTokenWaves) & (size - 1), size);
-    ahead = page_of(t + 2 * kTokenWaves);
-    if (!some) continue;                           // no page: no key
-    const int k0 = 32 * t;
-    float s[8];
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      f32x4 c = {0.0f, 0.0f, 0.0f, 0.0f};
-      const float step = fp4_step(tile.ke[x]);
+  for (int u = 0; u < U; ++u) {
+    page[u] = page_of(t + u * W);
+    if (page[u] != nullptr) next[u].load(page[u], 32 * (t + u * W) & (size - 1), size);
+    ahead[u] = page_of(t + (U + u) * W);
+  }
+  for (; t < t1; t += U * W) {
+    CacheTile<D> tile[U];
+    bool some[U];
 #pragma unroll
-      for (int n = 0; n < KC; ++n) {
-        const u32x4 k = fp4_decode(tile.k[x][n], step);
+    for (int u = 0; u < U; ++u) {
+      tile[u] = next[u];
+      some[u] = page[u] != nullptr;
+      page[u] = ahead[u];
+      if (page[u] != nullptr) next[u].load(page[u], 32 * (t + (U + u) * W) & (size - 1), size);
+      ahead[u] = page_of(t + (2 * U + u) * W);
+    }
+    float s[U][8];
 #pragma unroll
-        for (int q = NP - 1; q >= 0; --q) c = mfma4(k, row.qf[q][n], c);
+    for (int u = 0; u < U; ++u) {
+      const int k0 = 32 * (t + u * W);
+      const int end = some[u] ? kend : 0;          // no page, or past the last tile: no key
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        // the steps of keys that do not count may be anything
+        const float step = fp4_step(k0 + CacheTile<D>::row(1, x) < end ? tile[u].e[1][x] : 127);
+#pragma unroll
+        for (int n = 0; n < KC; ++n) values[u].put(x, n, fp4_decode(tile[u].w[1][x][n], step));
       }
 #pragma unroll
-      for (int r = 0; r < 4; ++r) s[4 * x + r] = c[r];
-    }
-    if (k0 + 32 > kend || (a.causal && k0 + 31 > pos_first)) {
-      const uint32_t bits = low_bits((a.causal ? min(kend, pos + 1) : kend) - k0 - 8 * g4);
+      for (int x = 0; x < 2; ++x) {
+        f32x4 c = {0.0f, 0.0f, 0.0f, 0.0f};
+        const float step = fp4_step(tile[u].e[0][x]);
 #pragma unroll
-      for (int r = 0; r < 8; ++r) s[r] = bits >> r & 1 ? s[r] : -INFINITY;
-      if (k0 + 32 > kend) tile.clean(low_bits(kend - k0 - 8 * g4));
-    }
-    u32x4 pw[NP];
-    row.tile(s, a.scale_log2, pw);
+        for (int n = 0; n < KC; ++n) {
+          const u32x4 k = fp4_decode(tile[u].w[0][x][n], step);
 #pragma unroll
-    for (int n = 0; n < D / 32; ++n) {
-      u32x4 lo, hi;
-      tile.values(n, lo, hi);
+          for (int q = NP - 1; q >= 0; --q) c = mfma4(k, row.qf[q][n], c);
+        }
 #pragma unroll
-      for (int q = NP - 1; q >= 0; --q) {
-        row.o[2 * n] = mfma4(lo, pw[q], row.o[2 * n]);
-        row.o[2 * n + 1] = mfma4(hi, pw[q], row.o[2 * n + 1]);
+        for (int r = 0; r < 4; ++r) s[u][4 * x + r] = c[r];
+      }
+      if (k0 + 32 > end || (a.causal && k0 + 31 > pos_first)) {
+        const uint32_t bits = low_bits((a.causal ? min(end, pos + 1) : end) - k0 - 8 * g4);
+#pragma unroll
+        for (int r = 0; r < 8; ++r) s[u][r] = bits >> r & 1 ? s[u][r] : -INFINITY;
       }
     }
+    u32x4 pw[U][NP];
+    row.tiles(s, a.scale_log2, pw);
+    wave_lds_sync();
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int x = 0; x < NT; ++x) {
+        const u32x4 v = values[u].get(x);
+#pragma unroll
+        for (int q = NP - 1; q >= 0; --q) row.o[x] = mfma4(v, pw[u][q], row.o[x]);
+      }
+    wave_lds_sync();
   }
   // the waves' sums relative to the largest reference, added in wave order
   float sum = column_sum(row.sum);
@@ -560,7 +510,7 @@ __global__ __launch_bounds__(kTokenWaves * kWave) void fp4_token_kernel(CacheAtt
   __syncthreads();
   float top = refs[0][lane];
 #pragma unroll
-  for (int x = 1; x < kTokenWaves; ++x) top = fmaxf(top, refs[x][lane]);
+  for (int x = 1; x < W; ++x) top = fmaxf(top, refs[x][lane]);
   auto factor = [&](float ref) { return ref == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ref - top); };
   const float f = factor(row.ref);
 #pragma unroll
@@ -572,7 +522,7 @@ __global__ __launch_bounds__(kTokenWaves * kWave) void fp4_token_kernel(CacheAtt
   if (w != 0) return;
   sum *= f;
 #pragma unroll
-  for (int p = 1; p < kTokenWaves; ++p) {
+  for (int p = 1; p < W; ++p) {
     sum += sums[p][lane] * factor(refs[p][lane]);
 #pragma unroll
     for (int x = 0; x < NT; ++x) row.o[x] += merged[p - 1][x][lane];
@@ -623,7 +573,7 @@ static hipError_t attention_case(const CacheAttentionArgs& a, const CachePlan& p
   float* part_o = static_cast<float*>(ws);
   float* part_l = part_o + (plan.splits > 1 ? plan.splits * heads * rows * D : 0);
   if (plan.few) {
-    fp4_token_kernel<NP, D><<<wgs, kTokenWaves * kWave, 0, stream>>>(a, plan.mtiles, plan.splits, part_o, part_l);
+    fp4_token_kernel<NP, D, kTokenWaves, 1><<<wgs, kTokenWaves * kWave, 0, stream>>>(a, plan.mtiles, plan.splits, part_o, part_l);
   } else {
     constexpr int W = row_waves(NP, D);
     constexpr size_t smem = 4 * CacheStage<D, W * kWave>::kKeys;

@@ -2,9 +2,7 @@
 //
 // Bound by memory: a value comes in as 2 or 4 bytes and leaves as 17/32 of one. A workgroup
 // takes 32 neighbouring tokens (aligned, so of one page) of one head, keys and values. A lane
-// has eight channels of a token, four lanes a block and its step. Keys leave from there; values,
-// which the cache holds eight tokens of a channel pair together (as the products of attention take them),
-// are put in order in LDS first.
+// has eight channels of a token, four lanes a block and its step.
 #include "fp4_tile.h"
 
 namespace mra {
@@ -74,8 +72,6 @@ __global__ __launch_bounds__(kThreads) void fp4_write_kernel(CacheRowsArgs a, in
   using Pg = Fp4Page<D>;
   constexpr int CPR = D / 8, E = DT == BF16 ? 2 : 4;
   constexpr int N = 2 * 32 * CPR / kThreads;       // units of eight channels per lane
-  constexpr int COPY = 16 * D / kThreads;          // bytes of values per lane
-  __shared__ __attribute__((aligned(16))) uint8_t vt[16 * D];
   const Span s = span_of(a, tiles);
   if (s.page == nullptr) return;
   const int tid = threadIdx.x, size = 1 << a.c.page_log2, slot = s.t0 & (size - 1);
@@ -95,43 +91,16 @@ __global__ __launch_bounds__(kThreads) void fp4_write_kernel(CacheRowsArgs a, in
 #pragma unroll
   for (int u = 0; u < N; ++u) {
     const int unit = u * kThreads + tid, value = unit / (32 * CPR), r = unit / CPR % 32, c = unit % CPR;
-    const bool on = s.t0 + r >= s.lo && s.t0 + r < s.hi;
     float top = 0.0f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(f[u][e]));
     top = fmaxf(top, __shfl_xor(top, 1));
     top = fmaxf(top, __shfl_xor(top, 2));
     const uint32_t ex = fp4_exponent(top);
-    const uint32_t w = fp4_encode(f[u], fp4_step(ex));
-    const uint32_t other = (uint32_t)__shfl_xor((int)w, 2);        // the channels 16 further on, or back
-    if (c % 4 == 0 && on)
-      s.page[(value ? Pg::value_steps(size) : Pg::key_steps(size)) + (slot + r) * Pg::NB + c / 4] = (char)ex;
-    if (value == 0) {
-      if (on) *reinterpret_cast<uint32_t*>(s.page + (slot + r) * (D / 2) + c * 4) = w;
-    } else {
-      // entries i = 8 (c % 2) + 0 .. 7: the lane of the lower channels does the even ones, its partner the odd
-      const int q = c % 4;
-      const uint32_t bytes = q < 2 ? (w & 0x0f0f0f0fu) | (other & 0x0f0f0f0fu) << 4
-                                   : (other >> 4 & 0x0f0f0f0fu) | (w & 0xf0f0f0f0u);
-      uint8_t* to = vt + r / 8 * Pg::kTile;
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        to[Pg::entry(r % 8, c / 4, 8 * (q & 1) + 2 * j + (q >> 1))] = (uint8_t)(bytes >> 8 * j);
-    }
-  }
-  __syncthreads();
-  char* to = s.page + Pg::values(size) + slot * (D / 2) + tid * COPY;
-  const uint8_t* from = vt + tid * COPY;
-  if (s.hi - s.lo == 32) {
-    if constexpr (COPY == 8) *reinterpret_cast<u32x2*>(to) = *reinterpret_cast<const u32x2*>(from);
-    if constexpr (COPY == 4) *reinterpret_cast<uint32_t*>(to) = *reinterpret_cast<const uint32_t*>(from);
-    if constexpr (COPY == 2) *reinterpret_cast<uint16_t*>(to) = *reinterpret_cast<const uint16_t*>(from);
-    return;
-  }
-#pragma unroll
-  for (int i = 0; i < COPY; ++i) {
-    const int at = tid * COPY + i, t = s.t0 + at / Pg::kTile * 8 + at / Pg::P % 8;
-    if (t >= s.lo && t < s.hi) to[i] = (char)from[i];
+    if (s.t0 + r < s.lo || s.t0 + r >= s.hi) continue;
+    *reinterpret_cast<uint32_t*>(s.page + Pg::codes(value, size) + (slot + r) * (D / 2) + c * 4) =
+        fp4_encode(f[u], fp4_step(ex));
+    if (c % 4 == 0) s.page[Pg::steps(value, size) + (slot + r) * Pg::NB + c / 4] = (char)ex;
   }
 }
 
@@ -140,42 +109,26 @@ __global__ __launch_bounds__(kThreads) void fp4_read_kernel(CacheRowsArgs a, int
   using Pg = Fp4Page<D>;
   constexpr int CPR = D / 8, E = DT == BF16 ? 2 : 4;
   constexpr int N = 2 * 32 * CPR / kThreads;
-  constexpr int COPY = 16 * D / kThreads;
-  __shared__ __attribute__((aligned(16))) uint8_t vt[16 * D];
   const Span s = span_of(a, tiles);
   const int tid = threadIdx.x, size = 1 << a.c.page_log2, slot = s.t0 & (size - 1);
-  const bool some = s.page != nullptr;             // the same for the whole workgroup
   uint32_t w[N], ex[N];
-  if (some) {
-    const char* from = s.page + Pg::values(size) + slot * (D / 2) + tid * COPY;
-    uint8_t* to = vt + tid * COPY;
-    if constexpr (COPY == 8) *reinterpret_cast<u32x2*>(to) = *reinterpret_cast<const u32x2*>(from);
-    if constexpr (COPY == 4) *reinterpret_cast<uint32_t*>(to) = *reinterpret_cast<const uint32_t*>(from);
-    if constexpr (COPY == 2) *reinterpret_cast<uint16_t*>(to) = *reinterpret_cast<const uint16_t*>(from);
-#pragma unroll
-    for (int u = 0; u < N; ++u) {
-      const int unit = u * kThreads + tid, value = unit / (32 * CPR), r = unit / CPR % 32, c = unit % CPR;
-      ex[u] = (uint8_t)s.page[(value ? Pg::value_steps(size) : Pg::key_steps(size)) + (slot + r) * Pg::NB + c / 4];
-      w[u] = value ? 0 : *reinterpret_cast<const uint32_t*>(s.page + (slot + r) * (D / 2) + c * 4);
-    }
-  }
-  __syncthreads();
 #pragma unroll
   for (int u = 0; u < N; ++u) {
     const int unit = u * kThreads + tid, value = unit / (32 * CPR), r = unit / CPR % 32, c = unit % CPR;
-    const int t = s.t0 + r;
-    if (t < s.start || t - s.start >= a.n) continue;
-    const bool on = some && t < s.hi;
-    if (value && on) {
-      const uint8_t* from = vt + r / 8 * Pg::kTile;
-      const int q = c % 4;
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        w[u] |= (uint32_t)(from[Pg::entry(r % 8, c / 4, 8 * (q & 1) + j)] >> 4 * (q >> 1) & 15) << 4 * j;
+    w[u] = 0;
+    ex[u] = 127;
+    if (s.page != nullptr && s.t0 + r < s.hi) {
+      w[u] = *reinterpret_cast<const uint32_t*>(s.page + Pg::codes(value, size) + (slot + r) * (D / 2) + c * 4);
+      ex[u] = (uint8_t)s.page[Pg::steps(value, size) + (slot + r) * Pg::NB + c / 4];
     }
+  }
+#pragma unroll
+  for (int u = 0; u < N; ++u) {
+    const int unit = u * kThreads + tid, value = unit / (32 * CPR), r = unit / CPR % 32, c = unit % CPR;
+    const int i = s.t0 + r - s.start;
+    if (i < 0 || i >= a.n) continue;
     const Rows& x = value ? a.v : a.k;
-    store8<DT>(x.p + s.b * x.sb + s.hk * x.sh + (long long)(t - s.start) * x.sn + c * 8 * E, on ? w[u] : 0,
-               fp4_step(on ? ex[u] : 127));
+    store8<DT>(x.p + s.b * x.sb + s.hk * x.sh + i * x.sn + c * 8 * E, w[u], fp4_step(ex[u]));
   }
 }
 

@@ -9,19 +9,12 @@
 
 namespace mra {
 
-// Offsets in bytes within a page of one head, of `size` tokens.
+// Offsets in bytes within a page of one head, of `size` tokens; x = 0: keys, 1: values.
 template <int D>
 struct Fp4Page {
-  static constexpr int P = D == 32 ? 1 : 2;        // blocks of 32 channels that lie together in `values`
   static constexpr int NB = D / 32;                // blocks, and step bytes, of a token
-  static constexpr int kTile = 4 * D;              // values of eight tokens
-  static __device__ __forceinline__ long long values(int size) { return (long long)size * (D / 2); }
-  static __device__ __forceinline__ long long key_steps(int size) { return (long long)size * D; }
-  static __device__ __forceinline__ long long value_steps(int size) { return (long long)size * (D + NB); }
-  // of token r (0 to 7) of a tile of values, block b, entry i (channels 32 b + i and + 16)
-  static __device__ __forceinline__ constexpr int entry(int r, int b, int i) {
-    return ((i * (NB / P) + b / P) * 8 + r) * P + b % P;
-  }
+  static __device__ __forceinline__ int codes(int x, int size) { return x * size * (D / 2); }
+  static __device__ __forceinline__ int steps(int x, int size) { return size * (D + x * NB); }
 };
 
 // The page of a head that holds token t of sequence b (t below the table's end), or null.

@@ -77,12 +77,9 @@ def test_written_and_read_back(gpu, case):
     for b in range(B):
         t = torch.arange(int(c0[b]), device="cuda") + int(s0[b])
         used[table[b].long()[t // page], t % page] = True
-    P, NB, half = min(2, d // 32), d // 32, page * d // 2
-    masks = [used[:, :, None].expand(-1, -1, d // 2).reshape(len(used), -1),
-             used.view(-1, page // 8, 1, 8, 1).expand(-1, -1, 16 * NB // P, 8, P).reshape(len(used), -1),
-             used[:, :, None].expand(-1, -1, NB).reshape(len(used), -1)]
-    mask = torch.cat(masks + masks[2:], 1)[:, None].expand_as(before)
-    assert mask.shape[2] == cache.data.shape[2] and masks[0].shape[1] == half
+    parts = [used[:, :, None].expand(-1, -1, x).reshape(len(used), -1) for x in (d // 2, d // 2, d // 32, d // 32)]
+    mask = torch.cat(parts, 1)[:, None].expand_as(before)
+    assert mask.shape[2] == cache.data.shape[2]
     assert torch.equal(cache.data[~mask], before[~mask])
 
 
@@ -93,7 +90,7 @@ def test_the_bytes_are_the_layouts(gpu, d):
     cache = gpu.fp4_cache(3, 2, 64, d)
     gpu.fp4_cache_write(cache, k, v, ints(2)[None])
     for h in range(2):
-        want = L.page_bytes(k[0, h].cpu(), v[0, h].cpu(), 64)
+        want = L.page_bytes(k[0, h].cpu(), v[0, h].cpu())
         got = cache.data[2, h].cpu()
         # a zero may carry a sign: codes 8 and 0
         codes = 64 * d

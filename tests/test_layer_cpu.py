@@ -304,24 +304,15 @@ def test_oracle_holds_by_hand():
 @pytest.mark.parametrize("size", [32, 64, 1024])
 def test_what_a_tile_addresses_lies_in_its_page(d, size):
     """The byte ranges of the kernels' loads and stores of a tile of 32 tokens at the last place of a page."""
-    nb, p = d // 32, min(2, d // 32)
+    nb = d // 32
     total = size * (d + d // 16)
     assert total == ops.fp4_page_bytes(size, d) and total % 16 == 0
     slot = size - 32
-    keys, values = 0, size * (d // 2)
-    ke, ve = size * d, size * (d + nb)
-    assert (slot + 31) * (d // 2) + (d // 8 - 1) * 4 + 4 <= values              # write, read: a dword of keys
-    assert (slot + 31) * (d // 2) + (nb - 1) * 16 + 16 <= values                # attention: 16 bytes
-    assert values + slot * (d // 2) + 16 * d <= ke                              # a tile of values
-    assert ke + (slot + 31) * nb + nb - 1 < ve and ve + (slot + 31) * nb + nb - 1 < total
-    assert ve + (slot + 24) * nb + 8 * nb <= total                              # the steps of eight tokens
-    for off in (values, ke, ve):
-        assert off % 16 == 0
-    entries = sorted(((i * (nb // p) + b // p) * 8 + r) * p + b % p for i in range(16) for b in range(nb) for r in range(8))
-    assert entries == list(range(4 * d))                                        # each byte of eight tokens' values once
-    # the write kernel's partial copy finds the token of a byte
-    for i in range(16):
-        for b in range(nb):
-            for r in range(8):
-                at = ((i * (nb // p) + b // p) * 8 + r) * p + b % p
-                assert at // (4 * d) * 8 + at // p % 8 == r
+    codes, steps = (0, size * (d // 2)), (size * d, size * (d + nb))
+    ends = (codes[1], steps[0], steps[1], total)
+    for x in (0, 1):
+        assert codes[x] + (slot + 31) * (d // 2) + (d // 8 - 1) * 4 + 4 <= ends[x]          # write, read: a dword
+        assert codes[x] + (slot + 31) * (d // 2) + (nb - 1) * 16 + 16 <= ends[x]            # many rows: 16 bytes
+        assert codes[x] + (slot + 31) * (d // 2) + 3 * (d // 8) + d // 8 <= ends[x]         # few rows: d / 8 bytes
+        assert steps[x] + (slot + 31) * nb + nb - 1 < ends[2 + x]
+        assert codes[x] % 16 == 0 and steps[x] % 16 == 0
