@@ -26,6 +26,26 @@ __device__ __forceinline__ int first_query(const CacheAttentionArgs& a, int b, i
   return a.q_start == nullptr ? keys - a.nq : min(max(a.q_start[b], -kFar), kFar);
 }
 
+// The pages of up to 64 tiles of 32 keys, every STEP-th from tile `first` on: a lane holds one entry of the table,
+// loaded once for all of them, so that no step of a loop waits for the table.
+template <int STEP>
+struct PageList {
+  int entry, first;
+  __device__ __forceinline__ void load(const CacheArgs& c, int b, int tile, int end) {
+    first = tile;
+    const int t = tile + lane_id() * STEP;
+    entry = t < end ? c.table[(long long)b * c.max_pages + (t >> (c.page_log2 - 5))] : -1;
+    wait_loads<0>();                               // here, not at each use beside the loads in flight
+  }
+  // Of tile t (wave-uniform, first + STEP i); tiles up to `end` exist. Null: no page.
+  __device__ __forceinline__ const char* get(const CacheArgs& c, int b, int hk, int t, int end) {
+    if (t >= end) return nullptr;
+    if (t - first >= 64 * STEP) load(c, b, t, end);
+    const int page = __builtin_amdgcn_readlane(entry, (t - first) / STEP);
+    return (unsigned)page < (unsigned)c.pages ? c.data + ((long long)page * c.Hkv + hk) * c.head_bytes : nullptr;
+  }
+};
+
 // A stage's 64 keys of one head on their way from the cache to LDS, by T threads.
 template <int D, int T>
 struct CacheStage {
@@ -268,14 +288,16 @@ struct CacheTile {
     return value ? 16 * x + i : 8 * (i >> 2) + 4 * x + (i & 3);
   }
 
+  // A lane's offsets are the same for every tile: uniform bases, so that a load needs no vector instruction.
   __device__ __forceinline__ void load(const char* page, int slot, int size) {
     const int g = lane_id() >> 4;
 #pragma unroll
-    for (int v = 0; v < 2; ++v)
+    for (int v = 0; v < 2; ++v) {
+      const char* codes = page + (Pg::codes(v, size) + slot * (D / 2));
+      const char* steps = page + (Pg::steps(v, size) + slot * Pg::NB);
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        const int r = slot + row(v, x);
-        const char* p = page + Pg::codes(v, size) + r * (D / 2) + g * (D / 8);
+        const char* p = codes + (uint32_t)(row(v, x) * (D / 2) + g * (D / 8));
         if constexpr (D == 128) {
           const u32x4 q = *reinterpret_cast<const u32x4*>(p);
 #pragma unroll
@@ -287,8 +309,9 @@ struct CacheTile {
         } else {
           w[v][x][0] = *reinterpret_cast<const uint32_t*>(p);
         }
-        e[v][x] = (uint8_t)page[Pg::steps(v, size) + r * Pg::NB + g * Pg::NB / 4];
+        e[v][x] = (uint8_t)steps[(uint32_t)(row(v, x) * Pg::NB + g * Pg::NB / 4)];
       }
+    }
   }
 };
 
@@ -435,18 +458,19 @@ __global__ __launch_bounds__(W * kWave) void fp4_token_kernel(CacheAttentionArgs
   TokenRows<NP, D> row;
   row.load_queries(a.q.p + b * a.q.sb + h * a.q.sh + i * a.q.sn, m < rows);
   row.init();
-  auto page_of = [&](int t) { return t < t1 ? fp4_page(a.c, b, hk, 32 * t) : nullptr; };
+  PageList<W> list;
+  list.load(a.c, b, t0 + w, t1);
+  auto page_of = [&](int t) { return list.get(a.c, b, hk, t, t1); };
   ValueTile<D> values[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) values[u].init(lds + (w * U + u) * 64 * D);
   CacheTile<D> next[U];
-  const char *page[U], *ahead[U];                  // of the tiles in next, and of those behind them
+  const char* page[U];                             // of the tiles in next
   int t = t0 + w;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     page[u] = page_of(t + u * W);
     if (page[u] != nullptr) next[u].load(page[u], 32 * (t + u * W) & (size - 1), size);
-    ahead[u] = page_of(t + (U + u) * W);
   }
   for (; t < t1; t += U * W) {
     CacheTile<D> tile[U];
@@ -455,9 +479,8 @@ __global__ __launch_bounds__(W * kWave) void fp4_token_kernel(CacheAttentionArgs
     for (int u = 0; u < U; ++u) {
       tile[u] = next[u];
       some[u] = page[u] != nullptr;
-      page[u] = ahead[u];
+      page[u] = page_of(t + (U + u) * W);
       if (page[u] != nullptr) next[u].load(page[u], 32 * (t + (U + u) * W) & (size - 1), size);
-      ahead[u] = page_of(t + (2 * U + u) * W);
     }
     float s[U][8];
 #pragma unroll
@@ -550,19 +573,25 @@ __global__ __launch_bounds__(W * kWave) void fp4_token_kernel(CacheAttentionArgs
 // Waves of fp4_rows_kernel: eight where a stage's conversion costs most and registers allow it.
 constexpr int row_waves(int np, int d) { return np == 1 && d == 128 ? 8 : 4; }
 
-// The token kernel serves up to 64 rows a key head. Where the rows' workgroups are fewer than two
-// per CU several share the keys of the same rows, each at least 256 (512 of the shared-tile kernel).
+// The token kernel serves up to 64 rows a key head, and more where its tiles (16 rows x keys) are few: the other's
+// stages take 2 to 3 us however little there is to do (bfloat16, d = 64, us; rows kernel, token kernel):
+//   64 heads x 4096 keys, 16 rows: 20, 13   64 rows: 23, 21   96 rows: 25, 24   128 rows: 26, 28
+//   8 heads x 4096 keys, 128 rows: 17, 12   256 rows: 19, 15   512 rows: 21, 20
+//   4 heads x 16384 keys, 128 rows: 19, 16   256 rows: 23, 21   512 rows: 31, 33
+// Where the rows' workgroups are fewer than two per CU (one of eight waves) several share the keys of the same
+// rows, each at least 256.
 CachePlan cache_plan(int B, int Hkv, long long rows, int cap, int d, int dtype) {
   CachePlan p{};
-  p.few = rows <= 64;
+  const long long heads = (long long)B * Hkv, tiles = heads * ((rows + kTokenRows - 1) / kTokenRows);
+  p.few = rows <= 64 || tiles <= (1 << 20) / (cap > 0 ? cap : 1);
   const int waves = p.few ? kTokenWaves : row_waves(dtype == BF16 ? 1 : 3, d);
   p.mtiles = (int)(p.few ? (rows + kTokenRows - 1) / kTokenRows : (rows + 32 * waves - 1) / (32 * waves));
-  const long long wgs = (long long)B * Hkv * p.mtiles, most = p.few ? (cap + 255) / 256 : (cap + 511) / 512;
+  const long long wgs = heads * p.mtiles, most = (cap + 255) / 256;
   long long want = ((waves == 8 ? 1 : 2) * kCus + wgs - 1) / wgs;
   if (want > most) want = most;
   if (want > 64) want = 64;
   p.splits = want > 1 ? (int)want : 1;
-  if (p.splits > 1) p.bytes = (size_t)p.splits * B * Hkv * rows * (d + 2) * sizeof(float);
+  if (p.splits > 1) p.bytes = (size_t)p.splits * heads * rows * (d + 2) * sizeof(float);
   return p;
 }
 
