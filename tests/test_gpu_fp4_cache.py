@@ -146,7 +146,9 @@ def test_bad_pages(gpu):
     kr, vr = gpu.fp4_cache_read(cache, bad, m * page)
     for got, x in ((kr, k), (vr, v)):
         assert torch.equal(got.double(), torch.where(ok[:, None, :, None], L.held(x)[0], 0.0))
-    for nq in (1, 5, 70):
+    for nq, wide in ((1, 0), (5, 0), (70, 0), (70, 1 << 20)):
+        if wide:
+            bad = torch.cat([bad, torch.full((B, wide // page), -1, dtype=torch.int32, device="cuda")], 1)
         q = rows(gen, "bf16", B, 4, nq, d, spread=False)
         lengths = ints(m * page, m * page - 3)
         lse = torch.empty(B, 4, nq, device="cuda")
@@ -156,7 +158,7 @@ def test_bad_pages(gpu):
 
 
 def attend(gpu, seed, dt, B, H, Hkv, nq, nk, d, page, layout="bhnd", causal=True, ragged=True, start=None, scale=None,
-           kv="bf16", empty=False):
+           kv="bf16", empty=False, wide=0):
     gen = torch.Generator("cuda").manual_seed(seed)
     k, v = rows(gen, kv, B, Hkv, nk, d, spread=False), rows(gen, kv, B, Hkv, nk, d, spread=False)
     q = rows(gen, dt, B, H, nq, d, layout, spread=False)
@@ -164,6 +166,8 @@ def attend(gpu, seed, dt, B, H, Hkv, nq, nk, d, page, layout="bhnd", causal=True
     cache = gpu.fp4_cache(B * m + 1, Hkv, page, d)
     cache.data.fill_(255)                                  # behind the sequences lies anything
     table = table_of(gen, B, m, B * m + 1)
+    if wide:                                               # entries that no length reaches
+        table = torch.cat([table, torch.full((B, wide // page - m), -1, dtype=torch.int32, device="cuda")], 1)
     lengths = torch.full((B,), nk, dtype=torch.int32, device="cuda")
     if ragged:
         lengths = torch.randint(0, nk + 1, (B,), generator=gen, device="cuda", dtype=torch.int32)
@@ -210,22 +214,31 @@ ATTENDS = [
     ("f32", 1, 40, 8, 1, 9000, 64, 512, dict(kv="f32")),
     ("bf16", 1, 2, 2, 600, 1100, 128, 64, {}),
     ("bf16", 16, 32, 8, 90, 200, 32, 32, {}),
+    ("bf16", 40, 32, 16, 70, 130, 64, 32, {}),
+    ("f32", 40, 16, 16, 70, 130, 64, 32, dict(empty=True)),
+    ("bf16", 24, 32, 16, 130, 140, 128, 64, dict(layout="bnhd")),
+    ("f32", 40, 16, 16, 66, 100, 128, 32, dict(start=(-30, 90))),
+    ("f32", 40, 32, 16, 65, 70, 32, 32, dict(causal=False)),
 ]
 
 
+# a table with room for 2^20 tokens: more workgroups share the keys, and from 65 rows a key head on the kernel
+# for many rows runs
+@pytest.mark.parametrize("wide", [0, 1 << 20])
 @pytest.mark.parametrize("case", range(len(ATTENDS)))
-def test_attention(gpu, case):
+def test_attention(gpu, case, wide):
     dt, B, H, Hkv, nq, nk, d, page, opts = ATTENDS[case]
-    print("attend", ATTENDS[case], flush=True)
-    attend(gpu, 50 + case, dt, B, H, Hkv, nq, nk, d, page, **opts)
+    print("attend", ATTENDS[case], wide, flush=True)
+    attend(gpu, 50 + case, dt, B, H, Hkv, nq, nk, d, page, wide=wide, **opts)
 
 
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
-@pytest.mark.parametrize("nq", [1, 40])
-def test_logits_of_hundreds(gpu, dt, nq):
-    """Rising, falling and level runs of large logits: the reference has to move."""
+@pytest.mark.parametrize("nq,wide", [(1, 0), (40, 0), (140, 1 << 20)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_logits_of_hundreds(gpu, dt, nq, wide, d):
+    """Rising and falling runs of large logits: the reference has to move."""
     gen = torch.Generator("cuda").manual_seed(7)
-    d, n = 64, 1500
+    n = 1500
     q = torch.zeros(1, 2, nq, d, device="cuda")
     q[..., 0] = 8.0
     q[:, 1, :, 0] = -8.0
@@ -233,7 +246,8 @@ def test_logits_of_hundreds(gpu, dt, nq):
     k[..., 0] = torch.linspace(-500, 500, n, device="cuda")
     v = torch.randn(1, 2, n, d, generator=gen, device="cuda")
     cache = gpu.fp4_cache(n // 32 + 1, 2, 32, d)
-    table = torch.arange(n // 32 + 1, dtype=torch.int32, device="cuda")[None]
+    table = torch.full((1, max(n, wide) // 32 + 1), -1, dtype=torch.int32, device="cuda")
+    table[0, : n // 32 + 1] = torch.arange(n // 32 + 1)
     gpu.fp4_cache_write(cache, k, v, table)
     lse = torch.empty(1, 2, nq, device="cuda")
     q = q.to(DT[dt])
@@ -252,11 +266,11 @@ def test_lengths_beyond_the_table_are_its_end(gpu):
 
 def test_results_do_not_depend_on_where_the_pages_lie(gpu):
     gen = torch.Generator("cuda").manual_seed(13)
-    for nq in (1, 60):
-        q, cache, table, lengths, z, _ = attend(gpu, 14, "bf16", 3, 8, 2, nq, 700, 64, 32)
+    for nq, wide in ((1, 0), (60, 0), (60, 1 << 20)):
+        q, cache, table, lengths, z, _ = attend(gpu, 14, "bf16", 3, 8, 2, nq, 700, 64, 32, wide=wide)
         order = torch.randperm(cache.data.shape[0], generator=gen, device="cuda")
         moved = gpu.Fp4Cache(cache.data[order].contiguous(), 32, 64)
-        there = torch.argsort(order)[table.long()].to(torch.int32)
+        there = torch.where(table < 0, -1, torch.argsort(order)[table.long().clamp(min=0)]).to(torch.int32)
         assert torch.equal(gpu.fp4_cache_attention(q, moved, there, lengths, causal=True), z)
 
 
@@ -372,7 +386,9 @@ def test_a_cache_past_32_bits(gpu):
     gpu.fp4_cache_write(cache, k, v, table)
     kr, vr = gpu.fp4_cache_read(cache, table, 1500)
     assert torch.equal(kr.double(), L.held(k)[0]) and torch.equal(vr.double(), L.held(v)[0])
-    for nq in (1, 50):
+    for nq, wide in ((1, 0), (50, 1 << 10)):
+        if wide:
+            table = torch.cat([table, table[:, :1].expand(1, wide)], 1)
         q = rows(gen, "bf16", 1, 16, nq, d, spread=False)
         lse = torch.empty(1, 16, nq, device="cuda")
         z = gpu.fp4_cache_attention(q, cache, table, ints(1500), causal=True, lse_out=lse)
