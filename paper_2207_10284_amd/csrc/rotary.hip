@@ -99,21 +99,12 @@ struct Tile {
   }
 };
 
-// cos and sin (times the magnitude) of the tile's tokens and frequencies, and each token's
-// batch and place.
-__device__ __forceinline__ void fill_angles(const RotaryArgs& a, long long first, int tokens, float2* cs, int2* at) {
-  const int half = a.rot / 2;
-  if ((int)threadIdx.x < tokens) {
-    const long long t = first + threadIdx.x;
-    const long long b = t / a.n;
-    at[threadIdx.x] = int2{(int)b, (int)(t - b * a.n)};
-  }
-  if (half == 0) return;
-  // half is a multiple of eight, at most 64, not always a power of two
+// cos and sin (times the magnitude) of the tile's tokens and frequencies. Tokens are below 2^24.
+__device__ __forceinline__ void fill_angles(const RotaryArgs& a, int first, int tokens, float2* cs) {
+  const int half = a.rot / 2;                      // a multiple of eight, at most 64, not always a power of two
   for (int i = threadIdx.x; i < tokens * half; i += kThreads) {
     const int t = i / half, f = i - t * half;
-    const long long g = first + t, b = g / a.n;
-    const int n = (int)(g - b * a.n);
+    const int b = (first + t) / a.n, n = first + t - b * a.n;
     const int pos = a.positions == nullptr ? n : a.positions[b * a.positions_stride + n];
     double turns = (double)pos * (a.freqs[f] * 0.15915494309189535);
     turns -= rint(turns);
@@ -134,71 +125,107 @@ __device__ __forceinline__ void read_angles(const float2* cs, int token, int hal
   }
 }
 
-// Row r of a side's tile: its token and head.
-__device__ __forceinline__ int2 row_of(const RotarySide& s, int r, int tokens) {
-  if (s.head_fast) {
-    const int t = r / s.heads;
-    return int2{t, r - t * s.heads};
+// Where row r of a side's tile lies: its token in the tile, batch, place in the batch, head.
+struct RowAt {
+  int token, b, i, h;
+  __device__ __forceinline__ RowAt(const RotaryArgs& a, const RotarySide& s, int first, int tokens, int r) {
+    if (s.head_fast) {
+      token = r / s.heads;
+      h = r - token * s.heads;
+    } else {
+      h = r / tokens;
+      token = r - h * tokens;
+    }
+    b = (first + token) / a.n;
+    i = first + token - b * a.n;
   }
-  const int h = r / tokens;
-  return int2{r - h * tokens, h};
-}
+  __device__ __forceinline__ long long in(const Rows& x) const { return b * x.sb + h * x.sh + i * x.sn; }
+};
 
-__device__ __forceinline__ long long row_offset(const Rows& r, const int2& at, int h) {
-  return at.x * r.sb + h * r.sh + at.y * r.sn;
+// Both sides' weights as float32 in LDS, and a lane's sixteen of one.
+template <size_t D>
+__device__ __forceinline__ void fill_weights(const RotaryArgs& a, float (&ws)[2][D]) {
+  const int x = threadIdx.x / (int)D, e = threadIdx.x % (int)D;
+  if (x > 1 || a.side[x].w == nullptr) return;
+  ws[x][e] = a.weight_bf16 ? bf16_to_f32(static_cast<const uint16_t*>(a.side[x].w)[e])
+                           : static_cast<const float*>(a.side[x].w)[e];
 }
-
-template <int DT, int D>
-__device__ __forceinline__ void load_weight(const RotaryArgs& a, const void* w, int e0, int e1, float (&f)[16]) {
+template <size_t D>
+__device__ __forceinline__ void read_weights(const float (&ws)[D], int e0, int e1, float (&f)[16]) {
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const int e = i < 8 ? e0 + i : e1 + i - 8;
-    f[i] = a.weight_bf16 ? bf16_to_f32(static_cast<const uint16_t*>(w)[e]) : static_cast<const float*>(w)[e];
+  for (int i = 0; i < 4; ++i) {
+    const f32x4 v = *reinterpret_cast<const f32x4*>(&ws[(i < 2 ? e0 : e1) + 4 * (i % 2)]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f[4 * i + j] = v[j];
   }
 }
 
 }  // namespace
 
-template <int DT, int D, bool INTER>
+// U rows of a lane, on their way from memory.
+template <int DT, int U>
+struct Batch {
+  static constexpr int E = DT == BF16 ? 2 : 4;
+  Chunk<DT> c[U][2];
+  int token[U];
+  long long to[U];
+
+  template <int D>
+  __device__ __forceinline__ void load(const RotaryArgs& a, const RotarySide& s, const Rows& from, const Tile<D>& t,
+                                       int first, int tokens, int r0, int rows) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int r = r0 + u * Tile<D>::ROWS;
+      if (r >= rows) break;                        // the same for all lanes of a row
+      const RowAt at(a, s, first, tokens, r);
+      const char* p = from.p + at.in(from);
+      c[u][0].load(p + t.e0 * E);
+      c[u][1].load(p + t.e1 * E);
+      token[u] = at.token;
+      to[u] = at.in(s.y);
+    }
+  }
+};
+
+template <int DT, int D, bool INTER, bool NORM>
 __global__ __launch_bounds__(kThreads) void rotary_forward_kernel(RotaryArgs a, int tile) {
   using T = Tile<D>;
   constexpr int E = DT == BF16 ? 2 : 4;
-  constexpr int U = 2;                             // rows of a lane in flight
+  // Rows of a lane in flight (8 x 24 heads x 4096 x 64 bfloat16: one 46, four 42 us; float32 4 x 10 x 2999 x 128: 25, 29;
+  // with a norm 20 x 32768 x 128 bfloat16: no difference)
+  constexpr int U = NORM || DT == F32 ? 1 : 4;
   __shared__ __attribute__((aligned(16))) float2 cs[kMaxTile * (D / 2)];
-  __shared__ int2 at[kMaxTile];
+  __shared__ __attribute__((aligned(16))) float ws[2][NORM ? D : 4];
   T t;
   t.init(a.rot, INTER);
-  const long long first = (long long)blockIdx.x * tile;
-  const int tokens = (int)min((long long)tile, a.tokens - first), half = a.rot / 2;
-  fill_angles(a, first, tokens, cs, at);
-  __syncthreads();
+  const int first = blockIdx.x * tile, tokens = min(tile, (int)a.tokens - first), half = a.rot / 2;
+  bool filled = false;
 #pragma unroll
   for (int x = 0; x < 2; ++x) {
     const RotarySide& s = a.side[x];
     const int rows = tokens * s.heads;
     if (rows == 0) continue;
+    int r0 = t.row;
+    Batch<DT, U> in;
+    in.load(a, s, s.x, t, first, tokens, r0, rows);
+    if (!filled) {                                 // beside the first rows' loads
+      fill_angles(a, first, tokens, cs);
+      if constexpr (NORM) fill_weights(a, ws);
+      __syncthreads();
+      filled = true;
+    }
     float w[16];
-    if (s.w != nullptr) load_weight<DT, D>(a, s.w, t.e0, t.e1, w);
-    for (int r0 = t.row; r0 < rows; r0 += U * T::ROWS) {
-      Chunk<DT> in[U][2];
-      long long to[U];
-      int token[U];
+    const bool norm = NORM && s.w != nullptr;
+    if (norm) read_weights(ws[x], t.e0, t.e1, w);
+    for (; r0 < rows; r0 += U * T::ROWS) {
+      if (r0 != t.row) in.load(a, s, s.x, t, first, tokens, r0, rows);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int2 rh = row_of(s, min(r0 + u * T::ROWS, rows - 1), tokens);
-        const int2 bi = at[rh.x];
-        const char* p = s.x.p + row_offset(s.x, bi, rh.y);
-        in[u][0].load(p + t.e0 * E);
-        in[u][1].load(p + t.e1 * E);
-        to[u] = row_offset(s.y, bi, rh.y);
-        token[u] = rh.x;
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
+        if (r0 + u * T::ROWS >= rows) break;
         float v[16];
-        in[u][0].get(v);
-        in[u][1].get(v + 8);
-        if (s.w != nullptr) {
+        in.c[u][0].get(v);
+        in.c[u][1].get(v + 8);
+        if (norm) {
           float sum = 0.0f;
 #pragma unroll
           for (int i = 0; i < 16; ++i) sum = fmaf(v[i], v[i], sum);
@@ -208,28 +235,27 @@ __global__ __launch_bounds__(kThreads) void rotary_forward_kernel(RotaryArgs a, 
         }
         if (t.c < t.pairs) {
           float2 c[8];
-          read_angles<D>(cs, token[u], half, t.c, c);
+          read_angles<D>(cs, in.token[u], half, t.c, c);
           turn<INTER>(v, c, 1.0f);
         }
-        if (u == 0 || r0 + u * T::ROWS < rows) {
-          char* p = s.y.p + to[u];
-          store_chunk<DT>(p + t.e0 * E, v);
-          store_chunk<DT>(p + t.e1 * E, v + 8);
-        }
+        char* p = s.y.p + in.to[u];
+        store_chunk<DT>(p + t.e0 * E, v);
+        store_chunk<DT>(p + t.e1 * E, v + 8);
       }
     }
   }
 }
 
 // Each workgroup takes every gridDim.x-th tile and leaves one row of sums of g y per side.
-template <int DT, int D, bool INTER>
+template <int DT, int D, bool INTER, bool NORM>
 __global__ __launch_bounds__(kThreads) void rotary_backward_kernel(RotaryArgs a, int tile) {
   using T = Tile<D>;
   constexpr int E = DT == BF16 ? 2 : 4;
-  constexpr int U = DT == BF16 ? 2 : 1;
+  // with a norm, 20 heads x 32768 x 128 bfloat16: one row in flight 118, two 112, three 108 us
+  constexpr int U = DT == BF16 ? 3 : 2;
   __shared__ __attribute__((aligned(16))) float2 cs[kMaxTile * (D / 2)];
-  __shared__ int2 at[kMaxTile];
-  __shared__ __attribute__((aligned(16))) float sums[kThreads * 16];
+  __shared__ __attribute__((aligned(16))) float ws[2][NORM ? D : 4];
+  __shared__ __attribute__((aligned(16))) float sums[NORM ? kThreads * 16 : 4];
   T t;
   t.init(a.rot, INTER);
   const int half = a.rot / 2;
@@ -238,53 +264,48 @@ __global__ __launch_bounds__(kThreads) void rotary_backward_kernel(RotaryArgs a,
   for (int x = 0; x < 2; ++x)
 #pragma unroll
     for (int i = 0; i < 16; ++i) dw[x][i] = 0.0f;
-  for (long long first = (long long)blockIdx.x * tile; first < a.tokens; first += (long long)gridDim.x * tile) {
-    const int tokens = (int)min((long long)tile, a.tokens - first);
-    __syncthreads();                               // the last tile's angles have been read
-    fill_angles(a, first, tokens, cs, at);
-    __syncthreads();
+  for (int first = blockIdx.x * tile; first < a.tokens; first += gridDim.x * tile) {
+    const int tokens = min(tile, (int)a.tokens - first);
+    bool filled = false;
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
       const RotarySide& s = a.side[x];
       const int rows = tokens * s.heads;
       if (rows == 0) continue;
-      const bool norm = s.w != nullptr;
+      const bool norm = NORM && s.w != nullptr;
+      int r0 = t.row;
+      Batch<DT, U> gr, in;
+      auto load = [&] {
+        gr.load(a, s, s.g, t, first, tokens, r0, rows);
+        if (norm) in.load(a, s, s.x, t, first, tokens, r0, rows);
+      };
+      load();
+      if (!filled) {                               // beside the first rows' loads
+        __syncthreads();                           // the last tile's angles have been read
+        fill_angles(a, first, tokens, cs);
+        if (NORM && first == (int)blockIdx.x * tile) fill_weights(a, ws);
+        __syncthreads();
+        filled = true;
+      }
       float w[16];
-      if (norm) load_weight<DT, D>(a, s.w, t.e0, t.e1, w);
-      for (int r0 = t.row; r0 < rows; r0 += U * T::ROWS) {
-        Chunk<DT> gr[U][2], in[U][2];
-        long long to[U];
-        int token[U];
+      if (norm) read_weights(ws[x], t.e0, t.e1, w);
+      for (; r0 < rows; r0 += U * T::ROWS) {
+        if (r0 != t.row) load();
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          const int2 rh = row_of(s, min(r0 + u * T::ROWS, rows - 1), tokens);
-          const int2 bi = at[rh.x];
-          const char* p = s.g.p + row_offset(s.g, bi, rh.y);
-          gr[u][0].load(p + t.e0 * E);
-          gr[u][1].load(p + t.e1 * E);
-          if (norm) {
-            p = s.x.p + row_offset(s.x, bi, rh.y);
-            in[u][0].load(p + t.e0 * E);
-            in[u][1].load(p + t.e1 * E);
-          }
-          to[u] = row_offset(s.y, bi, rh.y);
-          token[u] = rh.x;
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const bool on = u == 0 || r0 + u * T::ROWS < rows;
+          if (r0 + u * T::ROWS >= rows) break;
           float g[16];
-          gr[u][0].get(g);
-          gr[u][1].get(g + 8);
+          gr.c[u][0].get(g);
+          gr.c[u][1].get(g + 8);
           if (t.c < t.pairs) {
             float2 c[8];
-            read_angles<D>(cs, token[u], half, t.c, c);
+            read_angles<D>(cs, gr.token[u], half, t.c, c);
             turn<INTER>(g, c, -1.0f);
           }
           if (norm) {
             float v[16], sum = 0.0f, dot = 0.0f;
-            in[u][0].get(v);
-            in[u][1].get(v + 8);
+            in.c[u][0].get(v);
+            in.c[u][1].get(v + 8);
 #pragma unroll
             for (int i = 0; i < 16; ++i) sum = fmaf(v[i], v[i], sum);
             const float inv = 1.0f / sqrtf(row_sum<T::L>(sum) * (1.0f / D) + a.eps);
@@ -292,23 +313,21 @@ __global__ __launch_bounds__(kThreads) void rotary_backward_kernel(RotaryArgs a,
             for (int i = 0; i < 16; ++i) {
               v[i] *= inv;
               const float gy = g[i] * v[i];
-              dw[x][i] += on ? gy : 0.0f;
+              dw[x][i] += gy;
               dot = fmaf(gy, w[i], dot);
             }
             dot = row_sum<T::L>(dot) * (1.0f / D);
 #pragma unroll
             for (int i = 0; i < 16; ++i) g[i] = inv * (g[i] * w[i] - v[i] * dot);
           }
-          if (on) {
-            char* p = s.y.p + to[u];
-            store_chunk<DT>(p + t.e0 * E, g);
-            store_chunk<DT>(p + t.e1 * E, g + 8);
-          }
+          char* p = s.y.p + gr.to[u];
+          store_chunk<DT>(p + t.e0 * E, g);
+          store_chunk<DT>(p + t.e1 * E, g + 8);
         }
       }
     }
   }
-  if (a.part == nullptr) return;
+  if (!NORM || a.part == nullptr) return;
 #pragma unroll
   for (int x = 0; x < 2; ++x) {
     if (a.side[x].w == nullptr) continue;
@@ -333,7 +352,13 @@ __global__ __launch_bounds__(kSumThreads) void rotary_weight_kernel(const float*
   void* to = x == 0 ? dq_weight : dk_weight;
   if (to == nullptr) return;
   double v = 0.0;
-  for (int r = g; r < groups; r += 32) v += part[((long long)r * 2 + x) * D + e];
+  for (int r0 = g; r0 < groups; r0 += 8 * 32) {    // eight loads under way
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = part[((long long)min(r0 + 32 * i, groups - 1) * 2 + x) * D + e];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v += r0 + 32 * i < groups ? f[i] : 0.0f;
+  }
   sums[g][i] = v;
   __syncthreads();
   if (g != 0) return;
@@ -360,9 +385,13 @@ int rotary_backward_groups(long long tokens) {
 }
 
 template <class F>
-static hipError_t rotary_variant(int d, int dtype, int interleaved, F run) {
+static hipError_t rotary_variant(const RotaryArgs& a, int d, int dtype, int interleaved, F run) {
+  auto norm = [&](auto dt, auto dd, auto inter) {
+    return a.side[0].w != nullptr || a.side[1].w != nullptr ? run(dt, dd, inter, std::true_type{})
+                                                            : run(dt, dd, inter, std::false_type{});
+  };
   auto inter = [&](auto dt, auto dd) {
-    return interleaved ? run(dt, dd, std::true_type{}) : run(dt, dd, std::false_type{});
+    return interleaved ? norm(dt, dd, std::true_type{}) : norm(dt, dd, std::false_type{});
   };
   auto width = [&](auto dt) {
     if (d == 32) return inter(dt, std::integral_constant<int, 32>{});
@@ -374,8 +403,8 @@ static hipError_t rotary_variant(int d, int dtype, int interleaved, F run) {
 
 hipError_t launch_rotary_forward(const RotaryArgs& a, int d, int dtype, int interleaved, hipStream_t stream) {
   const int tile = rotary_tile(a.tokens);
-  return rotary_variant(d, dtype, interleaved, [&](auto dt, auto dd, auto inter) {
-    rotary_forward_kernel<dt.value, dd.value, inter.value>
+  return rotary_variant(a, d, dtype, interleaved, [&](auto dt, auto dd, auto inter, auto norm) {
+    rotary_forward_kernel<dt.value, dd.value, inter.value, norm.value>
         <<<(unsigned)((a.tokens + tile - 1) / tile), kThreads, 0, stream>>>(a, tile);
     return hipGetLastError();
   });
@@ -388,8 +417,8 @@ hipError_t launch_rotary_backward(const RotaryArgs& a, int d, int dtype, int int
   // without sums to leave, a workgroup per tile
   const unsigned groups = weights ? (unsigned)rotary_backward_groups(a.tokens) : (unsigned)((a.tokens + tile - 1) / tile);
   if (a.tokens > 0) {
-    const hipError_t e = rotary_variant(d, dtype, interleaved, [&](auto dt, auto dd, auto inter) {
-      rotary_backward_kernel<dt.value, dd.value, inter.value><<<groups, kThreads, 0, stream>>>(a, tile);
+    const hipError_t e = rotary_variant(a, d, dtype, interleaved, [&](auto dt, auto dd, auto inter, auto norm) {
+      rotary_backward_kernel<dt.value, dd.value, inter.value, norm.value><<<groups, kThreads, 0, stream>>>(a, tile);
       return hipGetLastError();
     });
     if (e != hipSuccess) return e;
