@@ -11,11 +11,19 @@ namespace {
 
 constexpr int kThreads = 256;
 
+constexpr int kTokens = 64;                       // of a workgroup's tile
+
 // Which tokens of a workgroup's tile a call writes or reads.
 struct Span {
   int b, hk, t0;                          // sequence, head, first token of the tile
   int start, lo, hi;                      // the call's first token; the tile's live ones are lo to hi - 1
-  char* page;                             // null: none
+  char* page[2];                          // of the tile's halves; null: none
+
+  __device__ __forceinline__ void pages(const CacheRowsArgs& a) {
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+      page[x] = max(lo, t0 + 32 * x) < min(hi, t0 + 32 * x + 32) ? fp4_page(a.c, b, hk, t0 + 32 * x) : nullptr;
+  }
 };
 
 __device__ __forceinline__ Span span_of(const CacheRowsArgs& a, int tiles) {
@@ -25,10 +33,9 @@ __device__ __forceinline__ Span span_of(const CacheRowsArgs& a, int tiles) {
   s.hk = bh - s.b * a.c.Hkv;
   s.start = a.starts == nullptr ? 0 : min(max(a.starts[s.b], 0), a.c.cap);
   const int count = min(a.counts == nullptr ? a.n : min(max(a.counts[s.b], 0), a.n), a.c.cap - s.start);
-  s.t0 = (s.start / 32 + g - bh * tiles) * 32;
+  s.t0 = (s.start / kTokens + g - bh * tiles) * kTokens;
   s.lo = max(s.t0, s.start);
-  s.hi = min(s.t0 + 32, s.start + count);
-  s.page = s.lo < s.hi ? fp4_page(a.c, s.b, s.hk, s.t0) : nullptr;
+  s.hi = min(s.t0 + kTokens, s.start + count);
   return s;
 }
 
@@ -70,37 +77,36 @@ __device__ __forceinline__ void store8(char* p, uint32_t w, float step) {
 template <int DT, int D>
 __global__ __launch_bounds__(kThreads) void fp4_write_kernel(CacheRowsArgs a, int tiles) {
   using Pg = Fp4Page<D>;
-  constexpr int CPR = D / 8, E = DT == BF16 ? 2 : 4;
-  constexpr int N = 2 * 32 * CPR / kThreads;       // units of eight channels per lane
-  const Span s = span_of(a, tiles);
-  if (s.page == nullptr) return;
-  const int tid = threadIdx.x, size = 1 << a.c.page_log2, slot = s.t0 & (size - 1);
-  float f[N][8];
+  constexpr int CPR = D / 16, E = DT == BF16 ? 2 : 4;
+  constexpr int N = 2 * kTokens * CPR / kThreads;  // units of sixteen channels per lane
+  Span s = span_of(a, tiles);
+  if (s.lo >= s.hi) return;
+  const int tid = threadIdx.x, size = 1 << a.c.page_log2;
+  float f[N][2][8];                                // on their way while the table is looked up
 #pragma unroll
   for (int u = 0; u < N; ++u) {
-    const int unit = u * kThreads + tid, value = unit / (32 * CPR), r = unit / CPR % 32, c = unit % CPR;
+    const int unit = u * kThreads + tid, value = unit / (kTokens * CPR), r = unit / CPR % kTokens, c = unit % CPR;
     const Rows& x = value ? a.v : a.k;
-    const int t = s.t0 + r;
-    if (t >= s.lo && t < s.hi) {
-      load8<DT>(x.p + s.b * x.sb + s.hk * x.sh + (t - s.start) * x.sn + c * 8 * E, f[u]);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) f[u][e] = 0.0f;
-    }
+    const int t = min(max(s.t0 + r, s.lo), s.hi - 1);
+    const char* p = x.p + s.b * x.sb + s.hk * x.sh + (t - s.start) * x.sn + c * 16 * E;
+    load8<DT>(p, f[u][0]);
+    load8<DT>(p + 8 * E, f[u][1]);
   }
+  s.pages(a);
 #pragma unroll
   for (int u = 0; u < N; ++u) {
-    const int unit = u * kThreads + tid, value = unit / (32 * CPR), r = unit / CPR % 32, c = unit % CPR;
+    const int unit = u * kThreads + tid, value = unit / (kTokens * CPR), r = unit / CPR % kTokens, c = unit % CPR;
     float top = 0.0f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(f[u][e]));
-    top = fmaxf(top, __shfl_xor(top, 1));
-    top = fmaxf(top, __shfl_xor(top, 2));
+    for (int e = 0; e < 8; ++e) top = fmaxf(top, fmaxf(fabsf(f[u][0][e]), fabsf(f[u][1][e])));
+    top = fmaxf(top, __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(top), 0xB1, 0xF, 0xF, true)));   // lane ^ 1
     const uint32_t ex = fp4_exponent(top);
-    if (s.t0 + r < s.lo || s.t0 + r >= s.hi) continue;
-    *reinterpret_cast<uint32_t*>(s.page + Pg::codes(value, size) + (slot + r) * (D / 2) + c * 4) =
-        fp4_encode(f[u], fp4_step(ex));
-    if (c % 4 == 0) s.page[Pg::steps(value, size) + (slot + r) * Pg::NB + c / 4] = (char)ex;
+    char* page = r < 32 ? s.page[0] : s.page[1];
+    const int t = s.t0 + r, slot = t & (size - 1);
+    if (page == nullptr || t < s.lo || t >= s.hi) continue;
+    *reinterpret_cast<u32x2*>(page + Pg::codes(value, size) + slot * (D / 2) + c * 8) =
+        u32x2{fp4_encode(f[u][0], fp4_step(ex)), fp4_encode(f[u][1], fp4_step(ex))};
+    if (c % 2 == 0) page[Pg::steps(value, size) + slot * Pg::NB + c / 2] = (char)ex;
   }
 }
 
@@ -108,23 +114,26 @@ template <int DT, int D>
 __global__ __launch_bounds__(kThreads) void fp4_read_kernel(CacheRowsArgs a, int tiles) {
   using Pg = Fp4Page<D>;
   constexpr int CPR = D / 8, E = DT == BF16 ? 2 : 4;
-  constexpr int N = 2 * 32 * CPR / kThreads;
-  const Span s = span_of(a, tiles);
-  const int tid = threadIdx.x, size = 1 << a.c.page_log2, slot = s.t0 & (size - 1);
+  constexpr int N = 2 * kTokens * CPR / kThreads;
+  Span s = span_of(a, tiles);
+  s.pages(a);
+  const int tid = threadIdx.x, size = 1 << a.c.page_log2;
   uint32_t w[N], ex[N];
 #pragma unroll
   for (int u = 0; u < N; ++u) {
-    const int unit = u * kThreads + tid, value = unit / (32 * CPR), r = unit / CPR % 32, c = unit % CPR;
+    const int unit = u * kThreads + tid, value = unit / (kTokens * CPR), r = unit / CPR % kTokens, c = unit % CPR;
+    const char* page = r < 32 ? s.page[0] : s.page[1];
+    const int t = s.t0 + r, slot = t & (size - 1);
     w[u] = 0;
     ex[u] = 127;
-    if (s.page != nullptr && s.t0 + r < s.hi) {
-      w[u] = *reinterpret_cast<const uint32_t*>(s.page + Pg::codes(value, size) + (slot + r) * (D / 2) + c * 4);
-      ex[u] = (uint8_t)s.page[Pg::steps(value, size) + (slot + r) * Pg::NB + c / 4];
+    if (page != nullptr && t < s.hi) {
+      w[u] = *reinterpret_cast<const uint32_t*>(page + Pg::codes(value, size) + slot * (D / 2) + c * 4);
+      ex[u] = (uint8_t)page[Pg::steps(value, size) + slot * Pg::NB + c / 4];
     }
   }
 #pragma unroll
   for (int u = 0; u < N; ++u) {
-    const int unit = u * kThreads + tid, value = unit / (32 * CPR), r = unit / CPR % 32, c = unit % CPR;
+    const int unit = u * kThreads + tid, value = unit / (kTokens * CPR), r = unit / CPR % kTokens, c = unit % CPR;
     const int i = s.t0 + r - s.start;
     if (i < 0 || i >= a.n) continue;
     const Rows& x = value ? a.v : a.k;
@@ -132,9 +141,9 @@ __global__ __launch_bounds__(kThreads) void fp4_read_kernel(CacheRowsArgs a, int
   }
 }
 
-// Tiles of 32 that n tokens can touch.
+// Tiles that n tokens can touch.
 static unsigned row_groups(const CacheRowsArgs& a, int* tiles) {
-  *tiles = (a.n + 30) / 32 + 1;
+  *tiles = (a.n + kTokens - 2) / kTokens + 1;
   return (unsigned)((long long)a.B * a.c.Hkv * *tiles);
 }
 
