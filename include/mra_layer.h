@@ -12,7 +12,9 @@
  *   strides in elements, dense rows of d elements, each stride >= 0 and a multiple of 16
  *   bytes. Input strides may be 0. Outputs must not overlap themselves or, where
  *   not said otherwise, another argument.
- * - d is 32, 64 or 128. Everything is computed in float32 (angles in float64)
+ * - d is 32, 64 or 128; rotary calls have below 2^28 tokens (B n), attention at most 2^30
+ *   rows (B H n_q), heads are at most 2^16.
+ * - Everything is computed in float32 (angles in float64)
  *   and rounded once, if not said otherwise.
  * - Results do not change from run to run.
  */
@@ -87,9 +89,10 @@ mra_status_t mra_rotary_backward(const mra_rotary_problem_t* p, const mra_stride
  * 32 consecutive channels of a token of one head share a step s = 2^e, the
  * smallest power of two with max |x| <= 7 s, -125 <= e <= 125. x / s (exact) is
  * rounded to the nearest of 0, 1/2, 1, 3/2, 2, 3, 4, 6 and their negatives, ties
- * to the even one in this order. So no value is off by more than half the distance of
- * its neighbours (beyond 6 s: by s; beyond 2^127: it is 6 2^125), all that the cache holds is exact in
- * bfloat16, and every way to evaluate the above gives the same. NaN: unspecified.
+ * to the even one in this order, to 6 beyond it. So no value is off by more than half the
+ * distance of its neighbours (s beyond 6 s; beyond 7 2^125, infinity included, it is 6 2^125), all that
+ * the cache holds is exact in bfloat16, and every way to evaluate the above gives the same. What is held
+ * for a block with a NaN is unspecified, and finite.
  *
  * The bytes of one page of one head, page_size tokens of d channels (4 bits: codes
  * 0 to 7 in the order above, 8 more for negative ones; e is held as e + 127):

@@ -15,7 +15,7 @@ namespace {
 thread_local int g_last_hip_error = 0;
 
 constexpr int kMaxLen = 1 << 26;
-constexpr long long kMaxRows = 2147483647LL;      // row indices are 32-bit integers
+constexpr long long kMaxRows = 1LL << 30;         // row indices, rounded up to a tile, are 32-bit integers
 constexpr long long kMaxGroups = (1LL << 32) / 256 - 1;   // a launch has below 2^32 threads per dimension, 256 a workgroup
 constexpr int64_t kMaxRowStride = 1 << 25;        // bytes
 constexpr int kMaxHeads = 1 << 16;
@@ -76,8 +76,8 @@ mra_status_t check_rotary(const mra_rotary_problem_t* p) {
   }
   if (p->positions != nullptr && p->positions_stride < 0) return MRA_ERR_INVALID_ARG;
   if (p->n > kMaxLen || p->H > kMaxHeads || p->H_kv > kMaxHeads) return MRA_ERR_UNSUPPORTED;
-  // tokens, and a workgroup for each at most
-  if ((long long)p->B * p->n > kMaxGroups) return MRA_ERR_UNSUPPORTED;
+  // a workgroup for 16 tokens, where they are many
+  if ((long long)p->B * p->n > 16 * kMaxGroups) return MRA_ERR_UNSUPPORTED;
   return MRA_OK;
 }
 

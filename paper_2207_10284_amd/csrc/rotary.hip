@@ -99,7 +99,7 @@ struct Tile {
   }
 };
 
-// cos and sin (times the magnitude) of the tile's tokens and frequencies. Tokens are below 2^24.
+// cos and sin (times the magnitude) of the tile's tokens and frequencies. Tokens are below 2^28.
 __device__ __forceinline__ void fill_angles(const RotaryArgs& a, int first, int tokens, float2* cs) {
   const int half = a.rot / 2;                      // a multiple of eight, at most 64, not always a power of two
   for (int i = threadIdx.x; i < tokens * half; i += kThreads) {

@@ -130,6 +130,21 @@ def test_every_border_and_tie(gpu):
         assert kr.isfinite().all() and torch.equal(kr.bfloat16().float(), kr)
 
 
+def test_infinities_and_nan(gpu):
+    """An infinity is the largest held value, its block's steps 2^125; a NaN's block is finite."""
+    k = torch.randn(1, 1, 32, 64, device="cuda")
+    k[0, 0, 3, 5], k[0, 0, 4, 40], k[0, 0, 5, 0] = math.inf, -math.inf, math.nan
+    cache = gpu.fp4_cache(1, 1, 32, 64)
+    gpu.fp4_cache_write(cache, k, k, ints(0)[None])
+    kr, vr = gpu.fp4_cache_read(cache, ints(0)[None], 32, dtype=torch.float32)
+    top = 6 * 2.0 ** 125
+    assert kr[0, 0, 3, 5] == top and kr[0, 0, 4, 40] == -top and kr.isfinite().all() and torch.equal(kr, vr)
+    keep = torch.ones(32, 2, dtype=torch.bool, device="cuda")
+    keep[3, 0] = keep[4, 1] = keep[5, 0] = False
+    keep = keep.repeat_interleave(32, 1)
+    assert torch.equal(kr[0, 0].double()[keep], L.held(torch.nan_to_num(k, 0.0, 0.0, 0.0))[0][0, 0][keep])
+
+
 def test_bad_pages(gpu):
     """Entries outside the cache are no pages: not written, read as zeros, not attended to."""
     gen = torch.Generator("cuda").manual_seed(4)
@@ -298,6 +313,60 @@ def test_streams_and_workspace(gpu):
         got = gpu.fp4_cache_attention(q, cache, table, lengths, causal=True)
     side.synchronize()
     assert torch.equal(got, z)
+
+
+def test_two_streams_at_once(gpu):
+    """Calls on two streams, each with its own cache, share nothing."""
+    a = attend(gpu, 30, "bf16", 2, 8, 2, 1, 3000, 64, 64)
+    b = attend(gpu, 31, "f32", 2, 8, 2, 90, 1500, 128, 32, wide=1 << 20)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(5):
+        for i, (stream, (q, cache, table, lengths, _, _)) in enumerate(zip(streams, (a, b))):
+            with torch.cuda.stream(stream):
+                got[i].append(gpu.fp4_cache_attention(q, cache, table, lengths, causal=True))
+    torch.cuda.synchronize()
+    for z, want in zip(got, (a, b)):
+        assert all(torch.equal(x, want[4]) for x in z)
+
+
+def test_refusals(gpu):
+    q, cache, table, lengths, _, _ = attend(gpu, 32, "bf16", 2, 8, 2, 3, 100, 64, 32)
+    k = torch.zeros(2, 2, 5, 64, device="cuda", dtype=torch.bfloat16)
+    wide = torch.zeros(2, 2, 5, 66, device="cuda", dtype=torch.bfloat16)[..., :64]
+    for bad, match in ((dict(k=k[:1]), "share shape"), (dict(v=k[:, :1]), "share shape"), (dict(v=k.float()), "v must be"),
+                       (dict(k=wide), "dense rows"), (dict(table=table[:1]), "share shape"),
+                       (dict(table=table.long()), "int32"), (dict(table=table[0]), "int32"),
+                       (dict(starts=lengths[:1]), "starts"), (dict(counts=lengths.long()), "counts"),
+                       (dict(table=table.cpu()), "int32")):
+        a = dict(k=k, v=k, table=table)
+        extra = {n: bad.pop(n) for n in ("starts", "counts") if n in bad}
+        a.update(bad)
+        with pytest.raises(ValueError, match=match):
+            gpu.fp4_cache_write(cache, a["k"], a["v"], a["table"], **extra)
+    with pytest.raises(TypeError, match="float16"):
+        gpu.fp4_cache_write(cache, k.half(), k.half(), table)
+    with pytest.raises(TypeError, match="Half|float16"):
+        gpu.fp4_cache_read(cache, table, 4, dtype=torch.float16)
+    with pytest.raises(ValueError, match="negative"):
+        gpu.fp4_cache_read(cache, table, -1)
+    with pytest.raises(ValueError, match="k_out"):
+        gpu.fp4_cache_read(cache, table, 4, k_out=torch.empty(2, 2, 5, 64, device="cuda", dtype=torch.bfloat16))
+    with pytest.raises(ValueError, match="broadcast"):
+        gpu.fp4_cache_read(cache, table, 5, v_out=k[:1].expand(2, 2, 5, 64))
+    for bad, match in ((dict(q=q[:1]), "q must have"), (dict(q=q[:, :7]), "q must have"), (dict(q=q[..., :32]), "q must have"),
+                       (dict(lengths=lengths.long()), "lengths"), (dict(q_start=lengths[:1]), "q_start"),
+                       (dict(out=q[:1].expand_as(q)), "broadcast"), (dict(out=q.float()), "out must be"),
+                       (dict(lse_out=torch.empty(2, 8, 4, device="cuda")), "lse_out"),
+                       (dict(workspace=torch.empty(9, 2, device="cuda")[:, 0]), "workspace")):
+        a = dict(q=q, lengths=lengths)
+        a.update(bad)
+        with pytest.raises(ValueError, match=match):
+            gpu.fp4_cache_attention(a.pop("q"), cache, table, a.pop("lengths"), **a)
+    for scale in (0.0, -1.0, math.nan, math.inf):
+        with pytest.raises(gpu.MraError, match="INVALID"):
+            gpu.fp4_cache_attention(q, cache, table, lengths, scale=scale)
 
 
 def test_a_captured_decoder_step(gpu):

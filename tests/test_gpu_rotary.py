@@ -202,6 +202,21 @@ def test_far_positions_are_as_exact_as_near_ones(gpu):
     assert (a - b).abs().max() <= 2.0 ** -21 * 2 * x.abs().max()
 
 
+def test_strides_past_32_bits(gpu):
+    """Heads and batches that begin past 2^32 bytes, read and written."""
+    big = torch.empty(5 << 30, dtype=torch.uint8, device="cuda").view(torch.bfloat16)
+    x = big.as_strided((2, 2, 40, 64), ((1 << 31) + 64 * 64, 64 * 80, 64))
+    y = big.as_strided((2, 2, 40, 64), ((1 << 31) + 64 * 64, 64 * 80, 64), 64 * 40)
+    gen = torch.Generator("cuda").manual_seed(2)
+    x.copy_(torch.randn(2, 2, 40, 64, generator=gen, device="cuda"))
+    y.zero_()
+    freqs = gpu.rotary_frequencies(64)
+    out = gpu.rotary_forward(x, None, freqs, q_out=y)
+    check(x, None, None, None, freqs, None, out)
+    assert torch.equal(gpu.rotary_backward(x, None, freqs=freqs, dq=y)[0],
+                       gpu.rotary_backward(x.contiguous(), None, freqs=freqs)[0])
+
+
 def test_repeats_are_the_same_bits(gpu):
     q, k, gq, gk, wq, wk, p = make(8, "bf16", 2, 8, 2, 3000, 64, "bnhd", "qk", None, "bn")
     freqs = gpu.rotary_frequencies(64)
@@ -258,3 +273,64 @@ def test_differentiated_once(gpu):
             torch.autograd.grad(dq.sum(), g)
         with pytest.warns(UserWarning, match="not differentiable"):
             torch.autograd.grad(call(), q, torch.ones_like(q), create_graph=True)
+
+
+@pytest.mark.parametrize("path", ["native", "python"])
+@pytest.mark.parametrize("which", ["q", "q_weight"])
+def test_a_captured_backward_with_an_eager_graph_alive_is_refused(gpu, path, which):
+    """The refusal alone is called, inside captures of forward calls: no such backward is run."""
+    q, k, _, _, wq, wk, p = make(13, "bf16", 2, 4, 2, 30, 64, norm="qk")
+    freqs = gpu.rotary_frequencies(64)
+    tensors = dict(q=q, k=k, q_weight=wq, k_weight=wk)
+    leaf = tensors[which] = tensors[which].clone().requires_grad_(True)
+
+    def forward():
+        t = [tensors[n] for n in ("q", "k", "q_weight", "k_weight")]
+        if path == "native":
+            return gpu.rotary(t[0], t[1], freqs, q_weight=t[2], k_weight=t[3])[0]
+        return gpu.Rotary.apply(*t, freqs, None, False, 1.0, 1e-6)[0]
+
+    def captured():
+        graph, error = torch.cuda.CUDAGraph(), None
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph):
+            try:
+                z = forward()
+                gpu.bind_layer().check_capture(z)
+                del z
+            except RuntimeError as e:
+                error = str(e)
+        return error
+
+    assert captured() is None
+    eager = leaf * 2.0
+    assert "eager graph" in captured()
+    gpu.bind_layer().check_capture(forward())      # not captured: nothing to refuse
+    del eager
+    assert captured() is None
+
+
+def test_refusals(gpu):
+    q, k, gq, gk, wq, wk, p = make(14, "bf16", 2, 4, 2, 30, 64, norm="qk", positions="bn")
+    freqs = gpu.rotary_frequencies(64)
+    for bad, match in ((dict(k=k[:1]), "share"), (dict(k=k.float()), "k must be"), (dict(k=k[..., :32]), "share"),
+                       (dict(freqs=freqs.float()), "freqs"), (dict(freqs=freqs[:4]), "freqs"),
+                       (dict(freqs=gpu.rotary_frequencies(128)), "freqs"), (dict(freqs=freqs.cpu()), "freqs"),
+                       (dict(positions=p.long()), "positions"), (dict(positions=p[:1]), "positions"),
+                       (dict(positions=p.t()), "positions"), (dict(q_weight=wq[:32]), "q_weight"),
+                       (dict(k_weight=wk.half()), "k_weight"), (dict(q_weight=wq.float()), "share their dtype"),
+                       (dict(q=q.transpose(2, 3)), "dense rows|share"), (dict(k=None), "k_weight without k"),
+                       (dict(q_out=q[:1].expand_as(q)), "broadcast")):
+        a = dict(q=q, k=k, freqs=freqs, positions=p, q_weight=wq, k_weight=wk)
+        a.update(bad)
+        with pytest.raises(ValueError, match=match):
+            gpu.rotary_forward(a.pop("q"), a.pop("k"), a.pop("freqs"), **a)
+    with pytest.raises(TypeError, match="float16|Half"):
+        gpu.rotary(q.half(), None, freqs)
+    for bad in (dict(eps=0.0), dict(eps=-1.0), dict(magnitude=float("inf"))):
+        with pytest.raises(gpu.MraError, match="INVALID"):
+            gpu.rotary(q, k, freqs, q_weight=wq, **bad)
+    with pytest.raises(ValueError, match="q is needed"):
+        gpu.rotary_backward(gq, gk, freqs=freqs, q_weight=wq)
+    with pytest.raises(ValueError, match="go with"):
+        gpu.rotary_backward(gq, None, freqs=freqs, dk=gk)

@@ -102,7 +102,7 @@ BAD_ROTARY = [
     (dict(q_weight=A, weight_dtype=7), UNSUPPORTED), (dict(q_weight=A, eps=0.0), INVALID),
     (dict(k_weight=A, eps=-1.0), INVALID), (dict(k_weight=A, eps=math.nan), INVALID), (dict(k_weight=A, eps=math.inf), INVALID),
     (dict(positions=A, positions_stride=-1), INVALID), (dict(n=(1 << 26) + 1), UNSUPPORTED),
-    (dict(H=(1 << 16) + 1), UNSUPPORTED), (dict(B=1 << 20, n=1 << 10), UNSUPPORTED), (dict(freqs=None), INVALID),
+    (dict(H=(1 << 16) + 1), UNSUPPORTED), (dict(B=1 << 18, n=1 << 10), UNSUPPORTED), (dict(freqs=None), INVALID),
 ]
 
 
@@ -182,7 +182,7 @@ BAD_ATTENTION = [
     (dict(H=-1), INVALID), (dict(n_q=-1), INVALID), (dict(H=7), INVALID), (dict(H=0), INVALID), (dict(scale=0.0), INVALID),
     (dict(scale=2.0 ** -65), INVALID), (dict(scale=math.inf), INVALID), (dict(scale=math.nan), INVALID),
     (dict(causal=2), INVALID), (dict(dtype=2), UNSUPPORTED), (dict(n_q=(1 << 26) + 1), UNSUPPORTED),
-    (dict(H=(1 << 16) + 2), UNSUPPORTED), (dict(H=1 << 14, n_q=1 << 20), UNSUPPORTED), (dict(lengths=None), INVALID),
+    (dict(H=(1 << 16) + 2), UNSUPPORTED), (dict(H=1 << 12, n_q=(1 << 18) // 3 + 1), UNSUPPORTED), (dict(lengths=None), INVALID),
 ]
 
 
