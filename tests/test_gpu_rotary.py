@@ -205,8 +205,8 @@ def test_far_positions_are_as_exact_as_near_ones(gpu):
 def test_strides_past_32_bits(gpu):
     """Heads and batches that begin past 2^32 bytes, read and written."""
     big = torch.empty(5 << 30, dtype=torch.uint8, device="cuda").view(torch.bfloat16)
-    x = big.as_strided((2, 2, 40, 64), ((1 << 31) + 64 * 64, 64 * 80, 64))
-    y = big.as_strided((2, 2, 40, 64), ((1 << 31) + 64 * 64, 64 * 80, 64), 64 * 40)
+    x = big.as_strided((2, 2, 40, 64), ((1 << 31) + 64 * 64, 64 * 80, 64, 1))
+    y = big.as_strided((2, 2, 40, 64), ((1 << 31) + 64 * 64, 64 * 80, 64, 1), 64 * 40)
     gen = torch.Generator("cuda").manual_seed(2)
     x.copy_(torch.randn(2, 2, 40, 64, generator=gen, device="cuda"))
     y.zero_()
