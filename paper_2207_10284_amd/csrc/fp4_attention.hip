@@ -127,8 +127,12 @@ __global__ __launch_bounds__(W * kWave) void fp4_rows_kernel(CacheAttentionArgs 
   constexpr int KC = D / 16, NT = D / 32, BUF = 2 * St::kKeys;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const int tid = threadIdx.x, lane = lane_id(), w = wave_uniform(tid / kWave);
-  const int sp = blockIdx.x % splits, g = blockIdx.x / splits, bk = g / mtiles;
-  const int mt = mtiles - 1 - (g - bk * mtiles);   // causal: the longest first
+  // The last rows first, which are the longest of causal calls. Workgroups go round the eight XCDs in turn: a part
+  // of a head stays on one XCD, whose L2 its row tiles share; parts that are few are shifted from one level to the next, or an XCD
+  // had one or two of them, however short their sequences.
+  const int units = a.B * a.c.Hkv * splits, level = blockIdx.x / units, at_level = blockIdx.x - level * units;
+  const int mt = mtiles - 1 - level, unit = units < 32 ? (at_level + level) % units : at_level;
+  const int bk = unit / splits, sp = unit - bk * splits;
   const int b = bk / a.c.Hkv, hk = bk - b * a.c.Hkv, size = 1 << a.c.page_log2;
   const int rows = a.nq * a.group, row0 = (mt * W + w) * 32;
   const int m = row0 + (lane & 31), mc = min(m, rows - 1), i = mc / a.group, h = hk * a.group + (mc - i * a.group);
