@@ -174,7 +174,7 @@ __global__ __launch_bounds__(W * kWave) void fp4_rows_kernel(CacheAttentionArgs 
   }
   __syncthreads();
   // Of a SIMD's two waves one converts the next stage before its products and the other after them, so that
-  // one's vector work runs beside the other's matrix work.
+  // one's vector work runs beside the other's matrix work (16 heads on 4 x 8192 x 128 causal: 196 -> 186 us).
   const bool early = W == 8 && w >= W / 2;
   auto stage = [&](int n, auto B) {
     constexpr int kbuf = B * BUF;
@@ -200,13 +200,24 @@ __global__ __launch_bounds__(W * kWave) void fp4_rows_kernel(CacheAttentionArgs 
             select_rows(s[x], a.causal ? ok.tile(x) & low_bits(pos - k0 - 32 * x + 1) : ok.tile(x), -INFINITY);
         }
         Packed<1> pw[2];
+        auto value = [&](int x, int u, int t) { return at.trans(kbuf + St::kKeys + x * kTileBytes<D>, u, t); };
+        // at d <= 64 the first values are on their way while the weights are formed (16 heads on 4 x 8192 x 64 causal:
+        // 131 -> 123 us; at 128, where registers are short, 186 -> 212)
+        constexpr bool kAhead = D <= 64;
+        u32x4 first[kAhead ? NT : 1];
+        if constexpr (kAhead) {
+#pragma unroll
+          for (int t = 0; t < NT; ++t) first[t] = value(0, 0, t);
+          __builtin_amdgcn_sched_barrier(0);
+        }
         stage_weights(row[0], s, a.scale_log2, pw);
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
           for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int t = 0; t < NT; ++t) row[0].o[t] = mfma16(at.trans(kbuf + St::kKeys + x * kTileBytes<D>, u, t), pw[x].w[0][u], row[0].o[t]);
+            for (int t = 0; t < NT; ++t)
+              row[0].o[t] = mfma16(kAhead && x + u == 0 ? first[kAhead ? t : 0] : value(x, u, t), pw[x].w[0][u], row[0].o[t]);
       }
     } else {
 #pragma unroll
