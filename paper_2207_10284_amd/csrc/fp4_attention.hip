@@ -221,31 +221,31 @@ __global__ __launch_bounds__(W * kWave) void fp4_rows_kernel(CacheAttentionArgs 
       }
     } else {
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const uint32_t kb = ok.tile(x);
-      const int k0 = 64 * n + 32 * x;
-      if (kb == 0 || (a.causal && k0 > pos_last)) continue;   // no key counts for the wave
-      f32x16 s[1] = {splat16(0.0f)};
+      for (int x = 0; x < 2; ++x) {
+        const uint32_t kb = ok.tile(x);
+        const int k0 = 64 * n + 32 * x;
+        if (kb == 0 || (a.causal && k0 > pos_last)) continue;   // no key counts for the wave
+        f32x16 s[1] = {splat16(0.0f)};
 #pragma unroll
-      for (int c = 0; c < KC; ++c) {
-        const u32x4 k = at.row(kbuf + x * kTileBytes<D>, c);
+        for (int c = 0; c < KC; ++c) {
+          const u32x4 k = at.row(kbuf + x * kTileBytes<D>, c);
 #pragma unroll
-        for (int q = NP - 1; q >= 0; --q) s[0] = mfma16(k, row[0].qf[q][c], s[0]);
-      }
-      const uint32_t bits = a.causal ? kb & low_bits(pos - k0 + 1) : kb;
-      if (kb != ~0u || (a.causal && k0 + 31 > pos_first)) select_rows(s[0], bits, -INFINITY);
-      const float mul[1] = {a.scale_log2}, add[1] = {0.0f};
-      Packed<NP> pw[1];
-      tile_weights<NP, D, 1>(row, s, mul, add, pw);
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          const u32x4 v = at.trans(kbuf + St::kKeys + x * kTileBytes<D>, u, t);
-#pragma unroll
-          for (int q = NP - 1; q >= 0; --q) row[0].o[t] = mfma16(v, pw[0].w[q][u], row[0].o[t]);
+          for (int q = NP - 1; q >= 0; --q) s[0] = mfma16(k, row[0].qf[q][c], s[0]);
         }
-    }
+        const uint32_t bits = a.causal ? kb & low_bits(pos - k0 + 1) : kb;
+        if (kb != ~0u || (a.causal && k0 + 31 > pos_first)) select_rows(s[0], bits, -INFINITY);
+        const float mul[1] = {a.scale_log2}, add[1] = {0.0f};
+        Packed<NP> pw[1];
+        tile_weights<NP, D, 1>(row, s, mul, add, pw);
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int t = 0; t < NT; ++t) {
+            const u32x4 v = at.trans(kbuf + St::kKeys + x * kTileBytes<D>, u, t);
+#pragma unroll
+            for (int q = NP - 1; q >= 0; --q) row[0].o[t] = mfma16(v, pw[0].w[q][u], row[0].o[t]);
+          }
+      }
     }
     if (more && !early) refill();
     ok = next;
@@ -416,22 +416,13 @@ struct TokenRows {
     return t;
   }
 
-  // Weights of U tiles' scores; a reference that they outgrow is moved first, in all lanes of its column.
-  template <int U>
-  __device__ __forceinline__ void tiles(const float (&s)[U][8], float mul, u32x4 (&w)[U][NP]) {
-    float t[U];
-    bool fits = true;
+  // Weights of a tile's scores; a reference that they outgrow is moved first, in all lanes of its column.
+  __device__ __forceinline__ void tile(const float (&s)[8], float mul, u32x4 (&w)[NP]) {
+    float t = weights(s, mul, ref, w);
+    if (__ballot(!(t <= kCap)) != 0) {             // also where ref is -inf
+      float mx = s[0];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      t[u] = weights(s[u], mul, ref, w[u]);
-      fits = fits && t[u] <= kCap;                 // not so where ref is -inf
-    }
-    if (__ballot(!fits) != 0) {
-      float mx = s[0][0];
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int r = 0; r < 8; ++r) mx = fmaxf(mx, s[u][r]);
+      for (int r = 1; r < 8; ++r) mx = fmaxf(mx, s[r]);
       mx = column_max(mx) * mul;
       const float next = mx > ref ? mx + kMargin : ref;
       const float f = next == ref ? 1.0f : __builtin_amdgcn_exp2f(ref - next);
@@ -439,21 +430,19 @@ struct TokenRows {
       for (int x = 0; x < D / 16; ++x) o[x] *= f;
       sum *= f;
       ref = next;
-#pragma unroll
-      for (int u = 0; u < U; ++u) t[u] = weights(s[u], mul, ref == -INFINITY ? 0.0f : ref, w[u]);   // no key yet: every s is -inf
+      t = weights(s, mul, ref == -INFINITY ? 0.0f : ref, w);    // no key yet: every s is -inf
     }
-#pragma unroll
-    for (int u = 0; u < U; ++u) sum += t[u];
+    sum += t;
   }
 };
 
-template <int NP, int D, int W, int U>
-__global__ __launch_bounds__(W * kWave) void fp4_token_kernel(CacheAttentionArgs a, int mtiles, int splits,
+template <int NP, int D>
+__global__ __launch_bounds__(kTokenWaves * kWave) void fp4_token_kernel(CacheAttentionArgs a, int mtiles, int splits,
                                                                         float* __restrict__ part_o,
                                                                         float* __restrict__ part_l) {
-  constexpr int KC = D / 32, NT = D / 16;
+  constexpr int W = kTokenWaves, KC = D / 32, NT = D / 16;
   // the waves' values, at the end the sums of all but the first
-  constexpr int kValues = W * U * 64 * D, kMerge = (W - 1) * NT * kWave * 16;
+  constexpr int kValues = W * 64 * D, kMerge = (W - 1) * NT * kWave * 16;
   __shared__ __attribute__((aligned(256))) char lds[kValues > kMerge ? kValues : kMerge];
   f32x4(*merged)[NT][kWave] = reinterpret_cast<f32x4(*)[NT][kWave]>(lds);
   __shared__ float refs[W][kWave], sums[W][kWave];
@@ -476,69 +465,52 @@ __global__ __launch_bounds__(W * kWave) void fp4_token_kernel(CacheAttentionArgs
   PageList<W> list;
   list.load(a.c, b, t0 + w, t1);
   auto page_of = [&](int t) { return list.get(a.c, b, hk, t, t1); };
-  ValueTile<D> values[U];
-#pragma unroll
-  for (int u = 0; u < U; ++u) values[u].init(lds + (w * U + u) * 64 * D);
-  CacheTile<D> next[U];
-  const char* page[U];                             // of the tiles in next
+  ValueTile<D> values;
+  values.init(lds + w * 64 * D);
+  CacheTile<D> next;
   int t = t0 + w;
+  const char* page = page_of(t);                   // of the tile in next
+  if (page != nullptr) next.load(page, 32 * t & (size - 1), size);
+  for (; t < t1; t += W) {
+    const CacheTile<D> tile = next;
+    const int k0 = 32 * t, end = page != nullptr ? kend : 0;  // no page: no key
+    page = page_of(t + W);
+    if (page != nullptr) next.load(page, 32 * (t + W) & (size - 1), size);
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    page[u] = page_of(t + u * W);
-    if (page[u] != nullptr) next[u].load(page[u], 32 * (t + u * W) & (size - 1), size);
-  }
-  for (; t < t1; t += U * W) {
-    CacheTile<D> tile[U];
-    bool some[U];
+    for (int x = 0; x < 2; ++x) {
+      // the steps of keys that do not count may be anything
+      const float step = fp4_step(k0 + CacheTile<D>::row(1, x) < end ? tile.e[1][x] : 127);
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      tile[u] = next[u];
-      some[u] = page[u] != nullptr;
-      page[u] = page_of(t + (U + u) * W);
-      if (page[u] != nullptr) next[u].load(page[u], 32 * (t + (U + u) * W) & (size - 1), size);
+      for (int n = 0; n < KC; ++n) values.put(x, n, fp4_decode(tile.w[1][x][n], step));
     }
-    float s[U][8];
+    float s[8];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int k0 = 32 * (t + u * W);
-      const int end = some[u] ? kend : 0;          // no page, or past the last tile: no key
+    for (int x = 0; x < 2; ++x) {
+      f32x4 c = {0.0f, 0.0f, 0.0f, 0.0f};
+      const float step = fp4_step(tile.e[0][x]);
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        // the steps of keys that do not count may be anything
-        const float step = fp4_step(k0 + CacheTile<D>::row(1, x) < end ? tile[u].e[1][x] : 127);
+      for (int n = 0; n < KC; ++n) {
+        const u32x4 k = fp4_decode(tile.w[0][x][n], step);
 #pragma unroll
-        for (int n = 0; n < KC; ++n) values[u].put(x, n, fp4_decode(tile[u].w[1][x][n], step));
+        for (int q = NP - 1; q >= 0; --q) c = mfma4(k, row.qf[q][n], c);
       }
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        f32x4 c = {0.0f, 0.0f, 0.0f, 0.0f};
-        const float step = fp4_step(tile[u].e[0][x]);
-#pragma unroll
-        for (int n = 0; n < KC; ++n) {
-          const u32x4 k = fp4_decode(tile[u].w[0][x][n], step);
-#pragma unroll
-          for (int q = NP - 1; q >= 0; --q) c = mfma4(k, row.qf[q][n], c);
-        }
-#pragma unroll
-        for (int r = 0; r < 4; ++r) s[u][4 * x + r] = c[r];
-      }
-      if (k0 + 32 > end || (a.causal && k0 + 31 > pos_first)) {
-        const uint32_t bits = low_bits((a.causal ? min(end, pos + 1) : end) - k0 - 8 * g4);
-#pragma unroll
-        for (int r = 0; r < 8; ++r) s[u][r] = bits >> r & 1 ? s[u][r] : -INFINITY;
-      }
+      for (int r = 0; r < 4; ++r) s[4 * x + r] = c[r];
     }
-    u32x4 pw[U][NP];
-    row.tiles(s, a.scale_log2, pw);
+    if (k0 + 32 > end || (a.causal && k0 + 31 > pos_first)) {
+      const uint32_t bits = low_bits((a.causal ? min(end, pos + 1) : end) - k0 - 8 * g4);
+#pragma unroll
+      for (int r = 0; r < 8; ++r) s[r] = bits >> r & 1 ? s[r] : -INFINITY;
+    }
+    u32x4 pw[NP];
+    row.tile(s, a.scale_log2, pw);
     wave_lds_sync();
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int x = 0; x < NT; ++x) {
+      const u32x4 v = values.get(x);
 #pragma unroll
-      for (int x = 0; x < NT; ++x) {
-        const u32x4 v = values[u].get(x);
-#pragma unroll
-        for (int q = NP - 1; q >= 0; --q) row.o[x] = mfma4(v, pw[u][q], row.o[x]);
-      }
+      for (int q = NP - 1; q >= 0; --q) row.o[x] = mfma4(v, pw[q], row.o[x]);
+    }
     wave_lds_sync();
   }
   // the waves' sums relative to the largest reference, added in wave order
@@ -617,7 +589,7 @@ static hipError_t attention_case(const CacheAttentionArgs& a, const CachePlan& p
   float* part_o = static_cast<float*>(ws);
   float* part_l = part_o + (plan.splits > 1 ? plan.splits * heads * rows * D : 0);
   if (plan.few) {
-    fp4_token_kernel<NP, D, kTokenWaves, 1><<<wgs, kTokenWaves * kWave, 0, stream>>>(a, plan.mtiles, plan.splits, part_o, part_l);
+    fp4_token_kernel<NP, D><<<wgs, kTokenWaves * kWave, 0, stream>>>(a, plan.mtiles, plan.splits, part_o, part_l);
   } else {
     constexpr int W = row_waves(NP, D);
     constexpr size_t smem = 4 * CacheStage<D, W * kWave>::kKeys;
