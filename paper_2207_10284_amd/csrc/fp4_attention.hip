@@ -26,22 +26,21 @@ __device__ __forceinline__ int first_query(const CacheAttentionArgs& a, int b, i
   return a.q_start == nullptr ? keys - a.nq : min(max(a.q_start[b], -kFar), kFar);
 }
 
-// The pages of up to 64 tiles of 32 keys, every STEP-th from tile `first` on: a lane holds one entry of the table,
-// loaded once for all of them, so that no step of a loop waits for the table.
-template <int STEP>
+// The pages of a wave's tiles of 32 keys, every step-th from `tile` on: a lane holds one entry of the table, loaded
+// once for 64 of them, so that no turn of a loop waits for the table.
 struct PageList {
-  int entry, first;
-  __device__ __forceinline__ void load(const CacheArgs& c, int b, int tile, int end) {
-    first = tile;
-    const int t = tile + lane_id() * STEP;
-    entry = t < end ? c.table[(long long)b * c.max_pages + (t >> (c.page_log2 - 5))] : -1;
+  int entry, tile, step, used;
+  __device__ __forceinline__ void load(const CacheArgs& c, int b) {
+    const int t = tile + lane_id() * step;         // tiles below 2^21, steps below 2^9
+    entry = t < c.cap >> 5 ? c.table[(long long)b * c.max_pages + (t >> (c.page_log2 - 5))] : -1;
+    used = 0;
     wait_loads<0>();                               // here, not at each use beside the loads in flight
   }
-  // Of tile t (wave-uniform, first + STEP i); tiles up to `end` exist. Null: no page.
-  __device__ __forceinline__ const char* get(const CacheArgs& c, int b, int hk, int t, int end) {
-    if (t >= end) return nullptr;
-    if (t - first >= 64 * STEP) load(c, b, t, end);
-    const int page = __builtin_amdgcn_readlane(entry, (t - first) / STEP);
+  // Of the next tile; null: no page, or past the table.
+  __device__ __forceinline__ const char* next(const CacheArgs& c, int b, int hk) {
+    if (used == 64) load(c, b);
+    const int page = __builtin_amdgcn_readlane(entry, used++);
+    tile += step;
     return (unsigned)page < (unsigned)c.pages ? c.data + ((long long)page * c.Hkv + hk) * c.head_bytes : nullptr;
   }
 };
@@ -441,9 +440,9 @@ __global__ __launch_bounds__(kTokenWaves * kWave) void fp4_token_kernel(CacheAtt
                                                                         float* __restrict__ part_o,
                                                                         float* __restrict__ part_l) {
   constexpr int W = kTokenWaves, KC = D / 32, NT = D / 16;
-  // the waves' values, at the end the sums of all but the first
-  constexpr int kValues = W * 64 * D, kMerge = (W - 1) * NT * kWave * 16;
-  __shared__ __attribute__((aligned(256))) char lds[kValues > kMerge ? kValues : kMerge];
+  // the waves' values, at the end their sums
+  static_assert(64 * D == NT * kWave * 16, "as large");
+  __shared__ __attribute__((aligned(256))) char lds[W * 64 * D];
   f32x4(*merged)[NT][kWave] = reinterpret_cast<f32x4(*)[NT][kWave]>(lds);
   __shared__ float refs[W][kWave], sums[W][kWave];
   const int lane = lane_id(), w = wave_uniform(threadIdx.x / kWave), g4 = lane >> 4;
@@ -452,30 +451,29 @@ __global__ __launch_bounds__(kTokenWaves * kWave) void fp4_token_kernel(CacheAtt
   const int b = bk / a.c.Hkv, hk = bk - b * a.c.Hkv, size = 1 << a.c.page_log2;
   const int rows = a.nq * a.group, row0 = mt * kTokenRows;
   const int m = row0 + (lane & 15), mc = min(m, rows - 1), i = mc / a.group, h = hk * a.group + (mc - i * a.group);
+  // A workgroup takes every splits-th group of W tiles: which ones does not depend on the length, so neither the look
+  // into the table nor the first tile waits for that.
+  PageList list{0, sp * W + w, splits * W, 0};
+  list.load(a.c, b);
+  CacheTile<D> next;
+  int t = sp * W + w;
+  const char* page = list.next(a.c, b, hk);        // of the tile in next
+  if (page != nullptr) next.load(page, 32 * t & (size - 1), size);
+  TokenRows<NP, D> row;
+  row.load_queries(a.q.p + b * a.q.sb + h * a.q.sh + i * a.q.sn, m < rows);
+  row.init();
+  ValueTile<D> values;
+  values.init(lds + w * 64 * D);
   const int limit = cached_keys(a, b), start = first_query(a, b, limit);
   const int pos = start + i, pos_first = start + row0 / a.group;
   const int pos_last = start + min(row0 + kTokenRows - 1, rows - 1) / a.group;
   const int kend = a.causal ? min(limit, pos_last + 1) : limit;
   const int tiles = kend > 0 ? (kend + 31) / 32 : 0;
-  const int t0 = (int)((long long)tiles * sp / splits), t1 = (int)((long long)tiles * (sp + 1) / splits);
-
-  TokenRows<NP, D> row;
-  row.load_queries(a.q.p + b * a.q.sb + h * a.q.sh + i * a.q.sn, m < rows);
-  row.init();
-  PageList<W> list;
-  list.load(a.c, b, t0 + w, t1);
-  auto page_of = [&](int t) { return list.get(a.c, b, hk, t, t1); };
-  ValueTile<D> values;
-  values.init(lds + w * 64 * D);
-  CacheTile<D> next;
-  int t = t0 + w;
-  const char* page = page_of(t);                   // of the tile in next
-  if (page != nullptr) next.load(page, 32 * t & (size - 1), size);
-  for (; t < t1; t += W) {
+  for (; t < tiles; t += splits * W) {
     const CacheTile<D> tile = next;
     const int k0 = 32 * t, end = page != nullptr ? kend : 0;  // no page: no key
-    page = page_of(t + W);
-    if (page != nullptr) next.load(page, 32 * (t + W) & (size - 1), size);
+    page = t + splits * W < tiles ? list.next(a.c, b, hk) : nullptr;
+    if (page != nullptr) next.load(page, 32 * (t + splits * W) & (size - 1), size);
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
       // the steps of keys that do not count may be anything
@@ -513,42 +511,39 @@ __global__ __launch_bounds__(kTokenWaves * kWave) void fp4_token_kernel(CacheAtt
     }
     wave_lds_sync();
   }
-  // the waves' sums relative to the largest reference, added in wave order
+  // the waves' sums relative to the largest reference, added in wave order, each wave some of the channels
   float sum = column_sum(row.sum);
   refs[w][lane] = row.ref;
   sums[w][lane] = sum;
-  __syncthreads();
+  __syncthreads();                                 // the values are idle
   float top = refs[0][lane];
 #pragma unroll
   for (int x = 1; x < W; ++x) top = fmaxf(top, refs[x][lane]);
   auto factor = [&](float ref) { return ref == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ref - top); };
   const float f = factor(row.ref);
 #pragma unroll
-  for (int x = 0; x < NT; ++x) row.o[x] *= f;
-  if (w != 0)
+  for (int x = 0; x < NT; ++x) merged[w][x][lane] = row.o[x] * f;
+  sum = 0.0f;
 #pragma unroll
-    for (int x = 0; x < NT; ++x) merged[w - 1][x][lane] = row.o[x];
+  for (int p = 0; p < W; ++p) sum += sums[p][lane] * factor(refs[p][lane]);
   __syncthreads();
-  if (w != 0) return;
-  sum *= f;
-#pragma unroll
-  for (int p = 1; p < W; ++p) {
-    sum += sums[p][lane] * factor(refs[p][lane]);
-#pragma unroll
-    for (int x = 0; x < NT; ++x) row.o[x] += merged[p - 1][x][lane];
-  }
   if (m >= rows) return;
   const float inv = splits > 1 ? 1.0f : sum > 0.0f ? 1.0f / sum : 0.0f;
   const long long pr = ((long long)sp * a.B * a.c.Hkv + bk) * rows + m;   // the partial row
   char* to = splits > 1 ? reinterpret_cast<char*>(part_o + pr * D) : a.out.p + b * a.out.sb + h * a.out.sh + i * a.out.sn;
 #pragma unroll
-  for (int x = 0; x < NT; ++x) {
-    const float z[4] = {row.o[x][0] * inv, row.o[x][1] * inv, row.o[x][2] * inv, row.o[x][3] * inv};
+  for (int y = 0; y < (NT + W - 1) / W; ++y) {
+    const int x = y * W + w;
+    if (x >= NT) break;
+    f32x4 o = merged[0][x][lane];
+#pragma unroll
+    for (int p = 1; p < W; ++p) o += merged[p][x][lane];
+    const float z[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
     const int c = 16 * x + 4 * g4;
     if (NP == 1 && splits == 1) store4<1>(to + 2 * c, z);
     else store4<3>(to + 4 * c, z);
   }
-  if (g4 != 0) return;
+  if (g4 != 0 || w != 0) return;
   if (splits > 1) {
     part_l[2 * pr] = top;
     part_l[2 * pr + 1] = sum;
