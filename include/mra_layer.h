@@ -12,7 +12,7 @@
  *   strides in elements, dense rows of d elements, each stride >= 0 and a multiple of 16
  *   bytes. Input strides may be 0. Outputs must not overlap themselves or, where
  *   not said otherwise, another argument.
- * - d is 32, 64 or 128; rotary calls have below 2^28 tokens (B n), attention at most 2^30
+ * - d is 32, 64 or 128; rotary calls have below 2^27 tokens (B n), attention at most 2^30
  *   rows (B H n_q), heads are at most 2^16.
  * - Everything is computed in float32 (angles in float64)
  *   and rounded once, if not said otherwise.

@@ -5,10 +5,20 @@
 // that moves only when a tile outgrows it. The rows of a key head, all queries of all its heads,
 // are one list: row m is query m / group of head hk group + m % group.
 //
-// fp4_rows_kernel: a workgroup's four waves take 32 rows each and walk the keys
-// together, 64 at a time. Codes come through registers and are converted once per workgroup: keys to
-// bfloat16 rows in LDS, values to rows of a channel's 64 tokens, which is the A operand that the second
-// product wants, so nothing is transposed.
+// fp4_rows_kernel: a workgroup's waves (eight, or four) take 32 rows each and walk the keys
+// together, 64 at a time. Codes come through registers and are converted once per workgroup, to
+// bfloat16 rows in LDS in the order and swizzle of the exact kernels, whose transposing reads give the second
+// product's operand. What bounds it is a stage's vector work (exponentials, packing, conversion) beside its matrix work, two waves a
+// SIMD: at 2 x 16 heads on 4, 512 queries on up to 16384 keys x 128 bfloat16, 115 us and the join 8 (820 TFLOP/s, 61% of
+// a large product's rate; matrix cores busy 36%, vector ALU 33%, waves waiting 27% of their time).
+//
+// fp4_token_kernel: few rows, single tokens above all. A wave takes 16 rows and 32 keys at a time on the
+// 16x16x32 matrix instructions. Keys go from memory to registers as the first product takes them; values
+// pass through the wave's own part of LDS, which transposes them. A workgroup's waves take every
+// kTokenWaves-th tile, and several workgroups may share the rows, each with a part of the keys
+// (exact_join_kernel adds them). What bounds it is the cache's bytes and, as much, the chain from tile to tile within a
+// wave: one token of 32 x 12 heads on up to 4096 keys x 64, 20 us (80 MB, 4.0 TB/s; loads alone, without any products, take
+// 2.5 us less) and the join 4; 4 x 16 heads on 4, up to 32768 x 128, 13 to 15 us (53 MB) and the join 4.
 #include "exact_rows.h"
 #include "fp4_tile.h"
 
@@ -272,6 +282,7 @@ __global__ __launch_bounds__(W * kWave) void fp4_rows_kernel(CacheAttentionArgs 
 
 // ---- few rows
 
+// Four waves and two workgroups a CU: eight waves and one 31 us, two and four 29, four and one 29, where these take 25.
 constexpr int kTokenWaves = 4;
 constexpr int kTokenRows = 16;
 

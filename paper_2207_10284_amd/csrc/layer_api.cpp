@@ -76,8 +76,8 @@ mra_status_t check_rotary(const mra_rotary_problem_t* p) {
   }
   if (p->positions != nullptr && p->positions_stride < 0) return MRA_ERR_INVALID_ARG;
   if (p->n > kMaxLen || p->H > kMaxHeads || p->H_kv > kMaxHeads) return MRA_ERR_UNSUPPORTED;
-  // a workgroup for 16 tokens, where they are many
-  if ((long long)p->B * p->n > 16 * kMaxGroups) return MRA_ERR_UNSUPPORTED;
+  // a workgroup for 8 tokens, where they are many
+  if ((long long)p->B * p->n > 8 * kMaxGroups) return MRA_ERR_UNSUPPORTED;
   return MRA_OK;
 }
 

@@ -4,7 +4,10 @@
 // written) for some ten operations. What is left to do is to keep the angles
 // cheap, a float64 product and a sine and cosine each: a workgroup takes a tile of
 // tokens with all their heads, makes the tile's sines and cosines once in LDS, and
-// its rows read them there.
+// its rows read them there. Measured on data that no cache holds: 8 x 24 heads x 4096 x 64 bfloat16, forward or backward
+// 41 us (201 MB, 4.9 TB/s, 97% of a large copy's rate); 20 heads x 32768 x 128 bfloat16 with norms, forward 62 us (336 MB,
+// 5.4 TB/s), backward 109 us (503 MB, 4.6 TB/s: three rows in flight take 190 registers, two waves a SIMD) and
+// 6 us for the weights' sums; 10 heads x 4 x 2999 x 128 float32, forward 28 us (123 MB, 4.4 TB/s).
 //
 // A row is shared by D / 16 lanes. A lane holds two chunks of eight elements such that
 // the eight pairs within them are its own: chunks i and rot/2 + i (half), or
@@ -20,7 +23,8 @@ namespace mra {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMaxTile = 16;                       // tokens of a tile
+// Tokens of a tile (24 heads x 8 x 4096 x 64 bfloat16, training: four 84.5, eight 81.7, sixteen 84.8 us)
+constexpr int kMaxTile = 8;
 
 // Eight consecutive elements.
 template <int DT>
@@ -99,7 +103,7 @@ struct Tile {
   }
 };
 
-// cos and sin (times the magnitude) of the tile's tokens and frequencies. Tokens are below 2^28.
+// cos and sin (times the magnitude) of the tile's tokens and frequencies. Tokens are below 2^27.
 __device__ __forceinline__ void fill_angles(const RotaryArgs& a, int first, int tokens, float2* cs) {
   const int half = a.rot / 2;                      // a multiple of eight, at most 64, not always a power of two
   for (int i = threadIdx.x; i < tokens * half; i += kThreads) {
@@ -372,7 +376,7 @@ __global__ __launch_bounds__(kSumThreads) void rotary_weight_kernel(const float*
   }
 }
 
-// Tokens of a tile: 16, fewer while that leaves CUs without a workgroup.
+// Tokens of a tile: kMaxTile, fewer while that leaves CUs without a workgroup.
 static int rotary_tile(long long tokens) {
   int tile = kMaxTile;
   while (tile > 1 && tokens < (long long)tile * 2 * kCus) tile /= 2;

@@ -102,7 +102,7 @@ BAD_ROTARY = [
     (dict(q_weight=A, weight_dtype=7), UNSUPPORTED), (dict(q_weight=A, eps=0.0), INVALID),
     (dict(k_weight=A, eps=-1.0), INVALID), (dict(k_weight=A, eps=math.nan), INVALID), (dict(k_weight=A, eps=math.inf), INVALID),
     (dict(positions=A, positions_stride=-1), INVALID), (dict(n=(1 << 26) + 1), UNSUPPORTED),
-    (dict(H=(1 << 16) + 1), UNSUPPORTED), (dict(B=1 << 18, n=1 << 10), UNSUPPORTED), (dict(freqs=None), INVALID),
+    (dict(H=(1 << 16) + 1), UNSUPPORTED), (dict(B=1 << 17, n=1 << 10), UNSUPPORTED), (dict(freqs=None), INVALID),
 ]
 
 
