@@ -12,8 +12,10 @@
  *   strides in elements, dense rows of d elements, each stride >= 0 and a multiple of 16
  *   bytes. Input strides may be 0. Outputs must not overlap themselves or, where
  *   not said otherwise, another argument.
- * - d is 32, 64 or 128; rotary calls have below 2^27 tokens (B n), attention at most 2^30
- *   rows (B H n_q), heads are at most 2^16.
+ * - d is 32, 64 or 128; rotary calls have below 2^27 tokens (B n); writing and reading the
+ *   cache, sequences times key heads times tiles of 32 tokens are below 2^24; attention has at most
+ *   2^30 rows (B H n_q) and below 2^23 row tiles (16 rows of a key head up to 64 of them, else 128);
+ *   heads are at most 2^16.
  * - Everything is computed in float32 (angles in float64)
  *   and rounded once, if not said otherwise.
  * - Results do not change from run to run.
@@ -40,7 +42,8 @@ extern "C" {
  * from rot on stay as they are.
  *
  * The angle is taken in turns, p f / (2 pi) in float64, and rounded to float32 only
- * after its whole turns are gone, so far positions are as exact as near ones.
+ * after its whole turns are gone, so far positions are as exact as near ones. Of rows with a
+ * norm the mean square is within float32's range.
  */
 typedef struct {
   int B, H, H_kv, n, d;       /* H or H_kv may be 0: no queries, no keys */

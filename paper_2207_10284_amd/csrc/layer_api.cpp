@@ -183,8 +183,9 @@ mra::CachePlan attention_plan(const mra_fp4_cache_t& c, const mra_fp4_attention_
                          (int)p.dtype);
 }
 
+// Workgroups have up to 512 threads. (The join has fewer: splits are several only below two workgroups a CU.)
 mra_status_t check_attention_grid(const mra_fp4_cache_t& c, const mra::CachePlan& plan) {
-  return (long long)c.B * c.H_kv * plan.mtiles <= kMaxGroups / plan.splits ? MRA_OK : MRA_ERR_UNSUPPORTED;
+  return (long long)c.B * c.H_kv * plan.mtiles <= kMaxGroups / 2 / plan.splits ? MRA_OK : MRA_ERR_UNSUPPORTED;
 }
 
 }  // namespace

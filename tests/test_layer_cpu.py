@@ -210,6 +210,32 @@ def test_attention_tensors_refused(lib):
     assert lib.mra_layer_last_hip_error() == 0
 
 
+# below 2^32 threads of a launch dimension: 2^23 - 1 workgroups of 512, 2^24 - 1 of 256. What is not
+# refused for its size is for a missing tensor, before anything is enqueued.
+@pytest.mark.parametrize("sizes,n_q,status", [
+    (dict(B=1 << 20, H_kv=8), 1, UNSUPPORTED), (dict(B=(1 << 20) - 1, H_kv=8), 1, INVALID),
+    (dict(B=1 << 19, H_kv=8), 17, UNSUPPORTED), (dict(B=1 << 19, H_kv=8), 16, INVALID),
+    (dict(B=1 << 16, H_kv=64), 65, INVALID), (dict(B=1 << 17, H_kv=64), 65, UNSUPPORTED),
+])
+def test_attention_launches_that_do_not_fit(lib, sizes, n_q, status):
+    c = cache(**sizes)
+    p = attention(H=c.H_kv, n_q=n_q, lengths=None)
+    assert attend(lib, c, p) == status
+    if status == UNSUPPORTED:
+        assert lib.mra_fp4_attention_workspace_bytes(ctypes.byref(c), ctypes.byref(p)) == 0
+
+
+@pytest.mark.parametrize("B,n,status", [((1 << 21) - 1, 33, INVALID), (1 << 22, 33, UNSUPPORTED)])
+def test_cache_launches_that_do_not_fit(lib, B, n, status):
+    for read in (False, True):
+        assert rows(lib, cache(B=B, H_kv=2), n=n, read=read, k=tensor(None)) == status
+
+
+@pytest.mark.parametrize("B,n,status", [((1 << 24) - 1, 8, INVALID), (1 << 24, 8, UNSUPPORTED)])
+def test_rotary_launches_that_do_not_fit(lib, B, n, status):
+    assert turn(lib, rotary(B=B, n=n), q=tensor(None)) == status
+
+
 def test_tensors_on_the_host_are_refused():
     q = torch.zeros(1, 2, 4, 32)
     f = ops.rotary_frequencies(32, device="cpu")
