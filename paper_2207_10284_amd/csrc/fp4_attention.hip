@@ -572,14 +572,16 @@ constexpr int row_waves(int np, int d) { return np == 1 && d == 128 ? 8 : 4; }
 //   8 heads x 4096 keys, 128 rows: 17, 12   256 rows: 19, 15   512 rows: 21, 20
 //   4 heads x 16384 keys, 128 rows: 19, 16   256 rows: 23, 21   512 rows: 31, 33
 // Where the rows' workgroups are fewer than two per CU (one of eight waves) several share the keys of the same
-// rows, each at least 256.
+// rows, each at least 256; in the token kernel only beyond 1024 keys, below which adding their parts costs more than it
+// saves (bfloat16, d = 64, one token, us, alone and shared: 16 heads x 512 keys 6.5, 10; 256 heads x 1024 keys 8.9, 11.9;
+// 16 heads x 1024 keys 8.4, 9.6, at d = 128 10.4, 9.6; 16 heads x 2048 keys 13, 9).
 CachePlan cache_plan(int B, int Hkv, long long rows, int cap, int d, int dtype) {
   CachePlan p{};
   const long long heads = (long long)B * Hkv, tiles = heads * ((rows + kTokenRows - 1) / kTokenRows);
   p.few = rows <= 64 || tiles <= (1 << 20) / (cap > 0 ? cap : 1);
   const int waves = p.few ? kTokenWaves : row_waves(dtype == BF16 ? 1 : 3, d);
   p.mtiles = (int)(p.few ? (rows + kTokenRows - 1) / kTokenRows : (rows + 32 * waves - 1) / (32 * waves));
-  const long long wgs = heads * p.mtiles, most = (cap + 255) / 256;
+  const long long wgs = heads * p.mtiles, most = p.few && cap <= 1024 ? 1 : (cap + 255) / 256;
   long long want = ((waves == 8 ? 1 : 2) * kCus + wgs - 1) / wgs;
   if (want > most) want = most;
   if (want > 64) want = 64;
