@@ -342,3 +342,55 @@ def test_what_a_tile_addresses_lies_in_its_page(d, size):
         assert codes[x] + (slot + 31) * (d // 2) + 3 * (d // 8) + d // 8 <= ends[x]         # few rows: d / 8 bytes
         assert steps[x] + (slot + 31) * nb + nb - 1 < ends[2 + x]
         assert codes[x] % 16 == 0 and steps[x] % 16 == 0
+
+
+def value_place(d, r, c):
+    """ValueTile::place of fp4_attention.hip."""
+    f = (r & 3) | (r >> 3 & 1) << 2 if d == 128 else (r >> 1 & 1) | (r >> 3 & 1) << 1 if d == 64 else r >> 3 & 1
+    return r * 2 * d + (((c >> 4) ^ f) << 5) + (((c >> 3 & 1) ^ (r >> 2 & 1)) << 4) + (c & 4) * 2
+
+
+@pytest.mark.parametrize("d", [32, 64, 128])
+def test_values_come_back_transposed(d):
+    """What lanes put and get in a wave's value tile: every place once, lane (g, i) of get(t) has channel
+    16 t + i of rows 8 g .. 8 g + 7, whose weights the first product left in the same lane group."""
+    places = [value_place(d, r, c) for r in range(32) for c in range(0, d, 4)]
+    assert sorted(places) == list(range(0, 64 * d, 8))
+    lds = {}
+    for lane in range(64):                          # put: row 16 x + i, chunk n of eight channels
+        g, i = lane >> 4, lane & 15
+        for x in range(2):
+            for n in range(d // 32):
+                at = (value_place(d, i, g * (d // 4)) ^ 16 * n) + x * 16 * 2 * d
+                for e in range(8):
+                    lds[at + 2 * e] = (16 * x + i, g * (d // 4) + 8 * n + e)
+    assert len(lds) == 32 * d
+    for t in range(d // 16):                        # get: lane i of 16 receives element i % 4 of the 8 bytes of lane 4 k + i / 4
+        for lane in range(64):
+            g, i = lane >> 4, lane & 15
+            for e in range(2):
+                for k in range(4):
+                    j = 4 * k + i // 4
+                    at = value_place(d, 8 * g + 4 * e + (j >> 2), 4 * (j & 3)) ^ 32 * t
+                    assert lds[at + 2 * (i % 4)] == (8 * g + 4 * e + k, 16 * t + i)
+    # scores: the product's row 4 g + r of part x is the key that lane i = 4 g + r loaded
+    for g in range(4):
+        for x in range(2):
+            for r in range(4):
+                i = 4 * g + r
+                assert 8 * (i >> 2) + 4 * x + (i & 3) == 8 * g + 4 * x + r
+
+
+@pytest.mark.parametrize("d,threads", [(32, 256), (64, 256), (128, 256), (128, 512)])
+def test_a_stage_converts_every_block_once(d, threads):
+    """CacheStage::unit: each token's blocks of keys and values belong to one lane each."""
+    nb, u = d // 32, 2 * d
+    per = 2 if 2 * u > threads else 1
+    seen = []
+    for tid in range(threads):
+        for n in range(per):
+            t = tid % u // nb
+            x = n if per == 2 else tid // u
+            if x < 2:
+                seen.append((x, (t & 48) | (t & 3) << 2 | (t >> 2 & 3), tid % u % nb))
+    assert sorted(seen) == [(x, r, b) for x in range(2) for r in range(64) for b in range(nb)]
