@@ -91,6 +91,8 @@ __device__ __forceinline__ void tile_weights(FwdRow<NP, D> (&row)[R], const f32x
   for (int x = 0; x < R; ++x) row[x].sum += t[x];
 }
 
+namespace {                                        // each library has a kernel of its own, also in a program that links both
+
 // Adds the partial rows of `splits` workgroups. D / 4 threads go across a row's columns
 // and `groups` (a power of two) across its splits, at most eight for a thread; the
 // groups' sums are added in their order. Rows of few splits share a workgroup (6144 rows of
@@ -164,5 +166,7 @@ inline void launch_join(const ExactArgs& a, float* lse, int splits, const float*
   const int per = 256 / (D / 4 * groups);
   exact_join_kernel<NP, D><<<(unsigned)((rows + per - 1) / per), 256, 0, stream>>>(a, lse, splits, groups, part_o, part_l);
 }
+
+}  // namespace
 
 }  // namespace mra
