@@ -147,6 +147,7 @@ mra_status_t mra_fp4_cache_read(const mra_fp4_cache_t* cache, const mra_strided_
  *   S_ij = scale q_i . k_j    L_i = ln sum_j exp(S_ij)    Z_i = sum_j exp(S_ij - L_i) v_j
  *
  * Query head h reads key head h / (H / H_kv). A query without keys has Z = 0, L = -infinity.
+ * One that has a key and holds a NaN or an infinity has NaN in all of Z and in L; other queries are as without it.
  * Products accumulate in float32; the cache's values enter them exactly, bfloat16 queries as they are with the
  * weights rounded to bfloat16; float32 queries and their weights as sums of three bfloat16 values.
  */

@@ -115,15 +115,19 @@ __global__ __launch_bounds__(256) void exact_join_kernel(ExactArgs a, float* __r
     const int s = grp + x * groups;
     const long long at = (s < splits ? s : 0) * all + pr;
     o[x] = *reinterpret_cast<const f32x4*>(part_o + at * D + 4 * c);
-    ref[x] = s < splits ? part_l[2 * at] : -INFINITY;
+    ref[x] = part_l[2 * at];
     l[x] = part_l[2 * at + 1];
+    if (s >= splits) {
+      ref[x] = -INFINITY;
+      l[x] = 0.0f;
+    }
   }
   float top = ref[0], sum = 0.0f;
 #pragma unroll
   for (int x = 1; x < kJoin; ++x) top = fmaxf(top, ref[x]);
   f32x4 z = {0.0f, 0.0f, 0.0f, 0.0f};
   auto add = [](const f32x4& o, float l, float ref, float top, f32x4& z, float& sum) {
-    if (ref == -INFINITY) return;                  // no key
+    if (l == 0.0f) return;                         // no key (a part whose scores are NaN has no reference either)
     const float f = __builtin_amdgcn_exp2f(ref - top);
     sum = fmaf(l, f, sum);
 #pragma unroll
@@ -153,7 +157,7 @@ __global__ __launch_bounds__(256) void exact_join_kernel(ExactArgs a, float* __r
   const float out[4] = {z[0] * inv, z[1] * inv, z[2] * inv, z[3] * inv};
   store4<NP>(a.out.p + b * a.out.sb + h * a.out.sh + i * a.out.sn + 4 * c * (NP == 1 ? 2 : 4), out);
   if (lse != nullptr && c == 0)
-    lse[((long long)b * a.H + h) * a.nq + i] = sum > 0.0f ? (log2f(sum) + top) * kLn2 : -INFINITY;
+    lse[((long long)b * a.H + h) * a.nq + i] = sum == 0.0f ? -INFINITY : (log2f(sum) + top) * kLn2;
 }
 
 // Enqueues the join of `splits` partial rows (at most 64).

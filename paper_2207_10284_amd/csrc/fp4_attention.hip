@@ -109,6 +109,22 @@ struct CacheStage {
   }
 };
 
+// A lane's part of a query that holds an infinity or a NaN becomes NaN whole, so that every score of the query is (an
+// infinity alone may give nothing but scores of -infinity, as float32's planes never do). Sums, and with them Z
+// and L, are NaN then; what has no key has sums of 0.
+template <int C>
+__device__ __forceinline__ void spread_nan(u32x4 (&q)[C]) {
+  uint32_t high = 0;
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) high |= (q[c][e] & 0x7fff7fffu) + 0x00800080u;   // bit 15 of a half: an exponent of ones
+  const bool bad = (high & 0x80008000u) != 0;
+  if (__ballot(bad) == 0) return;
+#pragma unroll
+  for (int c = 0; c < C; ++c) q[c] = bad ? u32x4{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u} : q[c];
+}
+
 // Weights of the scores s of a stage's two tiles (log2 logits s mul; -inf: does not count) and their sum; a
 // reference that they outgrow is moved first (see tile_weights).
 template <int D>
@@ -181,6 +197,7 @@ __global__ __launch_bounds__(W * kWave) void fp4_rows_kernel(CacheAttentionArgs 
     st.store(smem, ok, tid);
     if (n0 + 1 < n1) load(n0 + 1);
   }
+  if constexpr (NP == 1) spread_nan(row[0].qf[0]);
   __syncthreads();
   // Of a SIMD's two waves one converts the next stage before its products and the other after them, so that
   // one's vector work runs beside the other's matrix work (16 heads on 4 x 8192 x 128 causal: 196 -> 186 us).
@@ -277,7 +294,7 @@ __global__ __launch_bounds__(W * kWave) void fp4_rows_kernel(CacheAttentionArgs 
   store_rows<NP, D>(row[0].o, den > 0.0f ? 1.0f / den : 0.0f, a.out.p + b * a.out.sb + h * a.out.sh + i * a.out.sn,
                     m < rows);
   if (a.lse != nullptr && lane < 32 && m < rows)
-    a.lse[((long long)b * a.H + h) * a.nq + i] = den > 0.0f ? (log2f(den) + row[0].ref) * kLn2 : -INFINITY;
+    a.lse[((long long)b * a.H + h) * a.nq + i] = den == 0.0f ? -INFINITY : (log2f(den) + row[0].ref) * kLn2;
 }
 
 // ---- few rows
@@ -481,6 +498,7 @@ __global__ __launch_bounds__(kTokenWaves * kWave) void fp4_token_kernel(CacheAtt
   const int pos_last = start + min(row0 + kTokenRows - 1, rows - 1) / a.group;
   const int kend = a.causal ? min(limit, pos_last + 1) : limit;
   const int tiles = kend > 0 ? (kend + 31) / 32 : 0;
+  if constexpr (NP == 1) spread_nan(row.qf[0]);
   for (; t < tiles; t += splits * W) {
     const CacheTile<D> tile = next;
     const int k0 = 32 * t, end = page != nullptr ? kend : 0;  // no page: no key
@@ -560,7 +578,7 @@ __global__ __launch_bounds__(kTokenWaves * kWave) void fp4_token_kernel(CacheAtt
     part_l[2 * pr] = top;
     part_l[2 * pr + 1] = sum;
   } else if (a.lse != nullptr) {
-    a.lse[((long long)b * a.H + h) * a.nq + i] = sum > 0.0f ? (log2f(sum) + top) * kLn2 : -INFINITY;
+    a.lse[((long long)b * a.H + h) * a.nq + i] = sum == 0.0f ? -INFINITY : (log2f(sum) + top) * kLn2;
   }
 }
 

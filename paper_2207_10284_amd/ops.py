@@ -1078,7 +1078,7 @@ def fp4_cache_attention(q, cache: Fp4Cache, table, lengths, *, scale=None, causa
     ``lengths[b]`` (int32 [B]) tokens that the cache holds for each sequence; query
     head h reads key head h // (H / H_kv). Query i stands at ``q_start[b] + i`` (int32 [B];
     lengths[b] - n_q + i if not given) and with ``causal`` sees the tokens up to there. Tokens in an
-    entry of the table that is no page do not count; a query for which none counts gives zeros. ``scale``, ``out``, ``lse_out`` and
+    entry of the table that is no page do not count; a query for which none counts gives zeros, another that holds a NaN or an infinity NaN. ``scale``, ``out``, ``lse_out`` and
     ``workspace`` as in ``exact_attention_forward``. Not differentiable."""
     return bind_layer().attention(*cache._args(), q, table, lengths, scale, causal, q_start, _result(q, out), lse_out,
                                   workspace)
