@@ -31,6 +31,27 @@ void check_sizes(at::IntArrayRef sizes) {
 
 Opt opt(const at::Tensor& t) { return t.defined() ? Opt(t) : std::nullopt; }
 
+// A result tensor of the caller's. It may be an input, and autograd may know it: what takes part in a graph is refused
+// as by torch's own calls with given results, and what is written raises the tensor's version, so
+// that a backward which kept the old values is refused there.
+void check_graph(const at::Tensor& t, const char* name) {
+  TORCH_CHECK_VALUE(!(at::GradMode::is_enabled() && t.requires_grad()), name,
+                    " must not require a gradient: none would belong to its new values (torch.no_grad allows it)");
+}
+
+void check_result(const at::Tensor& t, const at::Tensor& ref, const char* name) {
+  check_out(t, ref, name);
+  check_graph(t, name);
+}
+
+void written(const at::Tensor& t) {
+  if (t.defined() && !t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
+void written(const Opt& t) {
+  if (t) written(*t);
+}
+
 // ---- rotary positions and head norms
 
 // What a rotary call has beside its rows.
@@ -108,12 +129,14 @@ std::pair<at::Tensor, at::Tensor> turned(const at::Tensor& q, const at::Tensor& 
   TORCH_CHECK_VALUE(k.defined() || !x.k_weight, "k_weight without k");
   TORCH_CHECK_VALUE(k.defined() || !k_out, "k_out without k");
   const mra_rotary_problem_t p = rotary_problem(q, k, x);
-  if (q_out) check_out(*q_out, q, "q_out");
-  if (k_out) check_out(*k_out, k, "k_out");
+  if (q_out) check_result(*q_out, q, "q_out");
+  if (k_out) check_result(*k_out, k, "k_out");
   const c10::DeviceGuard guard(q.device());
   const at::Tensor yq = q_out ? *q_out : rows_like(q), yk = k_out ? *k_out : k.defined() ? rows_like(k) : at::Tensor();
   const mra_strided_t vq = view(q), vk = view_or_none(k), wq = view(yq), wk = view_or_none(yk);
   ok("mra_rotary_forward", api.rotary_forward(&p, &vq, &vk, &wq, &wk, stream_of(q)));
+  written(q_out);
+  written(k_out);
   return {yq, yk};
 }
 
@@ -145,8 +168,8 @@ TurnedGrads turned_back(const at::Tensor& gq, const at::Tensor& gk, const at::Te
   };
   check_input(q, gq, x.q_weight, "q");
   check_input(k, gk, x.k_weight, "k");
-  if (dq) check_out(*dq, gq, "dq");
-  if (dk) check_out(*dk, gk, "dk");
+  if (dq) check_result(*dq, gq, "dq");
+  if (dk) check_result(*dk, gk, "dk");
   const at::Tensor& ref = gq.defined() ? gq : gk;
   const c10::DeviceGuard guard(ref.device());
   TurnedGrads r;
@@ -163,6 +186,8 @@ TurnedGrads turned_back(const at::Tensor& gq, const at::Tensor& gk, const at::Te
      api.rotary_backward(&p, &vq, &vk, &vgq, &vgk, &vdq, &vdk, r.q_weight.defined() ? r.q_weight.data_ptr() : nullptr,
                          r.k_weight.defined() ? r.k_weight.data_ptr() : nullptr, need ? ws.data_ptr() : nullptr, need,
                          stream_of(ref)));
+  written(dq);
+  written(dk);
   return r;
 }
 
@@ -290,6 +315,7 @@ void cache_write(const at::Tensor& data, int64_t page_size, int64_t d, const at:
   const c10::DeviceGuard guard(data.device());
   const mra_strided_t vk = view(k), vv = view(v);
   ok("mra_fp4_cache_write", api.cache_write(&c, &vk, &vv, (int)k.size(2), dtype, s, n, stream_of(data)));
+  written(data);
 }
 
 // ops.fp4_cache_read
@@ -309,7 +335,7 @@ std::tuple<at::Tensor, at::Tensor> cache_read(const at::Tensor& data, int64_t pa
       TORCH_CHECK_VALUE(out[i].sizes() == shape && out[i].scalar_type() == type && out[i].device() == data.device(),
                         i ? "v_out" : "k_out", " must be a tensor of dtype and shape ", tuple_of(shape),
                         on(data.device()));
-      check_out(out[i], out[i], i ? "v_out" : "k_out");
+      check_result(out[i], out[i], i ? "v_out" : "k_out");
     } else {
       out[i] = at::empty(shape, data.options().dtype(type));
     }
@@ -318,6 +344,8 @@ std::tuple<at::Tensor, at::Tensor> cache_read(const at::Tensor& data, int64_t pa
   const int32_t *s = ints(starts, c.B, "starts", data.device()), *m = ints(counts, c.B, "counts", data.device());
   const mra_strided_t vk = view(out[0]), vv = view(out[1]);
   ok("mra_fp4_cache_read", api.cache_read(&c, &vk, &vv, (int)n, dtype, s, m, stream_of(data)));
+  written(k_out);
+  written(v_out);
   return {out[0], out[1]};
 }
 
@@ -357,7 +385,7 @@ at::Tensor attention(const at::Tensor& data, int64_t page_size, int64_t d, const
                      const Opt& out, const Opt& lse_out, const Opt& workspace) {
   const mra_fp4_cache_t c = cache_of(data, page_size, d, table);
   const mra_fp4_attention_t p = attention_problem(c, data, q, lengths, scale, causal, q_start);
-  if (out) check_out(*out, q, "out");
+  if (out) check_result(*out, q, "out");
   const c10::DeviceGuard guard(q.device());
   const at::Tensor z = out ? *out : rows_like(q);
   float* lse = nullptr;
@@ -365,6 +393,7 @@ at::Tensor attention(const at::Tensor& data, int64_t page_size, int64_t d, const
     TORCH_CHECK_VALUE(lse_out->scalar_type() == at::kFloat && lse_out->sizes() == q.sizes().slice(0, 3) &&
                           lse_out->is_contiguous() && lse_out->device() == q.device(),
                       "lse_out must be a contiguous float32 device tensor of shape ", tuple_of(q.sizes().slice(0, 3)));
+    check_graph(*lse_out, "lse_out");
     lse = static_cast<float*>(lse_out->data_ptr());
   }
   at::Tensor ws;
@@ -378,6 +407,8 @@ at::Tensor attention(const at::Tensor& data, int64_t page_size, int64_t d, const
   const mra_strided_t vq = view(q), vo = view(z);
   ok("mra_fp4_attention", api.attention(&c, &p, &vq, &vo, lse, ws.defined() ? ws.data_ptr() : nullptr,
                                         ws.defined() ? ws.nbytes() : 0, stream_of(q)));
+  written(out);
+  written(lse_out);
   return z;
 }
 

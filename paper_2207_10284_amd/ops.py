@@ -939,7 +939,8 @@ def rotary_forward(q, k=None, freqs=None, *, positions=None, interleaved: bool =
     none: no rotation. ``positions``: int32 [n] or [B, n], 0 to n - 1 if not given. With
     ``q_weight`` or ``k_weight`` ([d], float32 or q's dtype) a row x is x / sqrt(mean(x^2) + eps) times the weight
     before it is turned. ``q_out`` may be q and ``k_out`` k: changed in place; they
-    overlap no other argument."""
+    overlap no other argument. A tensor given for a result, here and in the calls below, must not require a gradient (it may
+    under ``torch.no_grad``), and autograd sees that it was written."""
     return bind_layer().rotary_forward(q, k, freqs, positions, interleaved, magnitude, q_weight, k_weight, eps,
                                        _result(q, q_out), k_out if k is None else _result(k, k_out))
 
