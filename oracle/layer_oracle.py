@@ -3,12 +3,21 @@ any device), written from the definitions of mra_layer.h: the oracle of their te
 import torch
 
 GRID = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0)
+# 2 pi = TURN[0] + TURN[1] + TURN[2], the first of 23 bits: exact times a number of turns below 2^30
+TURN = (float.fromhex("0x1.921fb4p+2"), float.fromhex("0x1.4442d18469899p-22"), float.fromhex("-0x1.9d747f23e32edp-77"))
 
 
 def angles(n, freqs, positions, magnitude=1.0):
-    """cos and sin times the magnitude, [B or 1, 1, n, r / 2]."""
+    """cos and sin times the magnitude, [B or 1, 1, n, r / 2]. Positions have 32 bits, so their product with a
+    frequency's first 21 bits is exact; whole turns leave it before the rest comes in, and the angle is
+    off by less than 2^-40 at every position (a float64 product: by 2^-23 at 2^31)."""
     p = torch.arange(n, device=freqs.device) if positions is None else positions
-    t = (p if p.dim() == 2 else p[None]).double()[:, None, :, None] * freqs.double()
+    p, f = (p if p.dim() == 2 else p[None]).double()[:, None, :, None], freqs.double()
+    c = f * (2.0 ** 32 + 1)
+    first = c - (c - f)
+    t = p * first
+    k = torch.round(t / (TURN[0] + TURN[1]))
+    t = ((t - k * TURN[0]) - k * TURN[1]) - k * TURN[2] + p * (f - first)
     return torch.cos(t) * magnitude, torch.sin(t) * magnitude
 
 
