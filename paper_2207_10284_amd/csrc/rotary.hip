@@ -2,7 +2,7 @@
 //
 // Bound by memory: an element is read and written once (backward with a norm: two read, one
 // written) for some ten operations. What is left to do is to keep the angles
-// cheap, a float64 product and a sine and cosine each: a workgroup takes a tile of
+// cheap, some float64 products and a sine and cosine each: a workgroup takes a tile of
 // tokens with all their heads, makes the tile's sines and cosines once in LDS, and
 // its rows read them there. Measured on data that no cache holds: 8 x 24 heads x 4096 x 64 bfloat16, forward or backward
 // 41 us (201 MB, 4.9 TB/s, 97% of a large copy's rate); 20 heads x 32768 x 128 bfloat16 with norms, forward 62 us (336 MB,
@@ -103,15 +103,19 @@ struct Tile {
   }
 };
 
-// cos and sin (times the magnitude) of the tile's tokens and frequencies. Tokens are below 2^27.
+// cos and sin (times the magnitude) of the tile's tokens and frequencies. Tokens are below 2^27. What is
+// left of pos freq / (2 pi) without its whole turns is off by some 2^-53 of a turn, not of all turns: the
+// frequency in turns is the sum of two float64 values, and whole turns leave the product before it is rounded.
 __device__ __forceinline__ void fill_angles(const RotaryArgs& a, int first, int tokens, float2* cs) {
   const int half = a.rot / 2;                      // a multiple of eight, at most 64, not always a power of two
   for (int i = threadIdx.x; i < tokens * half; i += kThreads) {
     const int t = i / half, f = i - t * half;
     const int b = (first + t) / a.n, n = first + t - b * a.n;
-    const int pos = a.positions == nullptr ? n : a.positions[b * a.positions_stride + n];
-    double turns = (double)pos * (a.freqs[f] * 0.15915494309189535);
-    turns -= rint(turns);
+    const double pos = a.positions == nullptr ? n : a.positions[b * a.positions_stride + n];
+    constexpr double kHigh = 0x1.45f306dc9c883p-3, kLow = -0x1.6b01ec5417056p-57;   // 1 / (2 pi)
+    const double freq = a.freqs[f], high = freq * kHigh, low = fma(freq, kHigh, -high) + freq * kLow;
+    double turns = fma(pos, low, fma(pos, high, -rint(pos * high)));
+    turns -= rint(turns);                          // one more, or those of products past 2^53
     float s, c;
     sincospif(2.0f * (float)turns, &s, &c);
     cs[i] = float2{c * a.magnitude, s * a.magnitude};
