@@ -41,8 +41,8 @@ extern "C" {
  * Pair i is the elements i and i + rot/2, or 2i and 2i + 1 (interleaved). The elements
  * from rot on stay as they are.
  *
- * The angle is taken in turns, p f / (2 pi) in float64, and rounded to float32 only
- * after its whole turns are gone, so far positions are as exact as near ones. Of rows with a
+ * The angle p f is taken in turns, in float64, and its whole turns leave it before it is rounded; cosine and sine are
+ * float32, off by some 2^-23 at every position, far or near. Of rows with a
  * norm the mean square is within float32's range.
  */
 typedef struct {

@@ -116,9 +116,12 @@ __device__ __forceinline__ void fill_angles(const RotaryArgs& a, int first, int 
     const double freq = a.freqs[f], high = freq * kHigh, low = fma(freq, kHigh, -high) + freq * kLow;
     double turns = fma(pos, low, fma(pos, high, -rint(pos * high)));
     turns -= rint(turns);                          // one more, or those of products past 2^53
+    // sine and cosine of the float32 part, turned by the rest of at most 2^-26 turns (without it they are off by up to
+    // 1.1e-7, with it 7.8e-8; both make the same time)
+    const float near = (float)turns, rest = (float)((turns - near) * 6.283185307179586);
     float s, c;
-    sincospif(2.0f * (float)turns, &s, &c);
-    cs[i] = float2{c * a.magnitude, s * a.magnitude};
+    sincospif(2.0f * near, &s, &c);
+    cs[i] = float2{fmaf(-s, rest, c) * a.magnitude, fmaf(c, rest, s) * a.magnitude};
   }
 }
 

@@ -51,3 +51,21 @@ def test_gradients_turn_back_as_far(gpu):
     mag = L.turn(x, f, p, back=True, absolute=True)
     got = gpu.rotary_backward(x, None, freqs=f, positions=p)[0]
     assert bool(((got.double() - want).abs() <= (BAR + 2.0 ** -23) * mag).all())
+
+
+@pytest.mark.parametrize("where", [0, 2 ** 31 - 70000])
+def test_the_angle_is_not_rounded_to_float32(gpu, where):
+    """Without the angle's rounding what is left is that of sine and cosine. Errors of a vector (cosine, sine) along its
+    turn are the angle's: their mean square over many angles, each off by up to 2^-26 turns, evenly, would be
+    (2 pi 2^-26)^2 / 3 for turns of 1/4 to 1/2 alone; the results' rounding, 2^-25 at most, adds less than 2^-50 / 3 along it,
+    and sine and cosine, where correct to one unit, at most as much again twice."""
+    n, d = 60000, 32
+    f = frequencies(gpu, "any", d)
+    p = torch.arange(where, where + n, device="cuda").to(torch.int32)
+    x = torch.zeros(1, 1, 1, d, device="cuda")
+    x[..., : d // 2] = 1.0
+    y = gpu.rotary_forward(x.expand(1, 1, n, d), None, f, positions=p)[0].double()
+    cos, sin = L.angles(n, f, p)
+    along = (y[..., d // 2:] - sin) * cos - (y[..., : d // 2] - cos) * sin
+    quarter = cos < 0                                      # turns of 1/4 to 1/2, where float32's are rounded most
+    assert along[quarter].square().mean().item() < (2 * 3.1416 * 2.0 ** -26) ** 2 / 3
