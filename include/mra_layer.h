@@ -13,7 +13,7 @@
  *   bytes. Input strides may be 0. Outputs must not overlap themselves or, where
  *   not said otherwise, another argument.
  * - d is 32, 64 or 128; rotary calls have below 2^27 tokens (B n); writing and reading the
- *   cache, sequences times key heads times tiles of 32 tokens are below 2^24; attention has at most
+ *   cache, sequences times key heads times tiles of 64 tokens, (n + 62) / 64 + 1, are below 2^24; attention has at most
  *   2^30 rows (B H n_q) and below 2^23 row tiles (16 rows of a key head up to 64 of them, else 128);
  *   heads are at most 2^16.
  * - Everything is computed in float32 (angles in float64)

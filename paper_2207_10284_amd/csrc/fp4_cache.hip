@@ -144,9 +144,10 @@ __global__ __launch_bounds__(kThreads) void fp4_read_kernel(CacheRowsArgs a, int
   }
 }
 
-// Tiles that n tokens can touch.
+int cache_row_tiles(int n) { return (n + kTokens - 2) / kTokens + 1; }
+
 static unsigned row_groups(const CacheRowsArgs& a, int* tiles) {
-  *tiles = (a.n + kTokens - 2) / kTokens + 1;
+  *tiles = cache_row_tiles(a.n);
   return (unsigned)((long long)a.B * a.c.Hkv * *tiles);
 }
 

@@ -150,7 +150,7 @@ mra_status_t cache_rows(const mra_fp4_cache_t* cache, const mra_strided_t* k, co
   MRA_TRY(check_dtype(dtype));
   if (n < 0) return MRA_ERR_INVALID_ARG;
   if (n > kMaxLen) return MRA_ERR_UNSUPPORTED;
-  if ((long long)cache->B * cache->H_kv > kMaxGroups / ((n + 30) / 32 + 1)) return MRA_ERR_UNSUPPORTED;
+  if ((long long)cache->B * cache->H_kv > kMaxGroups / mra::cache_row_tiles(n)) return MRA_ERR_UNSUPPORTED;
   if (cache->B == 0 || cache->H_kv == 0 || n == 0) return MRA_OK;
   if (!read && (cache->pages == 0 || cache->max_pages == 0)) return MRA_OK;
   MRA_TRY(check_cache_memory(cache));

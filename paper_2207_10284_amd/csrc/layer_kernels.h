@@ -50,6 +50,8 @@ struct CacheRowsArgs {
   const int32_t *starts, *counts;
 };
 
+// Workgroups of one head: tiles of tokens that n neighbouring ones can touch.
+int cache_row_tiles(int n);
 hipError_t launch_cache_write(const CacheRowsArgs& a, int d, int dtype, hipStream_t stream);
 hipError_t launch_cache_read(const CacheRowsArgs& a, int d, int dtype, hipStream_t stream);
 
