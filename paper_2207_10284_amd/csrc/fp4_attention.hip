@@ -60,36 +60,25 @@ template <int D, int T>
 struct CacheStage {
   using Pg = Fp4Page<D>;
   static constexpr int kKeys = 128 * D;            // bytes of the keys in LDS; the values take as many
-  // 16 bytes of codes, a block, per lane: with fewer lanes than blocks a lane has keys and values
-  static constexpr int U = 2 * D, N = 2 * U > T ? 2 : 1;
-  static_assert(N == 1 || U == T, "a lane has one unit of either, or of one of them");
+  using Unit = Fp4StageUnit<D, T>;
+  static constexpr int N = Unit::N;
   u32x4 w[N];
   uint32_t e[N];
-
-  // Unit n of a lane: keys or values (x), token and block; false: none. 16 lanes' stores of a chunk reach every bank once:
-  // neighbouring tokens are four units apart (in their order: 4-way conflicts).
-  static __device__ __forceinline__ bool unit(int n, int tid, int& x, int& r, int& blk) {
-    const int u = tid % U, t = u / Pg::NB;
-    x = N == 2 ? n : tid / U;
-    r = (t & 48) | (t & 3) << 2 | (t >> 2 & 3);
-    blk = u % Pg::NB;
-    return x < 2;
-  }
 
   // pg: the pages of the two halves of the stage, null where no key counts
   __device__ __forceinline__ void load(const char* (&pg)[2], int k0, int size, int tid) {
     const int slot0 = k0 & (size - 1), slot1 = (k0 + 32) & (size - 1);
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      int x, r, blk;
-      if (!unit(n, tid, x, r, blk)) continue;
-      const char* p = r < 32 ? pg[0] : pg[1];
-      const int slot = (r < 32 ? slot0 : slot1) + r % 32;
+      const Unit u(n, tid);
+      if (u.x > 1) continue;
+      const char* p = u.r < 32 ? pg[0] : pg[1];
+      const int slot = (u.r < 32 ? slot0 : slot1) + u.r % 32;
       w[n] = u32x4{0, 0, 0, 0};
       e[n] = 127;
       if (p != nullptr) {
-        w[n] = *reinterpret_cast<const u32x4*>(p + Pg::codes(x, size) + slot * (D / 2) + blk * 16);
-        e[n] = (uint8_t)p[Pg::steps(x, size) + slot * Pg::NB + blk];
+        w[n] = *reinterpret_cast<const u32x4*>(p + Pg::codes(u.x, size) + slot * (D / 2) + u.blk * 16);
+        e[n] = (uint8_t)p[Pg::steps(u.x, size) + slot * Pg::NB + u.blk];
       }
     }
   }
@@ -98,13 +87,13 @@ struct CacheStage {
   __device__ __forceinline__ void store(char* lds, const RowBits<64>& ok, int tid) const {
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      int x, r, blk;
-      if (!unit(n, tid, x, r, blk)) continue;
-      const float step = fp4_step(ok.all() || ok.row(r) ? e[n] : 127);
-      char* to = lds + x * kKeys + (r >> 5) * kTileBytes<D>;
+      const Unit u(n, tid);
+      if (u.x > 1) continue;
+      const float step = fp4_step(ok.all() || ok.row(u.r) ? e[n] : 127);
+      char* to = lds + u.x * kKeys + (u.r >> 5) * kTileBytes<D>;
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        *reinterpret_cast<u32x4*>(to + raw_offset<D, exact_swz<D>>(r & 31, 32 * blk + 8 * j)) = fp4_decode(w[n][j], step);
+        *reinterpret_cast<u32x4*>(to + raw_offset<D, exact_swz<D>>(u.r & 31, 32 * u.blk + 8 * j)) = fp4_decode(w[n][j], step);
     }
   }
 };
@@ -325,10 +314,7 @@ struct CacheTile {
   using Pg = Fp4Page<D>;
   uint32_t w[2][2][D / 32], e[2][2];               // keys and values, x
 
-  static __device__ __forceinline__ int row(int value, int x) {
-    const int i = lane_id() & 15;
-    return value ? 16 * x + i : 8 * (i >> 2) + 4 * x + (i & 3);
-  }
+  static __device__ __forceinline__ int row(int value, int x) { return fp4_tile_row(value, x, lane_id() & 15); }
 
   // A lane's offsets are the same for every tile: uniform bases, so that a load needs no vector instruction.
   __device__ __forceinline__ void load(const char* page, int slot, int size) {
@@ -357,22 +343,16 @@ struct CacheTile {
   }
 };
 
-// A wave's 32 values of D channels in LDS (256-byte aligned), rows of bfloat16. A row's blocks of 16 channels, and the halves of a block,
-// are exchanged by row so that neither the stores of 8 rows at a time nor the transposing reads of 4 or 8 meet in a bank
-// (none counted at d = 128; at d = 64 32 cycles a tile are, of 96, whatever of the rows' bits decides, and cost no time).
+// A wave's 32 values of D channels in LDS (256-byte aligned), laid out by fp4_value_place.
 template <int D>
 struct ValueTile {
   uint32_t to, from[2];                            // this lane's first chunk of a row; transposed rows + 0 and + 4
 
-  static __device__ __forceinline__ int place(int r, int c) {    // of channel c, a multiple of 4
-    const int f = D == 128 ? (r & 3) | (r >> 3 & 1) << 2 : D == 64 ? (r >> 1 & 1) | (r >> 3 & 1) << 1 : r >> 3 & 1;
-    return r * 2 * D + (((c >> 4) ^ f) << 5) + (((c >> 3 & 1) ^ (r >> 2 & 1)) << 4) + (c & 4) * 2;
-  }
   __device__ __forceinline__ void init(const char* lds) {
     const int lane = lane_id(), g = lane >> 4, i = lane & 15;
-    to = lds_addr(lds) + place(i, g * (D / 4));
+    to = lds_addr(lds) + fp4_value_place<D>(i, g * (D / 4));
 #pragma unroll
-    for (int e = 0; e < 2; ++e) from[e] = lds_addr(lds) + place(8 * g + 4 * e + (i >> 2), 4 * (i & 3));
+    for (int e = 0; e < 2; ++e) from[e] = lds_addr(lds) + fp4_value_place<D>(8 * g + 4 * e + (i >> 2), 4 * (i & 3));
   }
   // chunk n (8 channels) of this lane's row 16 x + lane % 16
   __device__ __forceinline__ void put(int x, int n, const u32x4& v) const {

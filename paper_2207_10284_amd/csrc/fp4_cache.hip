@@ -14,7 +14,7 @@ namespace {
 
 constexpr int kThreads = 256;
 
-constexpr int kTokens = 64;                       // of a workgroup's tile
+constexpr int kTokens = kFp4RowTokens;
 
 // Which tokens of a workgroup's tile a call writes or reads.
 struct Span {
@@ -79,72 +79,70 @@ __device__ __forceinline__ void store8(char* p, uint32_t w, float step) {
 
 template <int DT, int D>
 __global__ __launch_bounds__(kThreads) void fp4_write_kernel(CacheRowsArgs a, int tiles) {
-  using Pg = Fp4Page<D>;
-  constexpr int CPR = D / 16, E = DT == BF16 ? 2 : 4;
-  constexpr int N = 2 * kTokens * CPR / kThreads;  // units of sixteen channels per lane
+  using Unit = Fp4RowUnit<D, 16>;
+  constexpr int E = DT == BF16 ? 2 : 4, N = Unit::kUnits / kThreads;
   Span s = span_of(a, tiles);
   if (s.lo >= s.hi) return;
   const int tid = threadIdx.x, size = 1 << a.c.page_log2;
   float f[N][2][8];                                // on their way while the table is looked up
 #pragma unroll
   for (int u = 0; u < N; ++u) {
-    const int unit = u * kThreads + tid, value = unit / (kTokens * CPR), r = unit / CPR % kTokens, c = unit % CPR;
-    const Rows& x = value ? a.v : a.k;
-    const int t = min(max(s.t0 + r, s.lo), s.hi - 1);
-    const char* p = x.p + s.b * x.sb + s.hk * x.sh + (t - s.start) * x.sn + c * 16 * E;
+    const Unit at(u * kThreads + tid);
+    const Rows& x = at.value ? a.v : a.k;
+    const int t = min(max(s.t0 + at.r, s.lo), s.hi - 1);
+    const char* p = x.p + s.b * x.sb + s.hk * x.sh + (t - s.start) * x.sn + at.c * 16 * E;
     load8<DT>(p, f[u][0]);
     load8<DT>(p + 8 * E, f[u][1]);
   }
   s.pages(a);
 #pragma unroll
   for (int u = 0; u < N; ++u) {
-    const int unit = u * kThreads + tid, value = unit / (kTokens * CPR), r = unit / CPR % kTokens, c = unit % CPR;
+    const Unit at(u * kThreads + tid);
     float top = 0.0f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) top = fmaxf(top, fmaxf(fabsf(f[u][0][e]), fabsf(f[u][1][e])));
     top = fmaxf(top, __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(top), 0xB1, 0xF, 0xF, true)));   // lane ^ 1
     const uint32_t ex = fp4_exponent(top);
-    char* page = r < 32 ? s.page[0] : s.page[1];
-    const int t = s.t0 + r, slot = t & (size - 1);
+    char* page = at.r < 32 ? s.page[0] : s.page[1];
+    const int t = s.t0 + at.r, slot = t & (size - 1);
     if (page == nullptr || t < s.lo || t >= s.hi) continue;
-    *reinterpret_cast<u32x2*>(page + Pg::codes(value, size) + slot * (D / 2) + c * 8) =
+    *reinterpret_cast<u32x2*>(page + at.codes_at(slot, size)) =
         u32x2{fp4_encode(f[u][0], fp4_step(ex)), fp4_encode(f[u][1], fp4_step(ex))};
-    if (c % 2 == 0) page[Pg::steps(value, size) + slot * Pg::NB + c / 2] = (char)ex;
+    if (at.c % 2 == 0) page[at.step_at(slot, size)] = (char)ex;
   }
 }
 
 template <int DT, int D>
 __global__ __launch_bounds__(kThreads) void fp4_read_kernel(CacheRowsArgs a, int tiles) {
-  using Pg = Fp4Page<D>;
-  constexpr int CPR = D / 8, E = DT == BF16 ? 2 : 4;
-  constexpr int N = 2 * kTokens * CPR / kThreads;
+  using Unit = Fp4RowUnit<D, 8>;
+  constexpr int E = DT == BF16 ? 2 : 4, N = Unit::kUnits / kThreads;
   Span s = span_of(a, tiles);
   s.pages(a);
   const int tid = threadIdx.x, size = 1 << a.c.page_log2;
   uint32_t w[N], ex[N];
 #pragma unroll
   for (int u = 0; u < N; ++u) {
-    const int unit = u * kThreads + tid, value = unit / (kTokens * CPR), r = unit / CPR % kTokens, c = unit % CPR;
-    const char* page = r < 32 ? s.page[0] : s.page[1];
-    const int t = s.t0 + r, slot = t & (size - 1);
+    const Unit at(u * kThreads + tid);
+    const char* page = at.r < 32 ? s.page[0] : s.page[1];
+    const int t = s.t0 + at.r, slot = t & (size - 1);
     w[u] = 0;
     ex[u] = 127;
     if (page != nullptr && t < s.hi) {
-      w[u] = *reinterpret_cast<const uint32_t*>(page + Pg::codes(value, size) + slot * (D / 2) + c * 4);
-      ex[u] = (uint8_t)page[Pg::steps(value, size) + slot * Pg::NB + c / 4];
+      w[u] = *reinterpret_cast<const uint32_t*>(page + at.codes_at(slot, size));
+      ex[u] = (uint8_t)page[at.step_at(slot, size)];
     }
   }
 #pragma unroll
   for (int u = 0; u < N; ++u) {
-    const int unit = u * kThreads + tid, value = unit / (kTokens * CPR), r = unit / CPR % kTokens, c = unit % CPR;
-    const int i = s.t0 + r - s.start;
+    const Unit at(u * kThreads + tid);
+    const int i = s.t0 + at.r - s.start;
     if (i < 0 || i >= a.n) continue;
-    const Rows& x = value ? a.v : a.k;
-    store8<DT>(x.p + s.b * x.sb + s.hk * x.sh + i * x.sn + c * 8 * E, w[u], fp4_step(ex[u]));
+    const Rows& x = at.value ? a.v : a.k;
+    store8<DT>(x.p + s.b * x.sb + s.hk * x.sh + i * x.sn + at.c * 8 * E, w[u], fp4_step(ex[u]));
   }
 }
 
-int cache_row_tiles(int n) { return (n + kTokens - 2) / kTokens + 1; }
+int cache_row_tiles(int n) { return fp4_row_tiles(n); }
 
 static unsigned row_groups(const CacheRowsArgs& a, int* tiles) {
   *tiles = cache_row_tiles(a.n);

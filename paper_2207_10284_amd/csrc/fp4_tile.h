@@ -4,18 +4,11 @@
 #pragma once
 
 #include "common.h"
+#include "fp4_layout.h"
 #include "layer_kernels.h"
 #include "tile_ops.h"
 
 namespace mra {
-
-// Offsets in bytes within a page of one head, of `size` tokens; x = 0: keys, 1: values.
-template <int D>
-struct Fp4Page {
-  static constexpr int NB = D / 32;                // blocks, and step bytes, of a token
-  static __device__ __forceinline__ int codes(int x, int size) { return x * size * (D / 2); }
-  static __device__ __forceinline__ int steps(int x, int size) { return size * (D + x * NB); }
-};
 
 // The page of a head that holds token t of sequence b (t below the table's end), or null.
 __device__ __forceinline__ char* fp4_page(const CacheArgs& c, int b, int hk, int t) {
