@@ -1024,7 +1024,7 @@ class Fp4Cache:
 
     def __init__(self, data, page_size: int, d: int):
         page_size, d = int(page_size), int(d)
-        if page_size < 0 or d < 0 or max(page_size, d) >= 1 << 31 or not (need := fp4_page_bytes(page_size, d)):
+        if not (need := fp4_page_bytes(page_size, d)):
             raise ValueError("page_size must be 32, 64, .. 1024 and d 32, 64 or 128")
         if data.dtype != torch.uint8 or data.dim() != 3 or data.shape[2] != need or not data.is_contiguous():
             raise ValueError(f"data must be a contiguous uint8 tensor [pages, H_kv, {need}]")
@@ -1036,12 +1036,14 @@ class Fp4Cache:
 
 def fp4_page_bytes(page_size: int, d: int) -> int:
     """Bytes of one page of one head: 17/32 byte a value (0: sizes that are not supported)."""
+    if not (0 <= page_size < 1 << 31 and 0 <= d < 1 << 31):      # what the library's integers hold
+        return 0
     return int(load_layer().mra_fp4_page_bytes(page_size, d))
 
 
 def fp4_cache(pages: int, kv_heads: int, page_size: int, d: int, device="cuda") -> Fp4Cache:
     """An empty cache of ``pages`` pages (all values 0). page_size: a power of two from 32 to 1024."""
-    if page_size < 0 or d < 0 or max(page_size, d) >= 1 << 31 or not (need := fp4_page_bytes(page_size, d)):
+    if not (need := fp4_page_bytes(page_size, d)):
         raise ValueError("page_size must be 32, 64, .. 1024 and d 32, 64 or 128")
     return Fp4Cache(torch.zeros(pages, kv_heads, need, dtype=torch.uint8, device=device), page_size, d)
 

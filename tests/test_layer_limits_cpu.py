@@ -17,3 +17,10 @@ def test_cache_calls_of_every_size_that_fits(n, read):
         if most >= H:
             assert rows(lib, cache(B=most // H, H_kv=H), n=n, read=read, k=tensor(None)) == INVALID
         assert rows(lib, cache(B=most // H + 1, H_kv=H), n=n, read=read, k=tensor(None)) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("size,d", [((1 << 32) + 32, 64), (32 - (1 << 32), 64), (32, (1 << 32) + 64), (1 << 70, 64), (-32, 64)])
+def test_pages_of_sizes_past_32_bits(size, d):
+    assert ops.fp4_page_bytes(size, d) == 0
+    with pytest.raises(ValueError, match="page_size"):
+        ops.fp4_cache(2, 2, size, d, device="cpu")
