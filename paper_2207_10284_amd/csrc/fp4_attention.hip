@@ -9,8 +9,10 @@
 // together, 64 at a time. Codes come through registers and are converted once per workgroup, to
 // bfloat16 rows in LDS in the order and swizzle of the exact kernels, whose transposing reads give the second
 // product's operand. What bounds it is a stage's vector work (exponentials, packing, conversion) beside its matrix work, two waves a
-// SIMD: at 2 x 16 heads on 4, 512 queries on up to 16384 keys x 128 bfloat16, 115 us and the join 8 (820 TFLOP/s, 61% of
-// a large product's rate; matrix cores busy 36%, vector ALU 33%, waves waiting 27% of their time).
+// SIMD: 2 x 16 heads on 4, 512 queries on up to 16384 keys x 128 bfloat16, with the join's 8 us, 119 to 146 us by the lengths
+// (equal ones 850 to 890 TFLOP/s, 63 to 66% of a large product's rate, unequal ones 710 to 840: each sequence has the same number of
+// parts; matrix cores busy 36%, vector ALU 34%, waves waiting 26% of their time); 8 x 12 heads x 2048 x 64, causal, 72 to 77 us
+// (matrix cores busy 27%, vector ALU 56%, waves waiting 29%).
 //
 // fp4_token_kernel: few rows, single tokens above all. A wave takes 16 rows and 32 keys at a time on the
 // 16x16x32 matrix instructions. Keys go from memory to registers as the first product takes them; values
@@ -19,6 +21,12 @@
 // (exact_join_kernel adds them). What bounds it is the cache's bytes and, as much, the chain from tile to tile within a
 // wave: one token of 32 x 12 heads on up to 4096 keys x 64, 20 us (80 MB, 4.0 TB/s; loads alone, without any products, take
 // 2.5 us less) and the join 4; 4 x 16 heads on 4, up to 32768 x 128, 13 to 15 us (53 MB) and the join 4.
+//
+// Weights of bfloat16 calls are rounded to bfloat16 for the second product, and their sums are of the rounded ones: a weight is off
+// by 2^-9 at most, as much as the result's own rounding, and the 2-norm of a result's error is 2.0 to 2.3e-3 of the result's where
+// that rounding alone gives 1.6e-3. As sums of two bfloat16 values they cost single tokens 4 to 6% (32 x 12 heads on up to
+// 4096 x 64: 26.7 -> 27.6 us, 4 x 16 heads on 4, up to 32768 x 128: 18.5 -> 19.7) and prompts 24 to 40% (the two calls
+// above: 137 -> 171, 86 -> 120). Float32 queries are for the caller who wants more.
 #include "exact_rows.h"
 #include "fp4_tile.h"
 

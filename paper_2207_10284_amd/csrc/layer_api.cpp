@@ -99,7 +99,8 @@ mra::RotaryArgs rotary_args(const mra_rotary_problem_t& p) {
   return a;
 }
 
-// Rows of one side are taken as they lie: `t` is what its loads go by.
+// Rows of one side are taken as they lie: `t` is what its loads go by. (Single tokens, whose stride is 0, are taken head by
+// head over the batches.)
 void order(mra::RotarySide& s, const mra::Rows& t, int heads) {
   s.heads = heads;
   s.head_fast = t.sh < t.sn;
